@@ -35,7 +35,8 @@
  *     synchronises its stream and returns PR2_ERR_ROUTE if any id was out of range or
  *     repeated within its row (PR2_ERR_UNSUPPORTED, nothing enqueued, if the stream is
  *     being captured into a HIP graph).
- *   - Inputs must be finite; NaN or Inf give unspecified (but memory-safe) results.
+ *   - Inputs must be finite; NaN or Inf give unspecified (but memory-safe) results, except
+ *     where a call says what they give.
  */
 #ifndef PR2_H
 #define PR2_H
@@ -66,8 +67,9 @@ typedef enum {
 /* act_dtype: storage type of activations (x, y, dy, dx) and expert weights.
  * The router W_r, its bias, the predictor factors A, B, gates and logits are always fp32. */
 enum { PR2_F32 = 0, PR2_BF16 = 1 };
-/* idx_dtype: storage type of recorded expert ids. */
-enum { PR2_I32 = 0, PR2_I16 = 1 };
+/* idx_dtype: storage type of recorded expert ids; token_dtype: of sampled token ids
+ * (PR2_I32 or PR2_I64). */
+enum { PR2_I32 = 0, PR2_I16 = 1, PR2_I64 = 2 };
 /* op codes for pr2_workspace_bytes. */
 enum {
     PR2_OP_ROUTE = 0,
@@ -75,7 +77,8 @@ enum {
     PR2_OP_REPLAY_BWD = 2,
     PR2_OP_ROLLOUT_FWD = 3,
     PR2_OP_ROUTE_DIAG = 4,
-    PR2_OP_PREDICTOR_LOSS = 5
+    PR2_OP_PREDICTOR_LOSS = 5,
+    PR2_OP_DISPATCH_PLAN = 6
 };
 
 /*
@@ -398,6 +401,192 @@ pr2_status pr2_predictor_loss(const pr2_moe_desc* desc, const void* h, const flo
                               const float* A, const float* B, int loss_kind, int mini_step,
                               float* kl_out, float* loss_out, float* dA, float* dB, void* ws,
                               size_t ws_bytes, pr2_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The policy's loss on the sampled tokens (Sec. 2, the clipped objective with a KL regulariser
+ * that the method is trained with; Appendix E.1: clip bounds 0.2 below and 0.28 above).
+ *
+ * Row t of the logits belongs to sampled token y_t.  With z = logits[t, 0..V) and
+ * s = inv_temp (1 / sampling temperature):
+ *   logp_t    = s z_y - log sum_v exp(s z_v),   p_v = exp(s z_v) / sum exp(s z),
+ *   entropy_t = -sum_v p_v log p_v,
+ *   ratio r_t = exp(logp_t - logp_old_t),
+ *   surr_t    = min(r_t A_t, clamp(r_t, 1 - clip_low, 1 + clip_high) A_t),
+ *   kl_t      = exp(d_t) - d_t - 1 with d_t = logp_ref_t - logp_t   (0 without logp_ref),
+ *   loss      = sum_t w_t (-surr_t + kl_coef kl_t),
+ *   coef_t    = d loss / d logp_t
+ *             = w_t (-A_t r_t [not clipped] + kl_coef (1 - exp(d_t))),   clipped meaning
+ *               A_t > 0 and r_t > 1 + clip_high, or A_t < 0 and r_t < 1 - clip_low,
+ *   dlogits[t, v] = coef_t s ([v = y_t] - p_v).
+ * A_t = 0 has surr_t = 0 and no gradient through it, whatever r_t is.
+ *
+ * A row counts only if w_t != 0, 0 <= y_t < V and some logit of it is above -infinity.  Any
+ * other row has loss, logp, entropy and coef 0 and a gradient of zeros, whatever stands in its
+ * other inputs (NaN included); its lse is -infinity.  A logit of -infinity (an id that may not
+ * be sampled) has probability 0.  NaN or +infinity in a row that counts make that row's
+ * results NaN.
+ *
+ * T rows (>= 0, below 2^25), V vocabulary size (>= 1), ldl and ldd (>= V) the row strides in
+ * elements of logits and dlogits (ldd is read only by calls that write dlogits), act_dtype of
+ * both, token_dtype PR2_I32 or PR2_I64 of the ids, inv_temp > 0, clip_low, clip_high and
+ * kl_coef >= 0, all finite.  Logits and gradients need only their element's alignment, rows
+ * may start anywhere.
+ * Per-token tensors are [T] fp32, contiguous.
+ */
+typedef struct {
+    int64_t T, ldl, ldd;
+    int32_t V;
+    int32_t act_dtype;
+    int32_t token_dtype;
+    float inv_temp;
+    float clip_low, clip_high;
+    float kl_coef;
+} pr2_policy_desc;
+
+/* Bytes of workspace that pr2_token_logprob and pr2_policy_loss need for this descriptor
+ * (0 for an invalid one, which the call then reports).  Does not decrease with T. */
+size_t pr2_policy_workspace_bytes(const pr2_policy_desc* desc);
+
+/*
+ * Log-probability of the sampled tokens, for the rollout's record and for the passes that
+ * form logp_old and logp_ref.  clip_low, clip_high, kl_coef and ldd are not read.
+ *   logits [T, V] act_dtype;  token [T]
+ *   logp_out [T];  lse_out [T] log sum_v exp(s z_v) or NULL;  entropy_out [T] or NULL
+ *   ws >= pr2_policy_workspace_bytes(desc)
+ */
+pr2_status pr2_token_logprob(const pr2_policy_desc* desc, const void* logits, const void* token,
+                             float* logp_out, float* lse_out, float* entropy_out, void* ws,
+                             size_t ws_bytes, pr2_stream_t stream);
+
+/*
+ * The loss, and in the same pass (dlogits not NULL) its gradient.
+ *   logp_old, adv [T];  logp_ref [T] or NULL (no KL term);  weight [T] or NULL (all 1)
+ *   sums_out [4]: sum_t w_t times the loss, kl_t, [clipped] and entropy_t
+ *   logp_out, lse_out, entropy_out, coef_out [T], each may be NULL (lse and coef are what
+ *              pr2_policy_loss_backward reads)
+ *   dlogits    [T, V] act_dtype at row stride ldd, or NULL; may be logits itself (same
+ *              stride), otherwise the two must not overlap
+ * Statistics are held in fp32 (differences to the row's maximum), the sums over tokens in fp64;
+ * the same call gives the same bits.  (Calls of other batch sizes may split a row differently
+ * and differ in its last bits.)  T = 0 writes zeros to sums_out.
+ */
+pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, const void* token,
+                           const float* logp_old, const float* logp_ref, const float* adv,
+                           const float* weight, float* sums_out, float* logp_out, float* lse_out,
+                           float* entropy_out, float* coef_out, void* dlogits, void* ws,
+                           size_t ws_bytes, pr2_stream_t stream);
+
+/*
+ * The gradient alone, from what the forward call kept: dlogits = grad coef_t s ([v = y_t] - p_v)
+ * with p_v = exp(s z_v - lse_t).  grad_loss: one fp32 on the device (the gradient of the first
+ * of the sums) or NULL for 1.  Rows with coef_t = 0 get zeros and are not read.  dlogits as
+ * above (it may be logits itself).  clip_low, clip_high and kl_coef are not read.  No workspace.
+ */
+pr2_status pr2_policy_loss_backward(const pr2_policy_desc* desc, const void* logits,
+                                    const void* token, const float* lse, const float* coef,
+                                    const float* grad_loss, void* dlogits, pr2_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Experts of the caller's own behind the recorded routes: tokens sorted by expert, the
+ * experts' outputs summed back under the route weights, and both gradients (Eq. pr2_output
+ * with any E_j).  desc.T, d, N, k, act_dtype and, for the plan, idx_dtype are read.
+ *
+ * A route is a (token t, slot s) pair, numbered t k + s.  Rows are the routes sorted by expert,
+ * stably in route order; expert e's rows are offsets[e] .. offsets[e + 1).  A route whose id
+ * is outside [0, N) (-1 for one that was dropped) has no row.  Rows from offsets[N] on belong
+ * to no route.
+ */
+
+/*
+ *   idx           token t's ids at idx + t * ldi, ldi >= k
+ *   offsets       [N + 1] int32 (out)
+ *   row_of_route  [T, k] int32 (out), -1 for a route without a row
+ *   route_of_row  [T * k] int32 (out), -1 for a row without a route
+ *   ws            >= pr2_workspace_bytes(desc, PR2_OP_DISPATCH_PLAN)
+ * A dropped or repeated id is no fault here: PR2_VALIDATE does not apply.  T = 0 writes zeros
+ * to offsets.
+ */
+pr2_status pr2_dispatch_plan(const pr2_moe_desc* desc, const void* idx, int64_t ldi,
+                             int32_t* offsets, int32_t* row_of_route, int32_t* route_of_row,
+                             void* ws, size_t ws_bytes, pr2_stream_t stream);
+
+/* xs[row_of_route[t, s], :] = x[t, :], zeros in the rows from offsets[N] on.
+ *   x [T, d], xs [T * k, d] act_dtype (16-byte aligned, not overlapping).  Here and in the
+ *   three calls below a row index outside [0, T k) counts as none. */
+pr2_status pr2_dispatch(const pr2_moe_desc* desc, const void* x, const int32_t* offsets,
+                        const int32_t* row_of_route, void* xs, pr2_stream_t stream);
+
+/* dx[t, :] = sum over slots of dxs[row_of_route[t, s], :], in slot order in fp32, zeros for a
+ * token without rows. */
+pr2_status pr2_dispatch_backward(const pr2_moe_desc* desc, const void* dxs,
+                                 const int32_t* row_of_route, void* dx, pr2_stream_t stream);
+
+/* y[t, :] = sum over slots of gate[t, s] o[row_of_route[t, s], :], in slot order in fp32.
+ *   o [T * k, d], y [T, d] act_dtype;  gate [T, k] fp32 */
+pr2_status pr2_combine(const pr2_moe_desc* desc, const void* o, const int32_t* row_of_route,
+                       const float* gate, void* y, pr2_stream_t stream);
+
+/* d_o[row_of_route[t, s], :] = gate[t, s] dy[t, :], zeros in the rows from offsets[N] on;
+ * dgate[t, s] = <dy[t, :], o[row_of_route[t, s], :]> in fp32, 0 for a route without a row.
+ * d_o may be o itself. */
+pr2_status pr2_combine_backward(const pr2_moe_desc* desc, const void* dy, const void* o,
+                                const int32_t* offsets, const int32_t* row_of_route,
+                                const float* gate, void* d_o, float* dgate,
+                                pr2_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Activations kept in 8 bits between the forward and the backward pass.
+ *
+ * The packed form of x [R, C]: q [R, C] int8 and scale [R, ceil(C / 32)] uint8, one scale for
+ * each group of 32 consecutive columns of a row (the last group may be shorter).  With E the
+ * exponent field (fp32) of the group's largest magnitude, scale = max(E - 6, 1) and
+ *   q = clamp(round_to_even(x 2^(127 - scale)), -127, 127),   value = q 2^(scale - 127):
+ * a power of two, so that value is exact in bf16 and fp32 and packing gives the same bits on
+ * any machine.  A bf16 group's largest magnitude is held exactly, the others to half a step
+ * of 1/64 to 1/128 of it.  A group that holds an infinity or a NaN has scale 255 and q = 0, and
+ * all its values are NaN.
+ * R >= 0 rows of C >= 1 columns, contiguous; q and scale 16-byte aligned.
+ */
+pr2_status pr2_act_pack(int64_t R, int32_t C, int act_dtype, const void* x, int8_t* q,
+                        uint8_t* scale, pr2_stream_t stream);
+/* x [R, C] act_dtype (out): the values that (q, scale) stand for. */
+pr2_status pr2_act_unpack(int64_t R, int32_t C, int act_dtype, const int8_t* q,
+                          const uint8_t* scale, void* x, pr2_stream_t stream);
+
+/* SwiGLU that keeps its input in 8 bits: au [R, 2m] holds a (first m columns) and u;
+ *   h [R, m] = silu(a) u (from au itself), (q, scale) = the packed form of au as [R, 2m]. */
+pr2_status pr2_swiglu_pack(int64_t R, int32_t m, int act_dtype, const void* au, void* h,
+                           int8_t* q, uint8_t* scale, pr2_stream_t stream);
+/* Its backward from the packed form, with a, u the values that it stands for:
+ *   d_au [R, 2m]: da = dh u sig(a) (1 + a (1 - sig(a))) and du = dh silu(a);
+ *   h_out [R, m] = silu(a) u (what a down projection's weight gradient reads), or NULL. */
+pr2_status pr2_swiglu_backward_packed(int64_t R, int32_t m, int act_dtype, const int8_t* q,
+                                      const uint8_t* scale, const void* dh, void* d_au,
+                                      void* h_out, pr2_stream_t stream);
+
+/*
+ * Weight gradients of linear layers (out = x W^T, W [n_out, n_in]) whose input x was packed:
+ *   dW[e] = sum over the rows r of expert e of dy[r, :]^T value(x)[src(r), :]
+ * with expert e's rows offsets[e] .. offsets[e + 1) and src(r) = route_of_row[r] / k (the token
+ * of the route), or src(r) = r when route_of_row is NULL.  A row whose route_of_row is
+ * outside [0, k Rx) adds nothing.  offsets NULL (then N = 1): one weight over all R rows.
+ *   R rows of dy [R, n_out];  q [Rx, n_in], scale [Rx, ceil(n_in / 32)] as packed;
+ *   dW [N, n_out, n_in] fp32, overwritten (zeros for an expert without rows).
+ *   Without route_of_row, R <= Rx.  N <= 1024; R and Rx below 2^31.
+ *   ws >= pr2_weight_grad_workspace_bytes(desc)
+ * act_dtype is dy's.  bf16: MFMA with fp32 accumulation of exact products (the packed values
+ * are bf16 values); fp32: fp32 products and sums.  Sums run in a fixed order.
+ */
+typedef struct {
+    int64_t R, Rx;
+    int32_t n_out, n_in, N, k;
+    int32_t act_dtype;
+} pr2_wgrad_desc;
+size_t pr2_weight_grad_workspace_bytes(const pr2_wgrad_desc* desc);
+pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, const int8_t* q,
+                                  const uint8_t* scale, const int32_t* offsets,
+                                  const int32_t* route_of_row, float* dW, void* ws,
+                                  size_t ws_bytes, pr2_stream_t stream);
 
 /* Status name ("PR2_OK", ...); never NULL. */
 const char* pr2_status_string(pr2_status s);

@@ -9,8 +9,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, byref, c_char_p, c_double, c_int, c_int32, c_int64, c_size_t,
-                    c_uint64, c_void_p)
+from ctypes import (POINTER, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64,
+                    c_size_t, c_uint64, c_void_p)
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 # PR2_LIBRARY names another build of the same library (the host-sanitizer build
@@ -18,8 +18,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("PR2_LIBRARY") or os.path.join(HERE, "libpr2.so")
 
 PR2_F32, PR2_BF16 = 0, 1
-PR2_I32, PR2_I16 = 0, 1
-OP_ROUTE, OP_REPLAY_FWD, OP_REPLAY_BWD, OP_ROLLOUT_FWD, OP_ROUTE_DIAG, OP_PREDICTOR_LOSS = range(6)
+PR2_I32, PR2_I16, PR2_I64 = 0, 1, 2
+(OP_ROUTE, OP_REPLAY_FWD, OP_REPLAY_BWD, OP_ROLLOUT_FWD, OP_ROUTE_DIAG, OP_PREDICTOR_LOSS,
+ OP_DISPATCH_PLAN) = range(7)
+PACK_GROUP = 32     # columns of a packed activation that share one scale
 
 STATUS = ["PR2_OK", "PR2_ERR_NULL", "PR2_ERR_SHAPE", "PR2_ERR_DTYPE", "PR2_ERR_ALIGN",
           "PR2_ERR_WORKSPACE", "PR2_ERR_UNSUPPORTED", "PR2_ERR_ROUTE", "PR2_ERR_DEVICE",
@@ -32,6 +34,11 @@ EXPORTS = ["pr2_workspace_bytes", "pr2_route_predict", "pr2_route_predict_reuse"
            "pr2_moe_replay_forward_save", "pr2_moe_replay_backward_saved",
            "pr2_moe_replay_backward", "pr2_moe_rollout_forward", "pr2_route_diagnostics",
            "pr2_feature_cache_positions", "pr2_route_predict_cached", "pr2_predictor_loss",
+           "pr2_policy_workspace_bytes", "pr2_token_logprob", "pr2_policy_loss",
+           "pr2_policy_loss_backward", "pr2_dispatch_plan", "pr2_dispatch",
+           "pr2_dispatch_backward", "pr2_combine", "pr2_combine_backward", "pr2_act_pack",
+           "pr2_act_unpack", "pr2_swiglu_pack", "pr2_swiglu_backward_packed",
+           "pr2_weight_grad_workspace_bytes", "pr2_weight_grad_packed",
            "pr2_status_string",
            "pr2_last_error", "pr2_version", "pr2_profile_enable",
            "pr2_profile_reset", "pr2_profile_collect"]
@@ -48,6 +55,17 @@ class MoeDesc(ctypes.Structure):
     _fields_ = [("T", c_int64), ("d", c_int32), ("N", c_int32), ("k", c_int32), ("m", c_int32),
                 ("r", c_int32), ("act_dtype", c_int32), ("idx_dtype", c_int32),
                 ("renorm", c_int32)]
+
+
+class PolicyDesc(ctypes.Structure):
+    _fields_ = [("T", c_int64), ("ldl", c_int64), ("ldd", c_int64), ("V", c_int32),
+                ("act_dtype", c_int32), ("token_dtype", c_int32), ("inv_temp", c_float),
+                ("clip_low", c_float), ("clip_high", c_float), ("kl_coef", c_float)]
+
+
+class WgradDesc(ctypes.Structure):
+    _fields_ = [("R", c_int64), ("Rx", c_int64), ("n_out", c_int32), ("n_in", c_int32),
+                ("N", c_int32), ("k", c_int32), ("act_dtype", c_int32)]
 
 
 _lib = None
@@ -101,6 +119,26 @@ def lib() -> ctypes.CDLL:
     L.pr2_predictor_loss.argtypes = [POINTER(MoeDesc), P, P, P, P, P, P, P, c_int, c_int, P, P, P,
                                      P, P, c_size_t, P]
     L.pr2_predictor_loss.restype = c_int
+    for name, args in (
+            ("pr2_token_logprob", [POINTER(PolicyDesc), P, P, P, P, P, P, c_size_t, P]),
+            ("pr2_policy_loss", [POINTER(PolicyDesc)] + [P] * 13 + [c_size_t, P]),
+            ("pr2_policy_loss_backward", [POINTER(PolicyDesc)] + [P] * 7),
+            ("pr2_dispatch_plan", [POINTER(MoeDesc), P, c_int64, P, P, P, P, c_size_t, P]),
+            ("pr2_dispatch", [POINTER(MoeDesc)] + [P] * 5),
+            ("pr2_dispatch_backward", [POINTER(MoeDesc)] + [P] * 4),
+            ("pr2_combine", [POINTER(MoeDesc)] + [P] * 5),
+            ("pr2_combine_backward", [POINTER(MoeDesc)] + [P] * 8),
+            ("pr2_act_pack", [c_int64, c_int32, c_int, P, P, P, P]),
+            ("pr2_act_unpack", [c_int64, c_int32, c_int, P, P, P, P]),
+            ("pr2_swiglu_pack", [c_int64, c_int32, c_int, P, P, P, P, P]),
+            ("pr2_swiglu_backward_packed", [c_int64, c_int32, c_int, P, P, P, P, P, P]),
+            ("pr2_weight_grad_packed", [POINTER(WgradDesc)] + [P] * 7 + [c_size_t, P])):
+        getattr(L, name).argtypes = args
+        getattr(L, name).restype = c_int
+    L.pr2_policy_workspace_bytes.argtypes = [POINTER(PolicyDesc)]
+    L.pr2_policy_workspace_bytes.restype = c_size_t
+    L.pr2_weight_grad_workspace_bytes.argtypes = [POINTER(WgradDesc)]
+    L.pr2_weight_grad_workspace_bytes.restype = c_size_t
     L.pr2_status_string.argtypes = [c_int]
     L.pr2_status_string.restype = c_char_p
     L.pr2_last_error.argtypes = []
@@ -614,6 +652,297 @@ def moe_replay_backward_saved(x, idx, W_r, b_r, W_gate, W_up, W_down, au_saved, 
                                               _ptr(db_r), _ptr(dW_gate), _ptr(dW_up),
                                               _ptr(dW_down), _ptr(ws), ws.numel(),
                                               _stream(stream)))
+
+
+# ------------------------------------------------------------ policy loss --
+
+def _logit_rows(t, name, device=None, shape=None, dtype=None):
+    """[T, V] logits (or their gradient): unit stride along V, rows at any stride >= V.
+    Returns that stride in elements."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D [T, V]")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    T, V = t.shape
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along V")
+    if T <= 1:
+        return V
+    if t.stride(0) < V:
+        raise ValueError(f"rows of {name} overlap: row stride below V")
+    return t.stride(0)
+
+
+def _policy_desc(logits, token, inv_temp, clip_low=0.0, clip_high=0.0, kl_coef=0.0, dlogits=None):
+    torch = _torch()
+    ldl = _logit_rows(logits, "logits")
+    dev = logits.device
+    T, V = logits.shape
+    if token.shape != (T,):
+        raise ValueError(f"token has shape {tuple(token.shape)}, expected {(T,)}")
+    if token.dtype == torch.int64:
+        code = PR2_I64
+    elif token.dtype == torch.int32:
+        code = PR2_I32
+    else:
+        raise TypeError(f"token must be int32 or int64, got {token.dtype}")
+    if not token.is_contiguous() or token.device != dev:
+        raise ValueError("token must be contiguous, on the logits' device")
+    ldd = 0
+    if dlogits is not None:
+        ldd = _logit_rows(dlogits, "dlogits", dev, logits.shape, logits.dtype)
+    return PolicyDesc(T, ldl, ldd, V, _act_code(logits), code, inv_temp, clip_low, clip_high,
+                      kl_coef), T, dev
+
+
+def policy_workspace(logits, stream=None):
+    """A workspace for token_logprob and policy_loss over up to logits.shape[0] rows."""
+    desc = PolicyDesc(logits.shape[0], logits.shape[1], 0, logits.shape[1], _act_code(logits),
+                      PR2_I32, 1.0, 0.0, 0.0, 0.0)
+    return _new_ws(int(lib().pr2_policy_workspace_bytes(byref(desc))), logits.device, stream)
+
+
+def token_logprob(logits, token, logp_out, lse_out=None, entropy_out=None, inv_temp=1.0, ws=None,
+                  stream=None):
+    """pr2_token_logprob on torch tensors: log-probabilities of the sampled tokens
+    (logits [T, V], rows at any stride; token int32/int64 [T])."""
+    torch = _torch()
+    desc, T, dev = _policy_desc(logits, token, inv_temp)
+    _need(logp_out, "logp_out", (T,), torch.float32, dev)
+    _need(lse_out, "lse_out", (T,), torch.float32, dev, optional=True)
+    _need(entropy_out, "entropy_out", (T,), torch.float32, dev, optional=True)
+    _need_ws(ws, dev)
+    if ws is None:
+        ws = policy_workspace(logits, stream)
+    check(lib().pr2_token_logprob(byref(desc), _ptr(logits), _ptr(token), _ptr(logp_out),
+                                  _ptr(lse_out), _ptr(entropy_out), _ptr(ws), ws.numel(),
+                                  _stream(stream)))
+
+
+def policy_loss(logits, token, logp_old, adv, sums_out, logp_ref=None, weight=None, logp_out=None,
+                lse_out=None, entropy_out=None, coef_out=None, dlogits=None, clip_low=0.2,
+                clip_high=0.28, kl_coef=0.0, inv_temp=1.0, ws=None, stream=None):
+    """pr2_policy_loss on torch tensors.  ``sums_out`` [4] receives the weighted sums of the
+    loss, the KL term, the clipped tokens and the entropy; with ``dlogits`` (which may be
+    ``logits`` itself) the gradient is formed in the same pass.  The clip bounds are those
+    the method is trained with."""
+    torch = _torch()
+    desc, T, dev = _policy_desc(logits, token, inv_temp, clip_low, clip_high, kl_coef, dlogits)
+    f = torch.float32
+    _need(logp_old, "logp_old", (T,), f, dev)
+    _need(adv, "adv", (T,), f, dev)
+    _need(sums_out, "sums_out", (4,), f, dev)
+    for t, name in ((logp_ref, "logp_ref"), (weight, "weight"), (logp_out, "logp_out"),
+                    (lse_out, "lse_out"), (entropy_out, "entropy_out"), (coef_out, "coef_out")):
+        _need(t, name, (T,), f, dev, optional=True)
+    _need_ws(ws, dev)
+    if ws is None:
+        ws = policy_workspace(logits, stream)
+    check(lib().pr2_policy_loss(byref(desc), _ptr(logits), _ptr(token), _ptr(logp_old),
+                                _ptr(logp_ref), _ptr(adv), _ptr(weight), _ptr(sums_out),
+                                _ptr(logp_out), _ptr(lse_out), _ptr(entropy_out), _ptr(coef_out),
+                                _ptr(dlogits), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def policy_loss_backward(logits, token, lse, coef, dlogits, grad_loss=None, inv_temp=1.0,
+                         stream=None):
+    """pr2_policy_loss_backward on torch tensors: dlogits from the ``lse`` and ``coef`` that
+    policy_loss wrote, times ``grad_loss`` (an fp32 tensor of one element) if given."""
+    torch = _torch()
+    desc, T, dev = _policy_desc(logits, token, inv_temp, dlogits=dlogits)
+    if dlogits is None:
+        raise ValueError("dlogits is required")
+    _need(lse, "lse", (T,), torch.float32, dev)
+    _need(coef, "coef", (T,), torch.float32, dev)
+    if grad_loss is not None and (grad_loss.numel() != 1 or grad_loss.dtype != torch.float32
+                                  or grad_loss.device != dev):
+        raise ValueError("grad_loss must be one fp32 element on the logits' device")
+    check(lib().pr2_policy_loss_backward(byref(desc), _ptr(logits), _ptr(token), _ptr(lse),
+                                         _ptr(coef), _ptr(grad_loss), _ptr(dlogits),
+                                         _stream(stream)))
+
+
+# ----------------------------------------- tokens sorted by expert and back --
+
+def dispatch_workspace(idx, N, stream=None):
+    desc = make_desc(idx.shape[0], 1, N, idx.shape[1], idx=_idx_code(idx))
+    return _new_ws(workspace_bytes(desc, OP_DISPATCH_PLAN), idx.device, stream)
+
+
+def dispatch_plan(idx, N, offsets, row_of_route, route_of_row, ws=None, stream=None):
+    """pr2_dispatch_plan on torch tensors: ``idx`` is a [T, k] view (any row stride) of
+    int16/int32 ids, those outside [0, N) dropped; the outputs are int32 [N + 1], [T, k]
+    and [T * k]."""
+    torch = _torch()
+    if idx.dim() != 2:
+        raise ValueError("idx must be 2-D [T, k]")
+    T, k = idx.shape
+    dev = idx.device
+    if dev.type != "cuda":
+        raise ValueError("idx must be a CUDA (HIP) tensor")
+    ldi = _need_ids(idx, "idx", T, k, dev)
+    if T <= 1:
+        ldi = k
+    _need(offsets, "offsets", (N + 1,), torch.int32, dev)
+    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
+    _need(route_of_row, "route_of_row", (T * k,), torch.int32, dev)
+    _need_ws(ws, dev)
+    desc = make_desc(T, 1, N, k, idx=_idx_code(idx))
+    if ws is None:
+        ws = _new_ws(workspace_bytes(desc, OP_DISPATCH_PLAN), dev, stream)
+    check(lib().pr2_dispatch_plan(byref(desc), _ptr(idx), ldi, _ptr(offsets), _ptr(row_of_route),
+                                  _ptr(route_of_row), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def _plan_shape(row_of_route, offsets, device):
+    """k and N of a plan; without offsets (the call reads none) N is k, the least allowed."""
+    torch = _torch()
+    if row_of_route.dim() != 2:
+        raise ValueError("row_of_route must be 2-D [T, k]")
+    k = row_of_route.shape[1]
+    if offsets is None:
+        return k, k
+    if offsets.dim() != 1 or offsets.shape[0] < 2:
+        raise ValueError("offsets must be 1-D [N + 1]")
+    _need(offsets, "offsets", offsets.shape, torch.int32, device)
+    return k, offsets.shape[0] - 1
+
+
+def dispatch(x, offsets, row_of_route, xs, stream=None):
+    """pr2_dispatch on torch tensors: the rows of x [T, d] sorted by expert into xs [T * k, d]."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(x)
+    k, N = _plan_shape(row_of_route, offsets, dev)
+    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
+    _need(xs, "xs", (T * k, d), adt, dev)
+    desc = make_desc(T, d, N, k, act=_act_code(x))
+    check(lib().pr2_dispatch(byref(desc), _ptr(x), _ptr(offsets), _ptr(row_of_route), _ptr(xs),
+                             _stream(stream)))
+
+
+def dispatch_backward(dxs, row_of_route, dx, stream=None):
+    """pr2_dispatch_backward on torch tensors: dx [T, d] = the sum of each token's rows of dxs."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(dx, "dx")
+    k, N = _plan_shape(row_of_route, None, dev)
+    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
+    _need(dxs, "dxs", (T * k, d), adt, dev)
+    desc = make_desc(T, d, N, k, act=_act_code(dx))
+    check(lib().pr2_dispatch_backward(byref(desc), _ptr(dxs), _ptr(row_of_route), _ptr(dx),
+                                      _stream(stream)))
+
+
+def combine(o, row_of_route, gate, y, stream=None):
+    """pr2_combine on torch tensors: y [T, d] = the rows of o [T * k, d] under ``gate`` [T, k]."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(y, "y")
+    k, N = _plan_shape(row_of_route, None, dev)
+    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
+    _need(gate, "gate", (T, k), torch.float32, dev)
+    _need(o, "o", (T * k, d), adt, dev)
+    desc = make_desc(T, d, N, k, act=_act_code(y))
+    check(lib().pr2_combine(byref(desc), _ptr(o), _ptr(row_of_route), _ptr(gate), _ptr(y),
+                            _stream(stream)))
+
+
+def combine_backward(dy, o, offsets, row_of_route, gate, d_o, dgate, stream=None):
+    """pr2_combine_backward on torch tensors: d_o [T * k, d] (may be ``o``) and dgate [T, k]."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(dy, "dy")
+    k, N = _plan_shape(row_of_route, offsets, dev)
+    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
+    _need(gate, "gate", (T, k), torch.float32, dev)
+    _need(o, "o", (T * k, d), adt, dev)
+    _need(d_o, "d_o", (T * k, d), adt, dev)
+    _need(dgate, "dgate", (T, k), torch.float32, dev)
+    desc = make_desc(T, d, N, k, act=_act_code(dy))
+    check(lib().pr2_combine_backward(byref(desc), _ptr(dy), _ptr(o), _ptr(offsets),
+                                     _ptr(row_of_route), _ptr(gate), _ptr(d_o), _ptr(dgate),
+                                     _stream(stream)))
+
+
+# ------------------------------------------------- activations kept in 8 bits --
+
+def _packed(q, scale, R, C, device):
+    torch = _torch()
+    _need(q, "q", (R, C), torch.int8, device)
+    _need(scale, "scale", (R, -(-C // PACK_GROUP)), torch.uint8, device)
+
+
+def act_pack(x, q, scale, stream=None):
+    """pr2_act_pack on torch tensors: x [R, C] to q int8 [R, C] and scale uint8
+    [R, ceil(C / 32)]."""
+    R, C, _, dev = _need_act(x)
+    _packed(q, scale, R, C, dev)
+    check(lib().pr2_act_pack(R, C, _act_code(x), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def act_unpack(q, scale, x, stream=None):
+    """pr2_act_unpack on torch tensors: the values of (q, scale) into x [R, C]."""
+    R, C, _, dev = _need_act(x)
+    _packed(q, scale, R, C, dev)
+    check(lib().pr2_act_unpack(R, C, _act_code(x), _ptr(q), _ptr(scale), _ptr(x),
+                               _stream(stream)))
+
+
+def swiglu_pack(au, h, q, scale, stream=None):
+    """pr2_swiglu_pack on torch tensors: h [R, m] = silu(a) u of au [R, 2m], au packed into
+    (q, scale)."""
+    R, C, adt, dev = _need_act(au, "au")
+    if C % 2:
+        raise ValueError("au must hold a and u, [R, 2m]")
+    _need(h, "h", (R, C // 2), adt, dev)
+    _packed(q, scale, R, C, dev)
+    check(lib().pr2_swiglu_pack(R, C // 2, _act_code(au), _ptr(au), _ptr(h), _ptr(q), _ptr(scale),
+                                _stream(stream)))
+
+
+def swiglu_backward_packed(q, scale, dh, d_au, h_out=None, stream=None):
+    """pr2_swiglu_backward_packed on torch tensors: d_au [R, 2m] from the packed au and
+    dh [R, m]; h_out [R, m] also receives silu(a) u."""
+    R, m, adt, dev = _need_act(dh, "dh")
+    _packed(q, scale, R, 2 * m, dev)
+    _need(d_au, "d_au", (R, 2 * m), adt, dev)
+    _need(h_out, "h_out", (R, m), adt, dev, optional=True)
+    check(lib().pr2_swiglu_backward_packed(R, m, _act_code(dh), _ptr(q), _ptr(scale), _ptr(dh),
+                                           _ptr(d_au), _ptr(h_out), _stream(stream)))
+
+
+def weight_grad_packed(dy, q, scale, dW, offsets=None, route_of_row=None, k=1, ws=None,
+                       stream=None):
+    """pr2_weight_grad_packed on torch tensors: dW [N, n_out, n_in] from dy [R, n_out] and a
+    packed x [Rx, n_in]; ``offsets`` [N + 1] and ``route_of_row`` [R] (with the layer's ``k``)
+    as dispatch_plan writes them."""
+    torch = _torch()
+    R, n_out, _, dev = _need_act(dy, "dy")
+    if q.dim() != 2:
+        raise ValueError("q must be 2-D [Rx, n_in]")
+    Rx, n_in = q.shape
+    _packed(q, scale, Rx, n_in, dev)
+    N = 1
+    if offsets is not None:
+        if offsets.dim() != 1 or offsets.shape[0] < 2:
+            raise ValueError("offsets must be 1-D [N + 1]")
+        N = offsets.shape[0] - 1
+        _need(offsets, "offsets", (N + 1,), torch.int32, dev)
+    _need(route_of_row, "route_of_row", (R,), torch.int32, dev, optional=True)
+    _need(dW, "dW", (N, n_out, n_in), torch.float32, dev)
+    _need_ws(ws, dev)
+    desc = WgradDesc(R, Rx, n_out, n_in, N, k, _act_code(dy))
+    if ws is None:
+        ws = _new_ws(int(lib().pr2_weight_grad_workspace_bytes(byref(desc))), dev, stream)
+    check(lib().pr2_weight_grad_packed(byref(desc), _ptr(dy), _ptr(q), _ptr(scale), _ptr(offsets),
+                                       _ptr(route_of_row), _ptr(dW), _ptr(ws), ws.numel(),
+                                       _stream(stream)))
 
 
 # ------------------------------------------------------ measurement hooks --

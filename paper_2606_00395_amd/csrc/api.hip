@@ -99,7 +99,7 @@ struct SplitRecord {
 static std::mutex g_split_mu;
 static std::map<uintptr_t, SplitRecord> g_splits;   // keyed by workspace address
 
-static void drop_split_records(const void* ws, size_t bytes) {
+void drop_split_records(const void* ws, size_t bytes) {
     if (!ws) return;
     const uintptr_t lo = (uintptr_t)ws, hi = lo + (bytes ? bytes : 1);
     std::lock_guard<std::mutex> lk(g_split_mu);
@@ -114,7 +114,7 @@ pr2_status hip_fail(hipError_t e, const char* what) {
 }
 
 // --------------------------------------------------- descriptor checks ----
-static pr2_status check_desc(const pr2_moe_desc* d, bool need_m, bool need_idx_dtype) {
+pr2_status check_desc(const pr2_moe_desc* d, bool need_m, bool need_idx_dtype) {
     if (!d) return fail(PR2_ERR_NULL, "desc is NULL");
     if (d->act_dtype != PR2_F32 && d->act_dtype != PR2_BF16)
         return fail(PR2_ERR_DTYPE, "act_dtype %d is not PR2_F32 or PR2_BF16", d->act_dtype);
@@ -382,6 +382,13 @@ size_t pr2_workspace_bytes(const pr2_moe_desc* desc, int op) {
             t_err = saved;
             if (s != PR2_OK || desc->r < 1) return 0;
             return pred_ws_layout(*desc, nullptr).bytes;
+        }
+        case PR2_OP_DISPATCH_PLAN: {
+            std::string saved = t_err;
+            pr2_status s = check_desc(desc, false, true);
+            t_err = saved;
+            if (s != PR2_OK) return 0;
+            return dispatch_plan_bytes(*desc);
         }
         case PR2_OP_REPLAY_BWD: {
             std::string saved = t_err;

@@ -160,6 +160,10 @@ pr2_status ok();
 pr2_status hip_fail(hipError_t e, const char* what);
 // the current device is usable and is a gfx950
 pr2_status device_ready();
+// forgets the router splits recorded in a workspace that a call is about to write
+void drop_split_records(const void* ws, size_t bytes);
+// descriptor checks; need_m, need_idx_dtype: the call reads those fields
+pr2_status check_desc(const pr2_moe_desc* d, bool need_m, bool need_idx_dtype);
 // argument checks shared by the route calls; *empty is set for T == 0 (a no-op)
 pr2_status check_route_args(const pr2_moe_desc* desc, const void* x, const float* W_r,
                             const float* b_r, const float* A, const float* B, void* idx_out,
@@ -236,7 +240,11 @@ hipError_t launch_route_diagnostics(const pr2_moe_desc& d, const void* x, const 
                                     const float* z_ref, void* cur_idx, int* overlap, float* kl,
                                     unsigned long long* hist, void* split_ws, hipStream_t s);
 
+// dispatch.hip
+size_t dispatch_plan_bytes(const pr2_moe_desc& d);
+
 // permute.hip
+// rows that no route has get perm_src = -1
 // counted: the per-block counts and the out-of-range count are already in the
 // workspace (written by the replay-weight pass)
 hipError_t launch_permute(const pr2_moe_desc& d, const void* idx, int64_t ldi, const ReplayWs& ws,

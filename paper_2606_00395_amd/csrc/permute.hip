@@ -11,7 +11,8 @@
 //   scatter one workgroup per chunk, 64 entries a wavefront; lanes with the same
 //           expert find each other with ballots over the id bits, so each
 //           entry's position is its block base + the entries of the same
-//           expert before it.  perm_src[pos] = t*k + s, inv[t*k + s] = pos.
+//           expert before it.  perm_src[pos] = t*k + s, inv[t*k + s] = pos; rows past
+//           the last expert's have perm_src = -1.
 // Out-of-range ids are not dispatched (inv = -1); the count pass is the one
 // place that counts them (in the workspace's error words).  The replay forward
 // and backward form the counts in their replay-weight pass instead, where that
@@ -244,7 +245,8 @@ constexpr int kScatterWaves = kEntriesPerPermBlock / 64;
 
 __global__ void __launch_bounds__(64 * kScatterWaves)
 perm_scatter_kernel(const void* idx, int idx_dtype, int64_t ldi, int64_t T, int k, int N,
-                    int tb, int64_t nblk, const int* bases, int* perm_src, int* inv) {
+                    int tb, int64_t nblk, const int* bases, const int* offsets, int* perm_src,
+                    int* inv) {
     extern __shared__ int first[];              // [kScatterWaves][N]
     const int tid = threadIdx.x;
     const int lane = tid & 63, wave = tid >> 6;
@@ -287,6 +289,7 @@ perm_scatter_kernel(const void* idx, int idx_dtype, int64_t ldi, int64_t T, int 
         }
     }
     inv[src] = pos;
+    if (src >= offsets[N]) perm_src[src] = -1;     // a row that no route has
 }
 
 // The whole permutation of a small batch in one launch of one workgroup: what
@@ -392,7 +395,7 @@ perm_small_kernel(const void* idx, int idx_dtype, int64_t ldi, int entries, int 
         __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
-    for (int i = tid; i < total; i += kScanThreads) perm_src[i] = sorted[i];
+    for (int i = tid; i < entries; i += kScanThreads) perm_src[i] = i < total ? sorted[i] : -1;
 }
 
 // bf16, d % 8 == 0: each thread owns 8 consecutive columns of kCombTok tokens
@@ -524,8 +527,8 @@ hipError_t launch_permute(const pr2_moe_desc& d, const void* idx, int64_t ldi, c
         LaunchScope scope("perm_scatter", s);
         hipLaunchKernelGGL(perm_scatter_kernel, dim3((unsigned)ws.nblk), dim3(64 * kScatterWaves),
                            kScatterWaves * sm, s, idx,
-                           d.idx_dtype, ldi, d.T, d.k, d.N, tb, ws.nblk, ws.bcount, ws.perm_src,
-                           ws.inv);
+                           d.idx_dtype, ldi, d.T, d.k, d.N, tb, ws.nblk, ws.bcount, ws.offsets,
+                           ws.perm_src, ws.inv);
     }
     return hipGetLastError();
 }

@@ -1,0 +1,662 @@
+// The policy's loss on the sampled tokens and its gradient.
+//
+// For each row of V logits z with target y and s = 1 / temperature: the running
+// maximum M and, relative to it, S = sum 2^(k (z - M)) and E = sum of the same terms
+// times their exponents, k = s log2(e), give in one pass
+//   logp = s (z_y - M) - ln S,  lse = s M + ln S,  entropy = ln S - ln2 E / S,
+// and with the gradient's coefficient c = d loss / d logp, which depends on logp alone,
+//   dlogits_v = c s ([v = y] - 2^(k (z_v - M)) / S).
+// Bound by HBM: V elements read per row, and V written where the gradient is wanted;
+// two exponentials per element (a quarter-rate instruction each) come next.
+#include "chunk.h"
+
+namespace pr2 {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.4028234663852886e38f;
+constexpr float kNegInf = -__builtin_huge_valf();
+
+// Running statistics of part of a row.  m starts at the lowest finite number, so that a row
+// of -infinity alone keeps s = 0 and no term ever subtracts -infinity from itself.
+struct Stat {
+    float m, s, e;
+};
+
+__device__ __forceinline__ float exp2_native(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// moves the terms to the maximum m (>= a.m); exponents are cut off where their power is 0
+__device__ __forceinline__ void rebase(Stat& a, float m, float k) {
+    const float t = (a.m - m) * k;
+    const float f = exp2_native(t);
+    a.e = f * (a.e + fmaxf(t, -1e4f) * a.s);
+    a.s *= f;
+    a.m = m;
+}
+
+template <int n>
+__device__ __forceinline__ void add_terms(Stat& a, const float* v, float k) {
+    float m = v[0];
+#pragma unroll
+    for (int i = 1; i < n; ++i) m = fmaxf(m, v[i]);
+    if (m > a.m) rebase(a, m, k);
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+        const float t = (v[i] - a.m) * k;
+        const float p = exp2_native(t);
+        a.s += p;
+        a.e += p * fmaxf(t, -1e4f);      // a term of 0 adds 0, also at -infinity
+    }
+}
+
+__device__ __forceinline__ void join_lanes(Stat& a, float k) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        Stat b{__shfl_xor(a.m, off, 64), __shfl_xor(a.s, off, 64), __shfl_xor(a.e, off, 64)};
+        const float m = fmaxf(a.m, b.m);
+        rebase(a, m, k);
+        rebase(b, m, k);
+        a.s += b.s;
+        a.e += b.e;
+    }
+}
+
+// all threads get the workgroup's statistics, joined in the same order every time
+template <int NT>
+__device__ __forceinline__ void join_block(Stat& a, float k) {
+    constexpr int W = NT / 64;
+    __shared__ float sm[W], ss[W], se[W];
+    join_lanes(a, k);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) {
+        sm[wave] = a.m;
+        ss[wave] = a.s;
+        se[wave] = a.e;
+    }
+    __syncthreads();
+    Stat r{sm[0], ss[0], se[0]};
+    float m = r.m;
+#pragma unroll
+    for (int w = 1; w < W; ++w) m = fmaxf(m, sm[w]);
+    rebase(r, m, k);
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+        Stat b{sm[w], ss[w], se[w]};
+        rebase(b, m, k);
+        r.s += b.s;
+        r.e += b.e;
+    }
+    a = r;
+}
+
+struct PolicyArgs {
+    const void* z;
+    const void* y;
+    const float* old;       // the loss's inputs; null for log-probabilities alone
+    const float* ref;       // may be null
+    const float* adv;
+    const float* w;         // may be null: 1
+    float* logp;            // outputs, each may be null
+    float* lse;
+    float* ent;
+    float* coef;
+    float4* rowsum;         // [T] the row's terms of the four sums (null without a loss)
+    float4* part;           // [T, S] statistics of the parts of split rows
+    void* dz;               // may be null, may be z
+    const float* grad;      // backward: one number or null
+    int64_t T, ldl, ldd;
+    int V, S, y64;
+    float it, k, lo, hi, beta;
+};
+
+// everything about row t that does not depend on its logits
+struct Row {
+    int64_t y;
+    float w;
+    bool on;
+};
+
+__device__ __forceinline__ Row open_row(const PolicyArgs& a, int64_t t) {
+    Row r;
+    r.y = a.y64 ? ((const int64_t*)a.y)[t] : (int64_t)((const int32_t*)a.y)[t];
+    r.w = a.w ? a.w[t] : 1.0f;
+    r.on = r.y >= 0 && r.y < a.V && r.w != 0.0f;
+    return r;
+}
+
+struct Result {
+    float coef;     // d loss / d logp
+    float logp;
+};
+
+// From a row's statistics to its results; `write` for the thread that stores them.
+__device__ __forceinline__ Result close_row(const PolicyArgs& a, int64_t t, const Row& r, float zy,
+                                            const Stat& st, bool write) {
+    const bool on = r.on && st.s != 0.0f;      // (NaN counts: it has to be seen)
+    float logp = 0.0f, lse = kNegInf, ent = 0.0f, coef = 0.0f;
+    float4 sums = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (on) {
+        const float ls = logf(st.s);
+        logp = (zy - st.m) * a.it - ls;
+        lse = st.m * a.it + ls;
+        ent = ls - kLn2 * (st.e / st.s);
+        if (a.old) {
+            const float A = a.adv[t];
+            const float ratio = expf(logp - a.old[t]);
+            const bool clipped = (A > 0.0f && ratio > a.hi) || (A < 0.0f && ratio < a.lo);
+            float surr = 0.0f, dl = 0.0f;
+            if (A != 0.0f) {
+                surr = clipped ? (A > 0.0f ? a.hi : a.lo) * A : ratio * A;
+                dl = clipped ? 0.0f : -A * ratio;
+            }
+            float kl = 0.0f, loss = -surr;
+            if (a.ref) {
+                const float d = a.ref[t] - logp;
+                const float x = expm1f(d);
+                kl = x - d;
+                if (a.beta != 0.0f) {
+                    loss += a.beta * kl;
+                    dl -= a.beta * x;
+                }
+            }
+            coef = r.w * dl;
+            sums = make_float4(r.w * loss, r.w * kl, clipped ? r.w : 0.0f, r.w * ent);
+        }
+    }
+    if (write) {
+        if (a.logp) a.logp[t] = logp;
+        if (a.lse) a.lse[t] = lse;
+        if (a.ent) a.ent[t] = ent;
+        if (a.coef) a.coef[t] = coef;
+        if (a.rowsum) a.rowsum[t] = sums;
+    }
+    return Result{coef, logp};
+}
+
+template <typename T>
+__device__ __forceinline__ void zero_chunks(T* row, int c0, int c1, int step, int full, int rem) {
+    float v[Chunk<T>::E] = {};
+    for (int c = c0; c < c1; c += step) store_chunk(row, c, full, rem, v);
+}
+
+// Statistics of row blockIdx.x / S, part blockIdx.x % S (whole rows finish here).
+constexpr int kStatThreads = 256;
+constexpr int kStatDeep = 4;        // chunks in flight per thread
+
+template <typename T>
+__global__ void __launch_bounds__(kStatThreads) policy_stats_kernel(PolicyArgs a) {
+    constexpr int E = Chunk<T>::E;
+    const int64_t t = blockIdx.x / a.S;
+    const int part = (int)(blockIdx.x - t * a.S);
+    const Row r = open_row(a, t);
+    Stat st{kLowest, 0.0f, 0.0f};
+    const T* z = (const T*)a.z + t * a.ldl;
+    float zy = 0.0f;
+    if (r.on) {
+        zy = Act<T>::to_f32(z[r.y]);
+        const int full = a.V / E, rem = a.V % E;
+        const int n = full + (rem != 0);
+        const int per = (n + a.S - 1) / a.S;
+        const int c0 = part * per, c1 = min(n, c0 + per);
+        int c = c0 + (int)threadIdx.x;
+        for (; c + (kStatDeep - 1) * kStatThreads < min(c1, full); c += kStatDeep * kStatThreads) {
+            u32x4 w[kStatDeep];
+#pragma unroll
+            for (int i = 0; i < kStatDeep; ++i)
+                w[i] = *(const u32x4_any*)(z + (int64_t)(c + i * kStatThreads) * E);
+#pragma unroll
+            for (int i = 0; i < kStatDeep; ++i) {
+                float v[E];
+                Chunk<T>::open(w[i], v);
+                add_terms<E>(st, v, a.k);
+            }
+        }
+        for (; c < c1; c += kStatThreads) {
+            float v[E];
+            Chunk<T>::open(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), v);
+            add_terms<E>(st, v, a.k);
+        }
+        join_block<kStatThreads>(st, a.k);
+    }
+    if (a.S > 1) {
+        if (threadIdx.x == 0) a.part[blockIdx.x] = make_float4(st.m, st.s, st.e, 0.0f);
+    } else {
+        close_row(a, t, r, zy, st, threadIdx.x == 0);
+    }
+}
+
+// Rows whose statistics came in S <= 64 parts: one wavefront per row.
+template <typename T>
+__global__ void __launch_bounds__(256) policy_finish_kernel(PolicyArgs a) {
+    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (t >= a.T) return;
+    const int lane = threadIdx.x & 63;
+    const Row r = open_row(a, t);
+    Stat st{kLowest, 0.0f, 0.0f};
+    if (lane < a.S) {
+        const float4 p = a.part[t * a.S + lane];
+        st = Stat{p.x, p.y, p.z};
+    }
+    join_lanes(st, a.k);
+    const float zy = r.on ? Act<T>::to_f32(((const T*)a.z)[t * a.ldl + r.y]) : 0.0f;
+    close_row(a, t, r, zy, st, lane == 0);
+}
+
+// dlogits of row blockIdx.x / S, part blockIdx.x % S, from lse and coef.
+template <typename T>
+__global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
+    constexpr int E = Chunk<T>::E;
+    const int64_t t = blockIdx.x / a.S;
+    const int part = (int)(blockIdx.x - t * a.S);
+    const T* z = (const T*)a.z + t * a.ldl;
+    T* dz = (T*)a.dz + t * a.ldd;
+    const int full = a.V / E, rem = a.V % E;
+    const int n = full + (rem != 0);
+    const int per = (n + a.S - 1) / a.S;
+    const int c0 = part * per, c1 = min(n, c0 + per);
+    const int64_t y = a.y64 ? ((const int64_t*)a.y)[t] : (int64_t)((const int32_t*)a.y)[t];
+    const float coef = a.coef[t];
+    if (coef == 0.0f || y < 0 || y >= a.V) {
+        zero_chunks(dz, c0 + (int)threadIdx.x, c1, 256, full, rem);
+        return;
+    }
+    const float lse = a.lse[t];
+    const float g = coef * a.it * (a.grad ? *a.grad : 1.0f);
+    const int yc = (int)(y / E), ye = (int)(y % E);
+    constexpr int D = 4;
+    for (int c = c0 + (int)threadIdx.x; c < c1; c += D * 256) {
+        u32x4 w[D];
+#pragma unroll
+        for (int i = 0; i < D; ++i)
+            if (c + i * 256 < c1)
+                w[i] = load_chunk(z, c + i * 256, full, rem, Chunk<T>::kNegInf);
+#pragma unroll
+        for (int i = 0; i < D; ++i) {
+            const int ci = c + i * 256;
+            if (ci >= c1) continue;
+            // log p first, in one rounding, then its power
+            float v[E];
+            Chunk<T>::open(w[i], v);
+            float ly = 0.0f;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                v[j] = fmaf(v[j], a.it, -lse);
+                if (j == ye) ly = v[j];
+                v[j] = -g * exp2_native(v[j] * kLog2e);
+            }
+            if (ci == yc) {
+                const float gy = -g * expm1f(ly);       // c s (1 - p_y)
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[j] = j == ye ? gy : v[j];
+            }
+            store_chunk(dz, ci, full, rem, v);
+        }
+    }
+}
+
+// Loss and gradient of one row per workgroup.  The row's first NT * NCH chunks stay in
+// registers between the two passes (a CU's register file is 512 KiB, a row of 151936 bf16
+// logits 297 KiB), the rest is read again.
+template <typename T, int NT, int NCH>
+__global__ void __launch_bounds__(NT) policy_fused_kernel(PolicyArgs a) {
+    constexpr int E = Chunk<T>::E;
+    const int64_t t = blockIdx.x;
+    const int tid = threadIdx.x;
+    const Row r = open_row(a, t);
+    const T* z = (const T*)a.z + t * a.ldl;
+    T* dz = (T*)a.dz + t * a.ldd;
+    const int full = a.V / E, rem = a.V % E;
+    const int n = full + (rem != 0);
+    Stat st{kLowest, 0.0f, 0.0f};
+    float zy = 0.0f;
+    u32x4 w[NCH];
+    if (r.on) {
+        zy = Act<T>::to_f32(z[r.y]);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i)
+            w[i] = load_chunk(z, i * NT + tid, full, rem, Chunk<T>::kNegInf);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+            float v[E];
+            Chunk<T>::open(w[i], v);
+            add_terms<E>(st, v, a.k);
+        }
+        for (int c = NCH * NT + tid; c < n; c += NT) {
+            float v[E];
+            Chunk<T>::open(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), v);
+            add_terms<E>(st, v, a.k);
+        }
+        // every thread holds z_y before the barrier behind which it may be overwritten
+        asm volatile("" ::"v"(zy));
+        join_block<NT>(st, a.k);
+    }
+    const Result res = close_row(a, t, r, zy, st, tid == 0);
+    if (res.coef == 0.0f) {
+        zero_chunks(dz, tid, n, NT, full, rem);
+        return;
+    }
+    const float g = res.coef * a.it;
+    const float gs = -g / st.s;
+    const float gy = -g * expm1f(res.logp);       // c s (1 - p_y) without the cancellation
+    const int yc = (int)(r.y / E), ye = (int)(r.y % E);
+    auto put = [&](const u32x4& raw, int c) __attribute__((always_inline)) {
+        float v[E];
+        Chunk<T>::open(raw, v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) v[j] = gs * exp2_native((v[j] - st.m) * a.k);
+        if (c == yc) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = j == ye ? gy : v[j];
+        }
+        store_chunk(dz, c, full, rem, v);
+    };
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) put(w[i], i * NT + tid);
+    for (int c = NCH * NT + tid; c < n; c += NT) put(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), c);
+}
+
+// the four sums over the tokens, in fp64 and a fixed order
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads)
+policy_sums_kernel(const float4* rows, int64_t T, float* out) {
+    __shared__ double sh[4][kSumThreads / 64];
+    double v[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int64_t t = threadIdx.x; t < T; t += kSumThreads) {
+        const float4 r = rows[t];
+        v[0] += r.x;
+        v[1] += r.y;
+        v[2] += r.z;
+        v[3] += r.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int off = 32; off >= 1; off >>= 1) v[i] += __shfl_xor(v[i], off, 64);
+        if ((threadIdx.x & 63) == 0) sh[i][threadIdx.x >> 6] = v[i];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) {
+        double s = 0.0;
+        for (int w = 0; w < kSumThreads / 64; ++w) s += sh[threadIdx.x][w];
+        out[threadIdx.x] = (float)s;
+    }
+}
+
+// ------------------------------------------------------------------ host ----
+constexpr int kMaxParts = 64;
+constexpr int64_t kMaxRows = 0x7fffffff / kMaxParts;    // the grid is T x parts
+constexpr int64_t kFillWgs = 2048;      // workgroups of 256 that fill the chip
+constexpr size_t kPartBytes = sizeof(float4) * 2 * kFillWgs;
+
+int row_chunks(const pr2_policy_desc& d) {
+    const int e = d.act_dtype == PR2_BF16 ? 8 : 4;
+    return (int)(((int64_t)d.V + e - 1) / e);
+}
+
+// Parts per row: enough workgroups to fill the chip, each with two chunks a thread at least.
+int row_parts(const pr2_policy_desc& d) {
+    const int64_t fill = (kFillWgs + d.T - 1) / d.T;
+    const int64_t most = row_chunks(d) / (2 * kStatThreads);
+    int64_t s = fill < most ? fill : most;
+    if (s > kMaxParts) s = kMaxParts;
+    return s < 1 ? 1 : (int)s;
+}
+
+// Below this many rows the fused kernel leaves CUs idle and its rows are read twice instead.
+constexpr int64_t kFusedRows = 192;
+
+struct PolicyWs {
+    float4* rowsum;
+    float4* part;
+    size_t bytes;
+};
+
+PolicyWs policy_ws(const pr2_policy_desc& d, void* base) {
+    char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
+    PolicyWs w{};
+    w.part = (float4*)p;
+    const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
+    w.rowsum = (float4*)(p ? p + kPartBytes : nullptr);
+    w.bytes = kPartBytes + 3 * stats + 256;
+    return w;
+}
+
+bool finite_nonneg(float v) { return v >= 0.0f && v <= 3.4028234663852886e38f; }
+bool aligned_to(const void* p, size_t a) { return (uintptr_t)p % a == 0; }
+
+pr2_status check_policy(const pr2_policy_desc* desc, bool loss, bool grad) {
+    if (!desc) return fail(PR2_ERR_NULL, "desc is NULL");
+    const pr2_policy_desc& d = *desc;
+    if (d.act_dtype != PR2_F32 && d.act_dtype != PR2_BF16)
+        return fail(PR2_ERR_DTYPE, "act_dtype %d is not PR2_F32 or PR2_BF16", d.act_dtype);
+    if (d.token_dtype != PR2_I32 && d.token_dtype != PR2_I64)
+        return fail(PR2_ERR_DTYPE, "token_dtype %d is not PR2_I32 or PR2_I64", d.token_dtype);
+    if (d.T < 0) return fail(PR2_ERR_SHAPE, "T = %lld < 0", (long long)d.T);
+    if (d.V < 1) return fail(PR2_ERR_SHAPE, "V = %d < 1", d.V);
+    if (d.ldl < d.V) return fail(PR2_ERR_SHAPE, "ldl = %lld < V = %d", (long long)d.ldl, d.V);
+    if (grad && d.ldd < d.V)
+        return fail(PR2_ERR_SHAPE, "ldd = %lld < V = %d", (long long)d.ldd, d.V);
+    if (!(d.inv_temp > 0.0f) || !finite_nonneg(d.inv_temp))
+        return fail(PR2_ERR_SHAPE, "inv_temp = %g is not positive and finite", (double)d.inv_temp);
+    if (loss && !(finite_nonneg(d.clip_low) && finite_nonneg(d.clip_high) && finite_nonneg(d.kl_coef)))
+        return fail(PR2_ERR_SHAPE, "clip_low, clip_high and kl_coef must be finite and >= 0");
+    if (d.T > kMaxRows)
+        return fail(PR2_ERR_UNSUPPORTED, "T = %lld rows exceed %lld", (long long)d.T,
+                    (long long)kMaxRows);
+    if (d.V > 0x7fffffff - 65536)
+        return fail(PR2_ERR_UNSUPPORTED, "V = %d is too large", d.V);
+    return PR2_OK;
+}
+
+pr2_status check_logits(const pr2_policy_desc& d, const void* logits, const void* token,
+                        const void* dlogits, bool grad) {
+    const size_t e = d.act_dtype == PR2_BF16 ? 2 : 4;
+    if (!logits) return fail(PR2_ERR_NULL, "logits is NULL");
+    if (!token) return fail(PR2_ERR_NULL, "token is NULL");
+    if (grad && !dlogits) return fail(PR2_ERR_NULL, "dlogits is NULL");
+    if (!aligned_to(logits, e) || (grad && !aligned_to(dlogits, e)))
+        return fail(PR2_ERR_ALIGN, "logits or dlogits is not aligned to its element size");
+    if (!aligned_to(token, d.token_dtype == PR2_I64 ? 8 : 4))
+        return fail(PR2_ERR_ALIGN, "token is not aligned to its element size");
+    if (grad) {
+        const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + e * ((size_t)(d.T - 1) * d.ldl + d.V);
+        const uintptr_t g0 = (uintptr_t)dlogits, g1 = g0 + e * ((size_t)(d.T - 1) * d.ldd + d.V);
+        if (z0 < g1 && g0 < z1 && !(z0 == g0 && d.ldl == d.ldd))
+            return fail(PR2_ERR_SHAPE, "dlogits overlaps logits without being the same rows");
+    }
+    return PR2_OK;
+}
+
+PolicyArgs policy_args(const pr2_policy_desc& d, const void* logits, const void* token) {
+    PolicyArgs a{};
+    a.z = logits;
+    a.y = token;
+    a.T = d.T;
+    a.ldl = d.ldl;
+    a.ldd = d.ldd;
+    a.V = d.V;
+    a.S = 1;
+    a.y64 = d.token_dtype == PR2_I64;
+    a.it = d.inv_temp;
+    a.k = d.inv_temp * kLog2e;
+    a.lo = 1.0f - d.clip_low;
+    a.hi = 1.0f + d.clip_high;
+    a.beta = d.kl_coef;
+    return a;
+}
+
+template <typename T>
+hipError_t launch_stats(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
+    a.S = row_parts(d);
+    {
+        LaunchScope scope("policy_stats", s);
+        hipLaunchKernelGGL(policy_stats_kernel<T>, dim3((unsigned)(d.T * a.S)), dim3(kStatThreads),
+                           0, s, a);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.S == 1) return e;
+    LaunchScope scope("policy_finish", s);
+    hipLaunchKernelGGL(policy_finish_kernel<T>, dim3((unsigned)((d.T + 3) / 4)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_grad(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
+    a.S = row_parts(d);
+    LaunchScope scope("policy_grad", s);
+    hipLaunchKernelGGL(policy_grad_kernel<T>, dim3((unsigned)(d.T * a.S)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, hipStream_t s) {
+    const int n = row_chunks(d);
+    const dim3 grid((unsigned)d.T);
+    LaunchScope scope("policy_fused", s);
+    if (n <= 256 * 4)
+        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
+    else if (n <= 256 * 16)
+        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
+    else if (n <= 512 * 18)
+        hipLaunchKernelGGL((policy_fused_kernel<T, 512, 18>), grid, dim3(512), 0, s, a);
+    else
+        hipLaunchKernelGGL((policy_fused_kernel<T, 1024, 20>), grid, dim3(1024), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace pr2
+
+using namespace pr2;
+
+extern "C" {
+
+size_t pr2_policy_workspace_bytes(const pr2_policy_desc* desc) {
+    if (!desc || desc->T < 0 || desc->T > kMaxRows || desc->V < 1) return 0;
+    return policy_ws(*desc, nullptr).bytes;
+}
+
+pr2_status pr2_token_logprob(const pr2_policy_desc* desc, const void* logits, const void* token,
+                             float* logp_out, float* lse_out, float* entropy_out, void* ws,
+                             size_t ws_bytes, pr2_stream_t stream) {
+    pr2_status s = check_policy(desc, false, false);
+    if (s != PR2_OK) return s;
+    const pr2_policy_desc& d = *desc;
+    if (d.T == 0) return ok();
+    s = check_logits(d, logits, token, nullptr, false);
+    if (s != PR2_OK) return s;
+    if (!logp_out) return fail(PR2_ERR_NULL, "logp_out is NULL");
+    if (!aligned_to(logp_out, 4) || !aligned_to(lse_out, 4) || !aligned_to(entropy_out, 4))
+        return fail(PR2_ERR_ALIGN, "a per-token output is not 4-byte aligned");
+    const size_t need = policy_ws(d, nullptr).bytes;
+    if (!ws) return fail(PR2_ERR_NULL, "ws is NULL (need %zu bytes)", need);
+    if (ws_bytes < need)
+        return fail(PR2_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    s = device_ready();
+    if (s != PR2_OK) return s;
+    drop_split_records(ws, ws_bytes);
+    PolicyArgs a = policy_args(d, logits, token);
+    a.logp = logp_out;
+    a.lse = lse_out;
+    a.ent = entropy_out;
+    a.part = policy_ws(d, ws).part;
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = d.act_dtype == PR2_BF16 ? launch_stats<bf16_t>(d, a, st)
+                                                 : launch_stats<float>(d, a, st);
+    if (e != hipSuccess) return hip_fail(e, "token_logprob launch");
+    return ok();
+}
+
+pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, const void* token,
+                           const float* logp_old, const float* logp_ref, const float* adv,
+                           const float* weight, float* sums_out, float* logp_out, float* lse_out,
+                           float* entropy_out, float* coef_out, void* dlogits, void* ws,
+                           size_t ws_bytes, pr2_stream_t stream) {
+    const bool grad = dlogits != nullptr;
+    pr2_status s = check_policy(desc, true, grad);
+    if (s != PR2_OK) return s;
+    const pr2_policy_desc& d = *desc;
+    if (!sums_out) return fail(PR2_ERR_NULL, "sums_out is NULL");
+    for (const void* p : {(const void*)logp_old, (const void*)logp_ref, (const void*)adv,
+                          (const void*)weight, (const void*)sums_out, (const void*)logp_out,
+                          (const void*)lse_out, (const void*)entropy_out, (const void*)coef_out})
+        if (!aligned_to(p, 4)) return fail(PR2_ERR_ALIGN, "a per-token tensor is not 4-byte aligned");
+    const hipStream_t st = (hipStream_t)stream;
+    if (d.T > 0) {
+        s = check_logits(d, logits, token, dlogits, grad);
+        if (s != PR2_OK) return s;
+        if (!logp_old || !adv) return fail(PR2_ERR_NULL, "logp_old and adv are required");
+        const size_t need = policy_ws(d, nullptr).bytes;
+        if (!ws) return fail(PR2_ERR_NULL, "ws is NULL (need %zu bytes)", need);
+        if (ws_bytes < need)
+            return fail(PR2_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    }
+    s = device_ready();
+    if (s != PR2_OK) return s;
+    const PolicyWs w = policy_ws(d, ws);
+    if (d.T > 0) {
+        drop_split_records(ws, ws_bytes);
+        PolicyArgs a = policy_args(d, logits, token);
+        a.old = logp_old;
+        a.ref = logp_ref;
+        a.adv = adv;
+        a.w = weight;
+        a.logp = logp_out;
+        a.lse = lse_out;
+        a.ent = entropy_out;
+        a.coef = coef_out;
+        a.rowsum = w.rowsum;
+        a.part = w.part;
+        a.dz = dlogits;
+        const bool bf = d.act_dtype == PR2_BF16;
+        hipError_t e;
+        if (grad && d.T >= kFusedRows) {
+            e = bf ? launch_fused<bf16_t>(d, a, st) : launch_fused<float>(d, a, st);
+        } else {
+            const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
+            if (grad && !a.lse) a.lse = (float*)((char*)w.rowsum + stats);
+            if (grad && !a.coef) a.coef = (float*)((char*)w.rowsum + 2 * stats);
+            e = bf ? launch_stats<bf16_t>(d, a, st) : launch_stats<float>(d, a, st);
+            if (e == hipSuccess && grad)
+                e = bf ? launch_grad<bf16_t>(d, a, st) : launch_grad<float>(d, a, st);
+        }
+        if (e != hipSuccess) return hip_fail(e, "policy_loss launch");
+    }
+    {
+        LaunchScope scope("policy_sums", st);
+        hipLaunchKernelGGL(policy_sums_kernel, dim3(1), dim3(kSumThreads), 0, st, w.rowsum, d.T,
+                           sums_out);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_fail(e, "policy_loss launch");
+    return ok();
+}
+
+pr2_status pr2_policy_loss_backward(const pr2_policy_desc* desc, const void* logits,
+                                    const void* token, const float* lse, const float* coef,
+                                    const float* grad_loss, void* dlogits, pr2_stream_t stream) {
+    pr2_status s = check_policy(desc, false, true);
+    if (s != PR2_OK) return s;
+    const pr2_policy_desc& d = *desc;
+    if (d.T == 0) return ok();
+    s = check_logits(d, logits, token, dlogits, true);
+    if (s != PR2_OK) return s;
+    if (!lse || !coef) return fail(PR2_ERR_NULL, "lse and coef are required");
+    if (!aligned_to(lse, 4) || !aligned_to(coef, 4) || !aligned_to(grad_loss, 4))
+        return fail(PR2_ERR_ALIGN, "lse, coef or grad_loss is not 4-byte aligned");
+    s = device_ready();
+    if (s != PR2_OK) return s;
+    PolicyArgs a = policy_args(d, logits, token);
+    a.lse = const_cast<float*>(lse);
+    a.coef = const_cast<float*>(coef);
+    a.grad = grad_loss;
+    a.dz = dlogits;
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = d.act_dtype == PR2_BF16 ? launch_grad<bf16_t>(d, a, st)
+                                                 : launch_grad<float>(d, a, st);
+    if (e != hipSuccess) return hip_fail(e, "policy_loss_backward launch");
+    return ok();
+}
+
+}  // extern "C"

@@ -1,0 +1,312 @@
+"""Activations in 8 bits and what is computed from them, against the float64 definitions.
+
+The packed form is compared bit for bit.  Tolerances of the rest, set before any run: the
+sigmoid takes one fast exponential (relative error 2^-22 + 2^-23 |a|), one addition and one
+fast reciprocal (2^-22), so silu(a) u is within 1e-6 (1 + |a|) relatively and the slope of
+silu, at most 1.1 in magnitude, within 1e-6 (1 + |a|)^2; a weight gradient over K rows is
+within (K + 2) 2^-23 of the sum of its terms' magnitudes; bf16 outputs add 2^-8 of the value.
+"""
+import numpy as np
+import pytest
+
+from oracle import operators_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def act(a, bf16):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).cuda()
+    return t.to(torch.bfloat16) if bf16 else t
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def packed_like(R, C):
+    import torch
+    return (torch.full((R, C), 99, dtype=torch.int8, device="cuda"),
+            torch.full((R, -(-C // 32)), 77, dtype=torch.uint8, device="cuda"))
+
+
+def do_pack(x):
+    from paper_2606_00395_amd import binding as B
+    q, e = packed_like(*x.shape)
+    B.act_pack(x, q, e)
+    return q, e
+
+
+def values(R, C, seed=0):
+    """Rows of very different sizes, zeros, subnormals and the largest numbers among them."""
+    g = np.random.default_rng([seed, R, C])
+    x = g.standard_normal((R, C)) * np.exp(g.normal(0, 8, (R, 1)))
+    x[g.random((R, C)) < 0.05] = 0.0
+    if R > 4:
+        x[0] = 0.0
+        x[1] *= 1e-40 / max(1e-30, np.abs(x[1]).max())
+        x[2] *= 3.3e38 / max(1e-30, np.abs(x[2]).max())
+        x[3] = np.where(np.arange(C) % 3 == 0, 1.999, 0.5 / 127)
+    return x
+
+
+SHAPES = [(1, 1), (3, 5), (7, 16), (6, 31), (9, 32), (5, 33), (8, 48), (70, 100), (4, 2049), (33, 2048),
+          (2, 70003), (1030, 15), (513, 512)]
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,C", SHAPES, ids=[f"{R}x{C}" for R, C in SHAPES])
+def test_packed_form_bit_for_bit(R, C, bf16):
+    import torch
+    from paper_2606_00395_amd import binding as B
+    x = act(values(R, C), bf16)
+    q, e = do_pack(x)
+    rq, re = O.pack(x.float().cpu().numpy())
+    assert np.array_equal(e.cpu().numpy(), re)
+    assert np.array_equal(q.cpu().numpy(), rq)
+    back = torch.full_like(x, float("nan"))
+    B.act_unpack(q, e, back)
+    assert np.array_equal(host(back), O.unpack(rq, re))
+
+
+def test_groups_that_are_not_finite():
+    import torch
+    from paper_2606_00395_amd import binding as B
+    for bf16 in (True, False):
+        x = act(values(9, 200, 1), bf16)
+        x[5, 40], x[6, 199], x[7, 0] = float("nan"), float("inf"), float("-inf")
+        q, e = do_pack(x)
+        rq, re = O.pack(x.float().cpu().numpy())
+        assert np.array_equal(e.cpu().numpy(), re) and np.array_equal(q.cpu().numpy(), rq)
+        back = torch.empty_like(x)
+        B.act_unpack(q, e, back)
+        bad = np.isnan(host(back))
+        assert bad[5, 32:64].all() and bad[6, 192:].all() and bad[7, :32].all() and bad.sum() == 32 + 8 + 32
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,m", [(1, 1), (3, 7), (5, 16), (4, 32), (130, 48), (65, 96), (17, 333), (9, 1408),
+                                 (300, 768), (2, 40001)])
+def test_swiglu_and_its_backward(R, m, bf16):
+    import torch
+    from paper_2606_00395_amd import binding as B
+    g = np.random.default_rng([R, m])
+    au = act(np.concatenate([g.normal(0, 4, (R, m)), g.normal(0, 1, (R, m))], 1), bf16)
+    au[0, 0] = -100.0 if m > 1 else 2.0
+    dh = act(g.standard_normal((R, m)), bf16)
+    h, hb, dau = torch.full_like(dh, float("nan")), torch.full_like(dh, float("nan")), torch.full_like(au, float("nan"))
+    q, e = packed_like(R, 2 * m)
+    B.swiglu_pack(au, h, q, e)
+    rq, re = O.pack(au.float().cpu().numpy())
+    assert np.array_equal(e.cpu().numpy(), re) and np.array_equal(q.cpu().numpy(), rq)
+    half = 2.0 ** -8 if bf16 else 0.0
+    a, u, d = host(au)[:, :m], host(au)[:, m:], host(dh)
+    want = O.swiglu(a, u)
+    assert np.all(np.abs(host(h) - want) <= (1e-6 * (1 + np.abs(a)) + half) * np.abs(want) + 1e-37)
+
+    B.swiglu_backward_packed(q, e, dh, dau, hb)
+    v = O.unpack(rq, re)
+    a, u = v[:, :m], v[:, m:]
+    da, du, want = O.swiglu_backward(a, u, d)
+    got = host(dau)
+    s = 1e-6 * (1 + np.abs(a))
+    assert np.all(np.abs(host(hb) - want) <= (s + half) * np.abs(want) + 1e-37)
+    assert np.all(np.abs(got[:, m:] - du) <= (s + half) * np.abs(du) + 1e-37)
+    assert np.all(np.abs(got[:, :m] - da) <= s * (1 + np.abs(a)) * np.abs(d * u) + half * np.abs(da) + 1e-37)
+    again = torch.full_like(dau, float("nan"))
+    B.swiglu_backward_packed(q, e, dh, again)           # without h
+    assert torch.equal(again, dau)
+
+
+def check_wgrad(dy, x, offsets=None, route=None, k=1, N=1):
+    import torch
+    from paper_2606_00395_amd import binding as B
+    q, e = do_pack(x)
+    dW = torch.full((N, dy.shape[1], x.shape[1]), float("nan"), device="cuda")
+    B.weight_grad_packed(dy, q, e, dW, offsets=offsets, route_of_row=route, k=k)
+    v = O.unpack(*O.pack(x.float().cpu().numpy()))
+    off = None if offsets is None else offsets.cpu().numpy()
+    want, mag = O.weight_grad(host(dy), v, off, None if route is None else route.cpu().numpy(), k)
+    rows = dy.shape[0] if off is None else int(max(np.diff(off)))
+    err = np.abs(host(dW) - want)
+    assert np.all(err <= (rows + 2) * 2.0 ** -23 * mag + 1e-37), (err - (rows + 2) * 2.0 ** -23 * mag).max()
+    return dW
+
+
+LINEAR = [(1, 1, 1), (2, 8, 16), (3, 70, 33), (31, 256, 256), (32, 264, 272), (33, 8, 512), (100, 135, 203),
+          (257, 520, 48), (1000, 256, 512), (2049, 64, 96), (130, 1032, 1040), (5000, 300, 260), (640, 2048, 64)]
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,n_out,n_in", LINEAR, ids=["x".join(map(str, c)) for c in LINEAR])
+def test_weight_gradient_of_one_layer(R, n_out, n_in, bf16):
+    g = np.random.default_rng([R, n_out, n_in])
+    check_wgrad(act(g.standard_normal((R, n_out)), bf16), act(g.standard_normal((R, n_in)), bf16))
+
+
+# T, N, k, n_out, n_in, dropped: experts without rows, with one row, with several hundred
+EXPERTS = [(1, 4, 1, 16, 32, 0.0), (5, 40, 3, 256, 256, 0.3), (40, 3, 2, 64, 96, 0.0), (300, 5, 2, 520, 272, 0.1),
+           (700, 8, 4, 264, 512, 0.0), (500, 1, 1, 512, 288, 0.0), (64, 60, 4, 1536, 256, 0.0), (333, 7, 3, 135, 203, 0.2)]
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("case", EXPERTS, ids=["x".join(map(str, c)) for c in EXPERTS])
+def test_weight_gradients_of_experts(case, bf16):
+    import torch
+    T, N, k, n_out, n_in, drop = case
+    g = np.random.default_rng(case[:5])
+    # a load as uneven as a hot expert makes it
+    w = np.exp(g.normal(0, 1.5, N))
+    idx = np.stack([g.choice(N, k, replace=False, p=w / w.sum()) for _ in range(T)])
+    idx = np.where(g.random((T, k)) < drop, -1, idx)
+    off, _, route = O.dispatch_plan(idx, N)
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+    dy = g.standard_normal((T * k, n_out))
+    dy[off[-1]:] = np.nan                               # rows of no expert are not read
+    dW = check_wgrad(act(dy, bf16), act(g.standard_normal((T, n_in)), bf16), i32(off), i32(route), k, N)
+    empty = np.nonzero(np.diff(off) == 0)[0]
+    assert torch.all(dW[torch.from_numpy(empty).cuda()] == 0)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_rows_without_a_source_add_nothing(bf16):
+    import torch
+    g = np.random.default_rng(3)
+    R, T, k = 100, 50, 2
+    route = g.integers(0, T * k, R)
+    route[10], route[40], route[99], route[5] = -1, T * k, 2 ** 31 - 1, -2 ** 31
+    dy = g.standard_normal((R, 264))
+    dy[[10, 40, 99, 5]] = np.inf
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+    from paper_2606_00395_amd import binding as B
+    x = act(g.standard_normal((T, 288)), bf16)
+    q, e = do_pack(x)
+    dW = torch.empty((1, 264, 288), device="cuda")
+    B.weight_grad_packed(act(dy, bf16), q, e, dW, offsets=i32([0, R]), route_of_row=i32(route), k=k)
+    keep = np.ones(R, bool)
+    keep[[10, 40, 99, 5]] = False
+    dyh = host(act(dy, bf16))
+    v = O.unpack(*O.pack(x.float().cpu().numpy()))
+    want, mag = O.weight_grad(dyh[keep], v, [0, keep.sum()], route[keep], k)
+    assert np.all(np.abs(host(dW) - want) <= (R + 2) * 2.0 ** -23 * mag)
+
+
+def test_infinite_gradients_stay_in_their_rows_and_columns():
+    """An infinity in one row and column of dy reaches that output row alone, with the
+    sign of its products; padding of tiles and of the last step adds no NaN."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    for bf16 in (True, False):
+        g = np.random.default_rng(4)
+        dy = act(g.standard_normal((77, 272)), bf16)
+        dy[76, 271] = float("inf")
+        x = act(np.abs(g.standard_normal((77, 304))) + 0.1, bf16)
+        q, e = do_pack(x)
+        dW = torch.empty((1, 272, 304), device="cuda")
+        B.weight_grad_packed(dy, q, e, dW)
+        assert torch.isinf(dW[0, 271]).all() and torch.isfinite(dW[0, :271]).all()
+
+
+def test_no_rows_give_zeros():
+    import torch
+    from paper_2606_00395_amd import binding as B
+    dW = torch.full((3, 8, 64), 5.0, device="cuda")
+    dy = torch.empty((0, 8), dtype=torch.bfloat16, device="cuda")
+    q, e = packed_like(0, 64)
+    B.weight_grad_packed(dy, q, e, dW, offsets=torch.zeros(4, dtype=torch.int32, device="cuda"),
+                         route_of_row=torch.empty(0, dtype=torch.int32, device="cuda"), k=2)
+    assert torch.all(dW == 0)
+    B.act_pack(torch.empty((0, 64), device="cuda"), q, e)
+
+
+def test_offsets_past_two_to_the_31():
+    """Packed and unpacked elements at indexes above 2^31, weight gradients of rows there."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    R, C = 2 ** 20 + 77, 2080
+    assert R * C > 2 ** 31
+    x = torch.zeros((R, C), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    tail = torch.randn((64, C), generator=g, device="cuda").to(torch.bfloat16)
+    x[-64:] = tail
+    q, e = do_pack(x)
+    tq, te = do_pack(tail)
+    assert torch.equal(q[-64:], tq) and torch.equal(e[-64:], te) and not q[:-64].any()
+    B.act_unpack(q, e, x)
+    small = torch.empty_like(tail)
+    B.act_unpack(tq, te, small)
+    assert torch.equal(x[-64:], small)
+    # the last rows alone have an expert
+    dy = torch.randn((64, 72), generator=g, device="cuda").to(torch.bfloat16)
+    route = torch.arange(R - 64, R, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 64], dtype=torch.int32, device="cuda")
+    a, b = torch.empty((1, 72, C), device="cuda"), torch.empty((1, 72, C), device="cuda")
+    B.weight_grad_packed(dy, q, e, a, offsets=off, route_of_row=route)
+    B.weight_grad_packed(dy, tq, te, b)
+    assert torch.equal(a, b)
+
+
+def test_another_stream_and_graph_replays():
+    import torch
+    from paper_2606_00395_amd import binding as B
+    T, N, k, d, m = 400, 6, 2, 256, 128
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    ids = torch.topk(torch.randn((T, N), generator=g, device="cuda"), k).indices.to(torch.int32).contiguous()
+    off, _, route = (torch.from_numpy(a.astype(np.int32)).cuda() for a in O.dispatch_plan(ids.cpu().numpy(), N))
+    x, au, dh = rnd(T, d), rnd(T * k, 2 * m), rnd(T * k, m)
+    q, e = packed_like(T, d)
+    qa, ea = packed_like(T * k, 2 * m)
+    h, dau, hb = torch.empty_like(dh), torch.empty_like(au), torch.empty_like(dh)
+    dW = torch.empty((N, 2 * m, d), device="cuda")
+    outs = (q, e, qa, ea, h, dau, hb, dW)
+
+    def step(st=None):
+        B.act_pack(x, q, e, stream=st)
+        B.swiglu_pack(au, h, qa, ea, stream=st)
+        B.swiglu_backward_packed(qa, ea, dh, dau, hb, stream=st)
+        B.weight_grad_packed(dau, q, e, dW, offsets=off, route_of_row=route, k=k, stream=st)
+
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    side = torch.cuda.Stream()
+    for t in outs:
+        t.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for rep in range(3):
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), rep
+        B.act_pack(torch.roll(x, 1, 0), *packed_like(T, d))
+        torch.cuda.synchronize()
+
+
+def test_refusals_of_the_binding():
+    import torch
+    from paper_2606_00395_amd import binding as B
+    x = torch.zeros((4, 64), device="cuda")
+    q, e = packed_like(4, 64)
+    with pytest.raises(TypeError):
+        B.act_pack(x.half(), q, e)
+    with pytest.raises(ValueError):
+        B.act_pack(x, q, e[:, :1])
+    with pytest.raises(TypeError):
+        B.act_pack(x, q.to(torch.uint8), e)
+    with pytest.raises(ValueError):
+        B.act_pack(x[:, ::2], *packed_like(4, 32))
+    with pytest.raises(ValueError):
+        B.swiglu_pack(torch.zeros((4, 63), device="cuda"), x, q, e)
+    with pytest.raises(ValueError):
+        B.weight_grad_packed(x, q, e, torch.zeros((2, 64, 64), device="cuda"))
+    with pytest.raises(B.Pr2Error, match="R = 8"):
+        B.weight_grad_packed(torch.zeros((8, 4), device="cuda"), q, e, torch.zeros((1, 4, 64), device="cuda"))
