@@ -1406,6 +1406,12 @@ hipError_t launch_zero_grads(const pr2_moe_desc& d, const BwdGrads& out, hipStre
     return zero(out.dW_down, wmd, s);
 }
 
+hipError_t launch_expert_order(const int* offsets, int N, int* order, hipStream_t s) {
+    LaunchScope scope("expert_order", s);
+    hipLaunchKernelGGL(expert_order_kernel, dim3(1), dim3(1024), 0, s, offsets, N, order);
+    return hipGetLastError();
+}
+
 hipError_t launch_replay_backward(const pr2_moe_desc& d, const void* x, const void* idx,
                                   int64_t ldi, const float* W_r, const void* W_gate,
                                   const void* W_up, const void* W_down, const void* dy,

@@ -295,6 +295,8 @@ hipError_t launch_predictor_zero(const pr2_moe_desc& d, float* kl_out, float* lo
                                  float* dB, hipStream_t s);
 
 // backward.hip
+// experts by decreasing row count (ties: lower id) from their N + 1 offsets
+hipError_t launch_expert_order(const int* offsets, int N, int* order, hipStream_t s);
 bool bwd_mfma_ok(const pr2_moe_desc& d);
 int bwd_partials(const pr2_moe_desc& d);    // partial gate-gradient sums per route
 int literal_chunks(const pr2_moe_desc& d);      // dW_r partials of the paper-literal backward

@@ -4,6 +4,8 @@
 //
 // A packed value is an int8 times a power of two, exact in bf16 and fp32, so nothing is
 // rounded on the way into the products.
+#include <type_traits>
+
 #include "chunk.h"
 
 namespace pr2 {
@@ -19,6 +21,10 @@ struct WgradArgs {
     int64_t R, Rx;
     int n_out, n_in, N, k;
     int groups;
+    // MFMA form
+    const int* order;           // [N] experts by decreasing row count; null with one weight
+    float* part;                // [S, N, n_out, n_in] partial sums of S > 1 slices of the rows
+    int S;
 };
 
 // rows of expert e, clamped to the R that there are
@@ -95,6 +101,330 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         }
 }
 
+// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs per workgroup, eight
+// wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through
+// four LDS stages of 16 KiB per operand.  Both operands lie along K rows of 512 bytes (the
+// tile's 256 columns as bf16) and are read as fragments by the transposing LDS read.  dy is
+// copied into LDS directly by four of the wavefronts; the other four load the packed rows
+// (8 KiB a step, half of dy's bytes), turn them into bf16 in registers and write them.
+// Row indexes go to LDS 8192 at a time; a row past the last one or without a source is zeros
+// in both operands, since a zero of one would turn an infinity of the other into NaN.
+constexpr int BM = 256, BN = 256;
+constexpr int kBK = 32;
+constexpr int kStages = 4;
+constexpr int WM = 64, WN = 128;
+constexpr int MI = WM / 32, NJ = WN / 32;
+constexpr int kMfmaThreads = 512;
+constexpr int kOpB = kBK * 512;
+constexpr int kStageB = 2 * kOpB;
+constexpr int kCopies = 4;              // copies per dy wavefront and step
+constexpr int kRowsHeld = 8192;
+constexpr int kNumXcd = 8;
+constexpr uint32_t kNoRow = 0xffffffffu;
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+__device__ __attribute__((aligned(16))) const bf16_t kZeros[8] = {};
+
+template <int n>
+__device__ __forceinline__ void wait_vmcnt() {
+    static_assert(n >= 0 && n < 16, "vmcnt field");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | n);
+}
+
+// 16 packed values as bf16 (exact): two 16-byte chunks
+struct Opened {
+    u32x4 lo, hi;
+};
+__device__ __forceinline__ Opened open_packed(const u32x4& q, float step) {
+    Opened r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        // the upper halves of the fp32 values, which have no lower bits
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = __float_as_uint((float)((int)(q[i] << (24 - 8 * j)) >> 24) * step);
+        const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
+        const uint32_t b = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
+        if (i < 2) {
+            r.lo[2 * i] = a;
+            r.lo[2 * i + 1] = b;
+        } else {
+            r.hi[2 * i - 4] = a;
+            r.hi[2 * i - 3] = b;
+        }
+    }
+    return r;
+}
+
+__global__ void __launch_bounds__(kMfmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+wgrad_mfma_kernel(WgradArgs a) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStageB];
+    __shared__ __attribute__((aligned(16))) uint32_t src[kRowsHeld];
+
+    // Work items (expert, slice, tile); experts are dealt to the XCDs round-robin in
+    // decreasing row count and an expert's tiles run on one XCD, whose L2 then holds its rows.
+    // One weight's tiles are dealt to the XCDs in contiguous ranges.
+    const int nct = (a.n_in + BN - 1) / BN;
+    const int nrt = (a.n_out + BM - 1) / BM;
+    const int per_e = nrt * nct * a.S;
+    int expert = 0, item;
+    if (a.order) {
+        const int xcd = blockIdx.x % kNumXcd;
+        const int local = blockIdx.x / kNumXcd;
+        const int slot = xcd + kNumXcd * (local / per_e);
+        if (slot >= a.N) return;
+        expert = __builtin_amdgcn_readfirstlane(a.order[slot]);
+        item = local % per_e;
+    } else {
+        const int each = (per_e + kNumXcd - 1) / kNumXcd;
+        item = (blockIdx.x % kNumXcd) * each + blockIdx.x / kNumXcd;
+        if (item >= per_e) return;
+    }
+    const int slice = item / (nrt * nct);
+    const int rt = item % (nrt * nct) / nct;
+    const int ct = item % nct;
+    int row0, last;
+    expert_rows(a, expert, &row0, &last);
+    if (a.S > 1) {
+        const int len = (((last - row0 + a.S - 1) / a.S) + kBK - 1) / kBK * kBK;
+        row0 = min(last, row0 + slice * len);
+        last = min(last, row0 + len);
+    }
+    row0 = __builtin_amdgcn_readfirstlane(row0);
+    const int klen = __builtin_amdgcn_readfirstlane(last) - row0;
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1;    // 64-row and 128-column block of the tile
+    const bool packs = wave >= 4;               // loads the packed operand, not dy
+    const int wq = wave & 3;                    // K rows 8 wq .. 8 wq + 7 of a step
+    // blocks past the matrix: their wavefronts only load
+    const bool active = rt * BM + wr * WM < a.n_out && ct * BN + wc * WN < a.n_in;
+
+    // dy: copy i moves K rows 8 wq + 2 i (lanes 0-31) and + 1 (lanes 32-63); chunk c of K row
+    // kr is stored at c ^ 4 (kr & 3)
+    const int hi = lane >> 5;
+    const int dcol[2] = {8 * ((lane & 31) ^ (4 * hi)), 8 * ((lane & 31) ^ (4 * (hi + 2)))};
+    const bool din[2] = {rt * BM + dcol[0] < a.n_out, rt * BM + dcol[1] < a.n_out};
+    const bf16_t* const dy = (const bf16_t*)a.dy + (int64_t)row0 * a.n_out + rt * BM;
+    // packed rows: piece p of a lane is row 8 wq + 4 p + lane / 16, columns 16 (lane % 16) on
+    const int pcol = ct * BN + 16 * (lane & 15);
+    const bool pin = pcol < a.n_in;
+    const int8_t* const qcol = a.q + (pin ? pcol : 0);
+    const uint8_t* const scol = a.scale + (pin ? pcol / 32 : 0);
+    // stored as chunks 2 (lane % 16) and + 1 of K row kr at c ^ 4 (kr & 3), kr & 3 = lane / 16
+    const int pchunk = (2 * (lane & 15)) ^ (4 * (lane >> 4));
+
+    f32x16 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+    // MFMA fragments by two transposing reads each
+    const int s16 = lane & 15, g4 = lane >> 4;
+    const int nl = 16 * (g4 & 1) + 4 * (s16 & 3);
+    const int kl = 8 * (g4 >> 1) + (s16 >> 2);
+    const int tsw = (nl >> 3) ^ (4 * (kl & 3));
+    auto tr_pos = [&](int cb) { return kl * 512 + ((((cb >> 3) ^ tsw)) << 4) + ((nl & 4) << 1); };
+    int a_pos[MI], b_pos[NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) a_pos[i] = tr_pos(wr * WM + i * 32);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) b_pos[j] = kOpB + tr_pos(wc * WN + j * 32);
+
+    auto barrier = [&]() __attribute__((always_inline)) {
+        // a plain barrier: __syncthreads() would wait for every load in flight
+        __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+
+    for (int kc = 0; kc < klen; kc += kRowsHeld) {
+        const int clen = min(kRowsHeld, klen - kc);
+        const int nh = (clen + kBK - 1) / kBK;
+        if (kc > 0) barrier();       // the last chunk's readers of src and of the stages are done
+        for (int i = tid; i < nh * kBK; i += kMfmaThreads)
+            src[i] = i < clen ? (uint32_t)source_row(a, row0 + kc + i) : kNoRow;
+        barrier();
+
+        auto copy_dy = [&](int h) __attribute__((always_inline)) {
+            unsigned char* dst = lds + (h % kStages) * kStageB + wq * 4096;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const int r = h * kBK + 8 * wq + 2 * i + hi;
+                const bool ok = src[r] != kNoRow && din[i & 1];
+                dma16(ok ? dy + (int64_t)(kc + r) * a.n_out + dcol[i & 1] : kZeros, dst + i * 1024);
+            }
+        };
+        // packed pieces in flight: two steps' worth
+        u32x4 q[2][2];
+        uint32_t sb[2][2];
+        auto load_packed = [&](auto S_, int h) __attribute__((always_inline)) {
+            constexpr int S = decltype(S_)::value;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const uint32_t t = src[h * kBK + 8 * wq + 4 * p + (lane >> 4)];
+                const bool ok = t != kNoRow && pin;
+                const int64_t row = ok ? t : 0;
+                q[S][p] = *(const u32x4*)(qcol + row * a.n_in);
+                const uint32_t b = scol[row * a.groups];
+                sb[S][p] = ok ? b : 0u;
+            }
+        };
+        auto write_packed = [&](auto S_, int h) __attribute__((always_inline)) {
+            constexpr int S = decltype(S_)::value;
+            unsigned char* dst = lds + (h % kStages) * kStageB + kOpB + (8 * wq + (lane >> 4)) * 512;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const Opened o = open_packed(q[S][p], __uint_as_float(sb[S][p] << 23));
+                *(u32x4*)(dst + p * 2048 + pchunk * 16) = o.lo;
+                *(u32x4*)(dst + p * 2048 + (pchunk ^ 1) * 16) = o.hi;
+            }
+        };
+        using C0 = std::integral_constant<int, 0>;
+        using C1 = std::integral_constant<int, 1>;
+        // at most n steps' copies may still be in flight
+        auto wait_steps = [&](int n) __attribute__((always_inline)) {
+            if (n >= 3) wait_vmcnt<3 * kCopies>();
+            else if (n == 2) wait_vmcnt<2 * kCopies>();
+            else if (n == 1) wait_vmcnt<kCopies>();
+            else wait_vmcnt<0>();
+        };
+        // dy's steps 0..3 are copied, the packed steps 0 and 1 written, 2 and 3 in flight
+        if (packs) {
+            load_packed(C0{}, 0);
+            if (nh > 1) load_packed(C1{}, 1);
+            write_packed(C0{}, 0);
+            if (nh > 1) write_packed(C1{}, 1);
+            if (nh > 2) load_packed(C0{}, 2);
+            if (nh > 3) load_packed(C1{}, 3);
+        } else {
+            for (int h = 0; h < min(nh, kStages); ++h) copy_dy(h);
+            wait_steps(min(nh, kStages) - 1);
+        }
+        barrier();
+
+        bf16x8 fa[2][MI], fb[2][NJ];
+        auto tr_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
+            const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * 512));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        // MFMAs on fragment set S, and among them the reads of sub-step ks of a stage into
+        // the other set
+        auto phase = [&](auto S_, int stage, int ks) __attribute__((always_inline)) {
+            constexpr int S = decltype(S_)::value;
+            const unsigned char* base = lds + stage * kStageB + ks * (16 * 512);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == 0) {
+                    fa[S ^ 1][0] = tr_frag(base + a_pos[0]);
+                    fa[S ^ 1][1] = tr_frag(base + a_pos[1]);
+                } else if (j < 3) {
+                    fb[S ^ 1][2 * j - 2] = tr_frag(base + b_pos[2 * j - 2]);
+                    fb[S ^ 1][2 * j - 1] = tr_frag(base + b_pos[2 * j - 1]);
+                }
+            }
+        };
+        // Step h between its two sub-steps: every wavefront holds the step's last fragments, so
+        // its stage is free for dy's step h + 4; the packed step h + 2 goes into a stage that
+        // has been free since step h - 2, and h + 4 is fetched.
+        auto turn = [&](auto S_, int h) __attribute__((always_inline)) {
+            if (packs) {
+                barrier();
+                if (h + 2 < nh) write_packed(S_, h + 2);
+                if (h + 4 < nh) load_packed(S_, h + 4);
+            } else {
+                wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
+                barrier();
+                if (h + kStages < nh) copy_dy(h + kStages);
+            }
+        };
+        auto step = [&](auto S_, int h) __attribute__((always_inline)) {
+            if (active) phase(C0{}, h % kStages, 1);
+            turn(S_, h);
+            // (past the last step the reads fetch an old stage; unused)
+            if (active) phase(C1{}, (h + 1) % kStages, 0);
+        };
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) fa[0][i] = tr_frag(lds + a_pos[i]);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
+        }
+        int h = 0;
+        for (; h + 1 < nh; h += 2) {
+            step(C0{}, h);
+            step(C1{}, h + 1);
+        }
+        if (h < nh) step(C0{}, h);
+    }
+    // Lane l holds output row l % 32 of each 32-row block and columns 8 (v / 4) + 4 (l / 32) +
+    // v % 4 of each 32-column block.  The rows are staged through this wavefront's share of
+    // the freed stages, one 32-row block at a time, and stored 16 bytes per lane along whole
+    // row segments, non-temporally: gradients are not read again here.
+    const int ncol0 = 4 * (lane >> 5);
+    __syncthreads();
+    if (!active) return;
+    float* const out = a.S > 1 ? a.part + (int64_t)slice * a.N * a.n_out * a.n_in : a.dW;
+    constexpr int RB = WN * 4, NCH = RB / 16;
+    unsigned char* sw = lds + wave * (32 * RB);
+    const int rows_left = a.n_out - rt * BM - wr * WM;
+    const int cols_left = a.n_in - ct * BN - wc * WN;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int row = lane & 31;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int a4 = 0; a4 < 4; ++a4) {
+                const int col = j * 32 + 8 * a4 + ncol0;
+                const int v0 = 4 * a4;
+                *(f32x4*)(sw + row * RB + (((col >> 2) ^ (row & (NCH - 1))) << 4)) =
+                    f32x4{acc[i][j][v0], acc[i][j][v0 + 1], acc[i][j][v0 + 2], acc[i][j][v0 + 3]};
+            }
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_wave_barrier();
+        const int ch = lane % NCH;
+#pragma unroll
+        for (int p = 0; p < 32 / (64 / NCH); ++p) {
+            const int row2 = p * (64 / NCH) + lane / NCH;
+            const int o = i * 32 + row2;
+            if (o < rows_left && ch * 4 < cols_left) {
+                float* orow = out + ((int64_t)expert * a.n_out + rt * BM + wr * WM + o) * a.n_in;
+                __builtin_nontemporal_store(*(const u32x4*)(sw + row2 * RB + ((ch ^ (row2 & (NCH - 1))) << 4)),
+                                            (u32x4*)(orow + ct * BN + wc * WN + ch * 4));
+            }
+        }
+        // the next block overwrites the region
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// dW = the slices' partial sums in slice order, four elements per thread
+__global__ void __launch_bounds__(256) wgrad_join_kernel(const float* part, int64_t n, int S, float* dW) {
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    f32x4 v = *(const f32x4*)(part + i);
+    for (int s = 1; s < S; ++s) v += *(const f32x4*)(part + s * n + i);
+    *(f32x4*)(dW + i) = v;
+}
+
 // ------------------------------------------------------------------ host ----
 pr2_status check_wgrad(const pr2_wgrad_desc* desc) {
     if (!desc) return fail(PR2_ERR_NULL, "desc is NULL");
@@ -113,7 +443,73 @@ pr2_status check_wgrad(const pr2_wgrad_desc* desc) {
                     (long long)d.R, (long long)d.Rx);
     if (d.n_out > (1 << 20) || d.n_in > (1 << 20))
         return fail(PR2_ERR_UNSUPPORTED, "n_out = %d or n_in = %d > 2^20", d.n_out, d.n_in);
+    if (((int64_t)(d.n_out + 63) / 64) * ((d.n_in + 63) / 64) * d.N > 0x7fffffff / 64)
+        return fail(PR2_ERR_UNSUPPORTED, "N n_out n_in is too large");
     return PR2_OK;
+}
+
+bool mfma_ok(const pr2_wgrad_desc& d) {
+    return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % 16 == 0;
+}
+
+int64_t mfma_tiles(const pr2_wgrad_desc& d) {
+    return (int64_t)((d.n_out + BM - 1) / BM) * ((d.n_in + BN - 1) / BN);
+}
+
+// Slices of the rows: with fewer tiles than CUs, as many as fill them once, each of at least
+// 256 rows (which pay for a tile's start, its stores and the join).
+constexpr int kCus = 256;
+int mfma_slices(const pr2_wgrad_desc& d) {
+    const int64_t tiles = mfma_tiles(d) * d.N;
+    const int64_t rows = d.R / d.N / 256;
+    int64_t s = kCus / tiles;
+    if (s > rows) s = rows;
+    return s < 1 ? 1 : (int)s;
+}
+
+struct WgradWs {
+    int* order;
+    float* part;
+    size_t bytes;
+};
+
+WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
+    WgradWs w{};
+    if (!mfma_ok(d)) return w;
+    char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
+    const size_t order = (sizeof(int) * (size_t)d.N + 255) & ~(size_t)255;
+    const int S = mfma_slices(d);
+    w.order = (int*)p;
+    w.part = (float*)(p ? p + order : nullptr);
+    w.bytes = order + (S > 1 ? sizeof(float) * (size_t)S * d.N * d.n_out * d.n_in : 0) + 256;
+    return w;
+}
+
+hipError_t launch_mfma(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
+    const int64_t tiles = mfma_tiles(d);
+    a.S = mfma_slices(d);
+    a.part = w.part;
+    int64_t grid;
+    hipError_t e;
+    if (d.N > 1) {
+        e = launch_expert_order(a.offsets, d.N, w.order, st);
+        if (e != hipSuccess) return e;
+        a.order = w.order;
+        grid = tiles * a.S * ((d.N + kNumXcd - 1) / kNumXcd) * kNumXcd;
+    } else {
+        grid = (tiles * a.S + kNumXcd - 1) / kNumXcd * kNumXcd;
+    }
+    {
+        LaunchScope scope("wgrad_mfma", st);
+        hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess || a.S == 1) return e;
+    const int64_t n = (int64_t)d.N * d.n_out * d.n_in;
+    LaunchScope scope("wgrad_join", st);
+    hipLaunchKernelGGL(wgrad_join_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st,
+                       a.part, n, a.S, a.dW);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -124,8 +520,10 @@ using namespace pr2;
 extern "C" {
 
 size_t pr2_weight_grad_workspace_bytes(const pr2_wgrad_desc* desc) {
-    (void)desc;
-    return 0;
+    if (!desc || desc->N < 1 || desc->N > kMaxExperts || desc->R < 0 || desc->n_out < 1 ||
+        desc->n_in < 1 || desc->n_out > (1 << 20) || desc->n_in > (1 << 20) || desc->R > 0x7fffffff)
+        return 0;
+    return wgrad_ws(*desc, nullptr).bytes;
 }
 
 pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, const int8_t* q,
@@ -157,16 +555,19 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
     drop_split_records(ws, ws_bytes);
     const hipStream_t st = (hipStream_t)stream;
     WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
-                d.N, d.k, (d.n_in + 31) / 32};
-    const unsigned tiles = (unsigned)((d.n_out + kTile - 1) / kTile) * ((d.n_in + kTile - 1) / kTile);
-    {
+                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1};
+    hipError_t e;
+    if (d.R > 0 && mfma_ok(d)) {
+        e = launch_mfma(d, a, wgrad_ws(d, ws), st);
+    } else {
+        const int64_t tiles = (int64_t)((d.n_out + kTile - 1) / kTile) * ((d.n_in + kTile - 1) / kTile);
         LaunchScope scope("wgrad_tile", st);
         if (d.act_dtype == PR2_BF16)
-            hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, dim3(tiles, d.N), dim3(256), 0, st, a);
+            hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, dim3((unsigned)tiles, d.N), dim3(256), 0, st, a);
         else
-            hipLaunchKernelGGL(wgrad_tile_kernel<float>, dim3(tiles, d.N), dim3(256), 0, st, a);
+            hipLaunchKernelGGL(wgrad_tile_kernel<float>, dim3((unsigned)tiles, d.N), dim3(256), 0, st, a);
+        e = hipGetLastError();
     }
-    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return hip_fail(e, "weight_grad_packed launch");
     return ok();
 }
