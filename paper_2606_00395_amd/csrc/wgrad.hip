@@ -101,24 +101,19 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         }
 }
 
-// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs per workgroup, eight
-// wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through
-// four LDS stages of 16 KiB per operand.  Both operands lie along K rows of 512 bytes (the
-// tile's 256 columns as bf16) and are read as fragments by the transposing LDS read.  dy is
-// copied into LDS directly by four of the wavefronts; the other four load the packed rows
-// (8 KiB a step, half of dy's bytes), turn them into bf16 in registers and write them.
-// Row indexes go to LDS 8192 at a time; a row past the last one or without a source is zeros
-// in both operands, since a zero of one would turn an infinity of the other into NaN.
-constexpr int BM = 256, BN = 256;
+// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x BN outputs per workgroup, NW
+// wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through a
+// ring of LDS stages.  Both operands lie along K rows (the tile's columns as bf16) and are
+// read as fragments by the transposing LDS read.  dy is copied into LDS directly by half of
+// the wavefronts; the other half loads the packed rows (half of dy's bytes), turns them into
+// bf16 in registers, among its MFMAs, and writes them.
+// Row indexes go to LDS a few thousand at a time; a row past the last one or without a source
+// is zeros in both operands, since a zero of one would turn an infinity of the other into NaN.
+constexpr int BM = 256;
 constexpr int kBK = 32;
-constexpr int kStages = 4;
 constexpr int WM = 64, WN = 128;
 constexpr int MI = WM / 32, NJ = WN / 32;
-constexpr int kMfmaThreads = 512;
-constexpr int kOpB = kBK * 512;
-constexpr int kStageB = 2 * kOpB;
-constexpr int kCopies = 4;              // copies per dy wavefront and step
-constexpr int kRowsHeld = 8192;
+constexpr int kOpA = kBK * 512;
 constexpr int kNumXcd = 8;
 constexpr uint32_t kNoRow = 0xffffffffu;
 
@@ -128,40 +123,47 @@ __device__ __attribute__((aligned(16))) const bf16_t kZeros[8] = {};
 
 template <int n>
 __device__ __forceinline__ void wait_vmcnt() {
-    static_assert(n >= 0 && n < 16, "vmcnt field");
-    __builtin_amdgcn_s_waitcnt(0x0f70 | n);
+    static_assert(n >= 0 && n < 64, "vmcnt field");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | (n & 15) | ((n >> 4) << 14));
 }
 
-// 16 packed values as bf16 (exact): two 16-byte chunks
-struct Opened {
-    u32x4 lo, hi;
-};
-__device__ __forceinline__ Opened open_packed(const u32x4& q, float step) {
-    Opened r;
+// 8 packed values as bf16 (exact).  With the sign bit flipped a byte is the value plus 128,
+// and one fused multiply-add takes the 128 off again.
+__device__ __forceinline__ u32x4 open_packed(uint32_t q0, uint32_t q1, float step) {
+    u32x4 r;
+    const float off = -128.0f * step;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t u = (i ? q1 : q0) ^ 0x80808080u;
+        const uint32_t w0 = __float_as_uint(fmaf((float)(u & 255u), step, off));
+        const uint32_t w1 = __float_as_uint(fmaf((float)((u >> 8) & 255u), step, off));
+        const uint32_t w2 = __float_as_uint(fmaf((float)((u >> 16) & 255u), step, off));
+        const uint32_t w3 = __float_as_uint(fmaf((float)(u >> 24), step, off));
         // the upper halves of the fp32 values, which have no lower bits
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = __float_as_uint((float)((int)(q[i] << (24 - 8 * j)) >> 24) * step);
-        const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x07060302u);
-        const uint32_t b = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
-        if (i < 2) {
-            r.lo[2 * i] = a;
-            r.lo[2 * i + 1] = b;
-        } else {
-            r.hi[2 * i - 4] = a;
-            r.hi[2 * i - 3] = b;
-        }
+        r[2 * i] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
+        r[2 * i + 1] = __builtin_amdgcn_perm(w3, w2, 0x07060302u);
     }
     return r;
 }
 
-__global__ void __launch_bounds__(kMfmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-wgrad_mfma_kernel(WgradArgs a) {
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStageB];
-    __shared__ __attribute__((aligned(16))) uint32_t src[kRowsHeld];
+template <int NW>
+struct Shape {
+    static constexpr int BN = 32 * NW;
+    static constexpr int kThreads = 64 * NW;
+    static constexpr int kStages = NW == 8 ? 4 : 3;
+    static constexpr int kPitch = 2 * BN;                       // bytes of a packed operand's K row
+    static constexpr int kStageB = kOpA + kBK * kPitch;
+    static constexpr int kRows = NW == 8 ? 8128 : 1984;         // row indexes held in LDS
+    static constexpr int kCopies = 32 / NW;                     // per dy wavefront and step
+    static constexpr int kWaveRows = 64 / NW;                   // K rows of a step per loading wavefront
+};
+
+// One tile, for the wavefronts that load packed rows (PACKS) or dy: two instances, so that what
+// the one kind keeps in flight is no merge of both kinds' registers.
+template <int NW, bool PACKS>
+__device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* lds, uint32_t* src, int* s_bad) {
+    using P = Shape<NW>;
+    constexpr int BN = P::BN, kStages = P::kStages, kStageB = P::kStageB, kPitch = P::kPitch;
 
     // Work items (expert, slice, tile); experts are dealt to the XCDs round-robin in
     // decreasing row count and an expert's tiles run on one XCD, whose L2 then holds its rows.
@@ -198,25 +200,33 @@ wgrad_mfma_kernel(WgradArgs a) {
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wr = wave >> 1, wc = wave & 1;    // 64-row and 128-column block of the tile
-    const bool packs = wave >= 4;               // loads the packed operand, not dy
-    const int wq = wave & 3;                    // K rows 8 wq .. 8 wq + 7 of a step
+    const int wr = NW == 8 ? wave >> 1 : wave;  // 64-row block of the tile
+    const int wc = NW == 8 ? wave & 1 : 0;      // 128-column block
+    const int wq = wave % (NW / 2);
+    const int krow = P::kWaveRows * wq;         // its first K row of a step
     // blocks past the matrix: their wavefronts only load
     const bool active = rt * BM + wr * WM < a.n_out && ct * BN + wc * WN < a.n_in;
 
-    // dy: copy i moves K rows 8 wq + 2 i (lanes 0-31) and + 1 (lanes 32-63); chunk c of K row
-    // kr is stored at c ^ 4 (kr & 3)
+    // dy: copy i moves K rows krow + 2 i (lanes 0-31) and + 1 (lanes 32-63); chunk c of K row
+    // kr is stored at c ^ 4 (kr & 3).  (Columns past the matrix read its first: they reach
+    // only outputs that are not stored.)
     const int hi = lane >> 5;
-    const int dcol[2] = {8 * ((lane & 31) ^ (4 * hi)), 8 * ((lane & 31) ^ (4 * (hi + 2)))};
-    const bool din[2] = {rt * BM + dcol[0] < a.n_out, rt * BM + dcol[1] < a.n_out};
-    const bf16_t* const dy = (const bf16_t*)a.dy + (int64_t)row0 * a.n_out + rt * BM;
-    // packed rows: piece p of a lane is row 8 wq + 4 p + lane / 16, columns 16 (lane % 16) on
-    const int pcol = ct * BN + 16 * (lane & 15);
+    uint32_t doff[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = 8 * ((lane & 31) ^ (4 * (hi + 2 * i)));
+        doff[i] = 2u * (uint32_t)(hi * a.n_out + (rt * BM + c < a.n_out ? c : 0));
+    }
+    const bf16_t* const dy = (const bf16_t*)a.dy + (int64_t)(row0 + krow) * a.n_out + rt * BM;
+    // packed rows: piece p of a lane is 16 columns of K row krow + p kWaveRows / 2 + lane / kPer,
+    // stored as chunks pchunk and pchunk ^ 1
+    constexpr int kPer = BN / 16;               // lanes per row
+    const int prow = lane / kPer;
+    const int pcol = ct * BN + 16 * (lane % kPer);
     const bool pin = pcol < a.n_in;
     const int8_t* const qcol = a.q + (pin ? pcol : 0);
     const uint8_t* const scol = a.scale + (pin ? pcol / 32 : 0);
-    // stored as chunks 2 (lane % 16) and + 1 of K row kr at c ^ 4 (kr & 3), kr & 3 = lane / 16
-    const int pchunk = (2 * (lane & 15)) ^ (4 * (lane >> 4));
+    const int pchunk = (2 * (lane % kPer)) ^ (4 * (prow & 3));
 
     f32x16 acc[MI][NJ];
 #pragma unroll
@@ -231,12 +241,14 @@ wgrad_mfma_kernel(WgradArgs a) {
     const int nl = 16 * (g4 & 1) + 4 * (s16 & 3);
     const int kl = 8 * (g4 >> 1) + (s16 >> 2);
     const int tsw = (nl >> 3) ^ (4 * (kl & 3));
-    auto tr_pos = [&](int cb) { return kl * 512 + ((((cb >> 3) ^ tsw)) << 4) + ((nl & 4) << 1); };
+    auto tr_pos = [&](int cb, int pitch) {
+        return kl * pitch + ((((cb >> 3) ^ tsw)) << 4) + ((nl & 4) << 1);
+    };
     int a_pos[MI], b_pos[NJ];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) a_pos[i] = tr_pos(wr * WM + i * 32);
+    for (int i = 0; i < MI; ++i) a_pos[i] = tr_pos(wr * WM + i * 32, 512);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) b_pos[j] = kOpB + tr_pos(wc * WN + j * 32);
+    for (int j = 0; j < NJ; ++j) b_pos[j] = kOpA + tr_pos(wc * WN + j * 32, kPitch);
 
     auto barrier = [&]() __attribute__((always_inline)) {
         // a plain barrier: __syncthreads() would wait for every load in flight
@@ -248,82 +260,104 @@ wgrad_mfma_kernel(WgradArgs a) {
         asm volatile("" ::: "memory");
     };
 
-    for (int kc = 0; kc < klen; kc += kRowsHeld) {
-        const int clen = min(kRowsHeld, klen - kc);
+    for (int kc = 0; kc < klen; kc += P::kRows) {
+        const int clen = min(P::kRows, klen - kc);
         const int nh = (clen + kBK - 1) / kBK;
         if (kc > 0) barrier();       // the last chunk's readers of src and of the stages are done
-        for (int i = tid; i < nh * kBK; i += kMfmaThreads)
-            src[i] = i < clen ? (uint32_t)source_row(a, row0 + kc + i) : kNoRow;
+        bool none = false;
+        for (int i = tid; i < nh * kBK; i += P::kThreads) {
+            const uint32_t r = i < clen ? (uint32_t)source_row(a, row0 + kc + i) : kNoRow;
+            none |= i < clen && r == kNoRow;
+            src[i] = r;
+        }
+        const int bad = __ballot(none) != 0;
+        if (lane == 0) s_bad[wave] = bad;
         barrier();
-
-        auto copy_dy = [&](int h) __attribute__((always_inline)) {
-            unsigned char* dst = lds + (h % kStages) * kStageB + wq * 4096;
+        int any = 0;
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const int r = h * kBK + 8 * wq + 2 * i + hi;
-                const bool ok = src[r] != kNoRow && din[i & 1];
-                dma16(ok ? dy + (int64_t)(kc + r) * a.n_out + dcol[i & 1] : kZeros, dst + i * 1024);
+        for (int w = 0; w < NW; ++w) any |= s_bad[w];
+        // steps before this one have a source for every row
+        const int whole = __builtin_amdgcn_readfirstlane(any) ? 0 : clen / kBK;
+
+        auto stage_of = [&](int h) __attribute__((always_inline)) { return lds + (h % kStages) * kStageB; };
+        auto copy_dy = [&](int h, int i) __attribute__((always_inline)) {
+            unsigned char* dst = stage_of(h) + krow * 512 + i * 1024;
+            const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
+            if (h < whole) {
+                dma16_at(p, doff[i & 1], dst);
+            } else {
+                const bool ok = src[h * kBK + krow + 2 * i + hi] != kNoRow;
+                dma16(ok ? (const unsigned char*)p + doff[i & 1] : (const unsigned char*)kZeros, dst);
             }
         };
-        // packed pieces in flight: two steps' worth
+        // Packed pieces in flight: two steps' worth.  Nothing is computed from them on arrival
+        // (a row that is none reads row 0 and becomes zeros when it is opened) and a step past
+        // the end reads the last one again, so that the wait for a piece leaves the later ones
+        // in flight.
         u32x4 q[2][2];
         uint32_t sb[2][2];
         auto load_packed = [&](auto S_, int h) __attribute__((always_inline)) {
             constexpr int S = decltype(S_)::value;
+            const int k0 = min(h, nh - 1) * kBK + krow + prow;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                const uint32_t t = src[h * kBK + 8 * wq + 4 * p + (lane >> 4)];
-                const bool ok = t != kNoRow && pin;
-                const int64_t row = ok ? t : 0;
-                q[S][p] = *(const u32x4*)(qcol + row * a.n_in);
-                const uint32_t b = scol[row * a.groups];
-                sb[S][p] = ok ? b : 0u;
+                const uint32_t t = src[k0 + p * (P::kWaveRows / 2)];
+                const uint32_t row = t == kNoRow ? 0u : t;
+                q[S][p] = *(const u32x4*)(qcol + (uint64_t)row * (uint32_t)a.n_in);
+                sb[S][p] = scol[(uint64_t)row * (uint32_t)a.groups];
             }
         };
-        auto write_packed = [&](auto S_, int h) __attribute__((always_inline)) {
+        // quarter i of a step's packed values
+        auto write_packed = [&](auto S_, int h, int i) __attribute__((always_inline)) {
             constexpr int S = decltype(S_)::value;
-            unsigned char* dst = lds + (h % kStages) * kStageB + kOpB + (8 * wq + (lane >> 4)) * 512;
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const Opened o = open_packed(q[S][p], __uint_as_float(sb[S][p] << 23));
-                *(u32x4*)(dst + p * 2048 + pchunk * 16) = o.lo;
-                *(u32x4*)(dst + p * 2048 + (pchunk ^ 1) * 16) = o.hi;
-            }
+            const int p = i >> 1;
+            const int k = krow + p * (P::kWaveRows / 2) + prow;
+            unsigned char* dst = stage_of(h) + kOpA + k * kPitch;
+            const float step = src[h * kBK + k] == kNoRow ? 0.0f : __uint_as_float(sb[S][p] << 23);
+            if (i & 1) *(u32x4*)(dst + (pchunk ^ 1) * 16) = open_packed(q[S][p][2], q[S][p][3], step);
+            else *(u32x4*)(dst + pchunk * 16) = open_packed(q[S][p][0], q[S][p][1], step);
         };
         using C0 = std::integral_constant<int, 0>;
         using C1 = std::integral_constant<int, 1>;
         // at most n steps' copies may still be in flight
         auto wait_steps = [&](int n) __attribute__((always_inline)) {
-            if (n >= 3) wait_vmcnt<3 * kCopies>();
-            else if (n == 2) wait_vmcnt<2 * kCopies>();
-            else if (n == 1) wait_vmcnt<kCopies>();
+            if (n >= 3) wait_vmcnt<3 * P::kCopies>();
+            else if (n == 2) wait_vmcnt<2 * P::kCopies>();
+            else if (n == 1) wait_vmcnt<P::kCopies>();
             else wait_vmcnt<0>();
         };
-        // dy's steps 0..3 are copied, the packed steps 0 and 1 written, 2 and 3 in flight
-        if (packs) {
+        // dy's first steps are copied, the packed steps 0 and 1 written, 2 and 3 in flight
+        if (PACKS) {
             load_packed(C0{}, 0);
-            if (nh > 1) load_packed(C1{}, 1);
-            write_packed(C0{}, 0);
-            if (nh > 1) write_packed(C1{}, 1);
-            if (nh > 2) load_packed(C0{}, 2);
-            if (nh > 3) load_packed(C1{}, 3);
+            load_packed(C1{}, 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) write_packed(C0{}, 0, i);
+            if (nh > 1) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) write_packed(C1{}, 1, i);
+            }
+            load_packed(C0{}, 2);
+            load_packed(C1{}, 3);
         } else {
-            for (int h = 0; h < min(nh, kStages); ++h) copy_dy(h);
+            for (int h = 0; h < min(nh, kStages); ++h) {
+#pragma unroll
+                for (int i = 0; i < P::kCopies; ++i) copy_dy(h, i);
+            }
             wait_steps(min(nh, kStages) - 1);
         }
         barrier();
 
         bf16x8 fa[2][MI], fb[2][NJ];
-        auto tr_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
+        auto tr_frag = [&](const unsigned char* p, int pitch) __attribute__((always_inline)) {
             const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
-            const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * 512));
+            const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * pitch));
             return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
         };
-        // MFMAs on fragment set S, and among them the reads of sub-step ks of a stage into
-        // the other set
-        auto phase = [&](auto S_, int stage, int ks) __attribute__((always_inline)) {
+        // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the
+        // other set, and part(0..3)
+        auto phase = [&](auto S_, int stage, int ks, auto part) __attribute__((always_inline)) {
             constexpr int S = decltype(S_)::value;
-            const unsigned char* base = lds + stage * kStageB + ks * (16 * 512);
+            const unsigned char* base = lds + stage * kStageB;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 __builtin_amdgcn_sched_barrier(0);
@@ -332,39 +366,47 @@ wgrad_mfma_kernel(WgradArgs a) {
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
                 if (j == 0) {
-                    fa[S ^ 1][0] = tr_frag(base + a_pos[0]);
-                    fa[S ^ 1][1] = tr_frag(base + a_pos[1]);
+                    fa[S ^ 1][0] = tr_frag(base + ks * (16 * 512) + a_pos[0], 512);
+                    fa[S ^ 1][1] = tr_frag(base + ks * (16 * 512) + a_pos[1], 512);
                 } else if (j < 3) {
-                    fb[S ^ 1][2 * j - 2] = tr_frag(base + b_pos[2 * j - 2]);
-                    fb[S ^ 1][2 * j - 1] = tr_frag(base + b_pos[2 * j - 1]);
+                    fb[S ^ 1][2 * j - 2] = tr_frag(base + ks * (16 * kPitch) + b_pos[2 * j - 2], kPitch);
+                    fb[S ^ 1][2 * j - 1] = tr_frag(base + ks * (16 * kPitch) + b_pos[2 * j - 1], kPitch);
                 }
+                part(j);
             }
         };
-        // Step h between its two sub-steps: every wavefront holds the step's last fragments, so
-        // its stage is free for dy's step h + 4; the packed step h + 2 goes into a stage that
-        // has been free since step h - 2, and h + 4 is fetched.
-        auto turn = [&](auto S_, int h) __attribute__((always_inline)) {
-            if (packs) {
-                barrier();
-                if (h + 2 < nh) write_packed(S_, h + 2);
-                if (h + 4 < nh) load_packed(S_, h + 4);
-            } else {
-                wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
-                barrier();
-                if (h + kStages < nh) copy_dy(h + kStages);
-            }
-        };
+        // Step h.  Behind the barrier between its sub-steps every wavefront holds the step's
+        // last fragments, so its stage takes dy's step h + kStages; the packed step h + 2 goes
+        // into a stage whose last reader was a step earlier at least, and h + 4 is fetched.
+        // (Past the last step the reads fetch an old stage; unused.)
+        auto nothing = [](int) __attribute__((always_inline)) {};
         auto step = [&](auto S_, int h) __attribute__((always_inline)) {
-            if (active) phase(C0{}, h % kStages, 1);
-            turn(S_, h);
-            // (past the last step the reads fetch an old stage; unused)
-            if (active) phase(C1{}, (h + 1) % kStages, 0);
+            if (active) phase(C0{}, h % kStages, 1, nothing);
+            if (!PACKS) wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
+            barrier();
+            const bool more = h + (PACKS ? 2 : kStages) < nh;
+            auto part = [&](int j) __attribute__((always_inline)) {
+                if (PACKS) {
+                    if (more) write_packed(S_, h + 2, j);
+                    if (j == 3) load_packed(S_, h + 4);
+                } else if (more) {
+#pragma unroll
+                    for (int i = 0; i < P::kCopies / 4; ++i)
+                        copy_dy(h + kStages, j * (P::kCopies / 4) + i);
+                }
+            };
+            if (active) {
+                phase(C1{}, (h + 1) % kStages, 0, part);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) part(j);
+            }
         };
         if (active) {
 #pragma unroll
-            for (int i = 0; i < MI; ++i) fa[0][i] = tr_frag(lds + a_pos[i]);
+            for (int i = 0; i < MI; ++i) fa[0][i] = tr_frag(lds + a_pos[i], 512);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
+            for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j], kPitch);
         }
         int h = 0;
         for (; h + 1 < nh; h += 2) {
@@ -382,6 +424,7 @@ wgrad_mfma_kernel(WgradArgs a) {
     if (!active) return;
     float* const out = a.S > 1 ? a.part + (int64_t)slice * a.N * a.n_out * a.n_in : a.dW;
     constexpr int RB = WN * 4, NCH = RB / 16;
+    static_assert(NW * 32 * RB <= kStages * kStageB, "staged rows");
     unsigned char* sw = lds + wave * (32 * RB);
     const int rows_left = a.n_out - rt * BM - wr * WM;
     const int cols_left = a.n_in - ct * BN - wc * WN;
@@ -414,6 +457,17 @@ wgrad_mfma_kernel(WgradArgs a) {
         __builtin_amdgcn_s_waitcnt(0xc07f);
         __builtin_amdgcn_wave_barrier();
     }
+}
+
+template <int NW>
+__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+wgrad_mfma_kernel(WgradArgs a) {
+    using P = Shape<NW>;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[P::kStages * P::kStageB];
+    __shared__ __attribute__((aligned(16))) uint32_t src[P::kRows];
+    __shared__ int s_bad[NW];
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW / 2) wgrad_tile<NW, true>(a, lds, src, s_bad);
+    else wgrad_tile<NW, false>(a, lds, src, s_bad);
 }
 
 // dW = the slices' partial sums in slice order, four elements per thread
@@ -452,13 +506,18 @@ bool mfma_ok(const pr2_wgrad_desc& d) {
     return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % 16 == 0;
 }
 
+#ifndef WG_NW
+#define WG_NW 4
+#endif
+constexpr int kWaves = WG_NW;
 int64_t mfma_tiles(const pr2_wgrad_desc& d) {
+    constexpr int BN = Shape<kWaves>::BN;
     return (int64_t)((d.n_out + BM - 1) / BM) * ((d.n_in + BN - 1) / BN);
 }
 
 // Slices of the rows: with fewer tiles than CUs, as many as fill them once, each of at least
 // 256 rows (which pay for a tile's start, its stores and the join).
-constexpr int kCus = 256;
+constexpr int kCus = kWaves == 8 ? 256 : 512;
 int mfma_slices(const pr2_wgrad_desc& d) {
     const int64_t tiles = mfma_tiles(d) * d.N;
     const int64_t rows = d.R / d.N / 256;
@@ -501,7 +560,7 @@ hipError_t launch_mfma(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, h
     }
     {
         LaunchScope scope("wgrad_mfma", st);
-        hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
+        hipLaunchKernelGGL(wgrad_mfma_kernel<kWaves>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
@@ -557,7 +616,7 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
     WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
                 d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1};
     hipError_t e;
-    if (d.R > 0 && mfma_ok(d)) {
+    if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
         e = launch_mfma(d, a, wgrad_ws(d, ws), st);
     } else {
         const int64_t tiles = (int64_t)((d.n_out + kTile - 1) / kTile) * ((d.n_in + kTile - 1) / kTile);
