@@ -291,11 +291,11 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
             }
         };
         // Packed pieces in flight: two steps' worth.  Nothing is computed from them on arrival
-        // (a row that is none reads row 0 and becomes zeros when it is opened) and a step past
+        // (a row that is none reads row 0, and its scale is masked when it is opened) and a step past
         // the end reads the last one again, so that the wait for a piece leaves the later ones
         // in flight.
         u32x4 q[2][2];
-        uint32_t sb[2][2];
+        uint32_t sb[2][2], mask[2][2];
         auto load_packed = [&](auto S_, int h) __attribute__((always_inline)) {
             constexpr int S = decltype(S_)::value;
             const int k0 = min(h, nh - 1) * kBK + krow + prow;
@@ -303,6 +303,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
             for (int p = 0; p < 2; ++p) {
                 const uint32_t t = src[k0 + p * (P::kWaveRows / 2)];
                 const uint32_t row = t == kNoRow ? 0u : t;
+                mask[S][p] = t == kNoRow ? 0u : 255u << 23;
                 q[S][p] = *(const u32x4*)(qcol + (uint64_t)row * (uint32_t)a.n_in);
                 sb[S][p] = scol[(uint64_t)row * (uint32_t)a.groups];
             }
@@ -313,7 +314,7 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
             const int p = i >> 1;
             const int k = krow + p * (P::kWaveRows / 2) + prow;
             unsigned char* dst = stage_of(h) + kOpA + k * kPitch;
-            const float step = src[h * kBK + k] == kNoRow ? 0.0f : __uint_as_float(sb[S][p] << 23);
+            const float step = __uint_as_float((sb[S][p] << 23) & mask[S][p]);
             if (i & 1) *(u32x4*)(dst + (pchunk ^ 1) * 16) = open_packed(q[S][p][2], q[S][p][3], step);
             else *(u32x4*)(dst + pchunk * 16) = open_packed(q[S][p][0], q[S][p][1], step);
         };
@@ -507,7 +508,7 @@ bool mfma_ok(const pr2_wgrad_desc& d) {
 }
 
 #ifndef WG_NW
-#define WG_NW 4
+#define WG_NW 8
 #endif
 constexpr int kWaves = WG_NW;
 int64_t mfma_tiles(const pr2_wgrad_desc& d) {
