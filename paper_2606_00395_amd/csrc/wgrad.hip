@@ -25,6 +25,7 @@ struct WgradArgs {
     const int* order;           // [N] experts by decreasing row count; null with one weight
     float* part;                // [S, N, n_out, n_in] partial sums of S > 1 slices of the rows
     int S;
+    int G;                      // column tiles per workgroup
 };
 
 // rows of expert e, clamped to the R that there are
@@ -101,19 +102,27 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         }
 }
 
-// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x BN outputs per workgroup, NW
+// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs at a time, eight
 // wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through a
-// ring of LDS stages.  Both operands lie along K rows (the tile's columns as bf16) and are
-// read as fragments by the transposing LDS read.  dy is copied into LDS directly by half of
-// the wavefronts; the other half loads the packed rows (half of dy's bytes), turns them into
-// bf16 in registers, among its MFMAs, and writes them.
+// ring of four LDS stages.  Both operands lie along K rows of 512 bytes (the tile's columns
+// as bf16) and are read as fragments by the transposing LDS read.  dy is copied into LDS
+// directly by four of the wavefronts; the other four load the packed rows (half of dy's
+// bytes), turn them into bf16 in registers, among their MFMAs, and write them.
 // Row indexes go to LDS a few thousand at a time; a row past the last one or without a source
 // is zeros in both operands, since a zero of one would turn an infinity of the other into NaN.
-constexpr int BM = 256;
+// A workgroup goes through several tiles of the same rows of dy: the row indexes stay, and
+// the next tile's first steps are fetched before this one's outputs are stored.
+constexpr int BM = 256, BN = 256;
 constexpr int kBK = 32;
 constexpr int WM = 64, WN = 128;
 constexpr int MI = WM / 32, NJ = WN / 32;
-constexpr int kOpA = kBK * 512;
+constexpr int kMfmaThreads = 512;
+constexpr int kPitch = 512;                 // bytes of a K row
+constexpr int kOpB = kBK * kPitch;
+constexpr int kStageB = 2 * kOpB;
+constexpr int kStages = 4;
+constexpr int kCopies = 4;                  // per dy wavefront and step
+constexpr int kRowsHeld = 8128;             // row indexes held in LDS
 constexpr int kNumXcd = 8;
 constexpr uint32_t kNoRow = 0xffffffffu;
 
@@ -146,31 +155,18 @@ __device__ __forceinline__ u32x4 open_packed(uint32_t q0, uint32_t q1, float ste
     return r;
 }
 
-template <int NW>
-struct Shape {
-    static constexpr int BN = 32 * NW;
-    static constexpr int kThreads = 64 * NW;
-    static constexpr int kStages = NW == 8 ? 4 : 3;
-    static constexpr int kPitch = 2 * BN;                       // bytes of a packed operand's K row
-    static constexpr int kStageB = kOpA + kBK * kPitch;
-    static constexpr int kRows = NW == 8 ? 8128 : 1984;         // row indexes held in LDS
-    static constexpr int kCopies = 32 / NW;                     // per dy wavefront and step
-    static constexpr int kWaveRows = 64 / NW;                   // K rows of a step per loading wavefront
-};
-
-// One tile, for the wavefronts that load packed rows (PACKS) or dy: two instances, so that what
-// the one kind keeps in flight is no merge of both kinds' registers.
-template <int NW, bool PACKS>
-__device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* lds, uint32_t* src, int* s_bad) {
-    using P = Shape<NW>;
-    constexpr int BN = P::BN, kStages = P::kStages, kStageB = P::kStageB, kPitch = P::kPitch;
-
-    // Work items (expert, slice, tile); experts are dealt to the XCDs round-robin in
-    // decreasing row count and an expert's tiles run on one XCD, whose L2 then holds its rows.
-    // One weight's tiles are dealt to the XCDs in contiguous ranges.
+// The tiles of one work item, for the wavefronts that load packed rows (PACKS) or dy: two
+// instances, so that what the one kind keeps in flight is no merge of both kinds' registers.
+template <bool PACKS>
+__device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* lds, uint32_t* src,
+                                            int* s_bad) {
+    // Work items (expert, slice, row tile, group of column tiles); experts are dealt to the
+    // XCDs round-robin in decreasing row count and an expert's items run on one XCD, whose L2
+    // then holds its rows.  One weight's items are dealt to the XCDs in contiguous ranges.
     const int nct = (a.n_in + BN - 1) / BN;
+    const int ngr = (nct + a.G - 1) / a.G;
     const int nrt = (a.n_out + BM - 1) / BM;
-    const int per_e = nrt * nct * a.S;
+    const int per_e = nrt * ngr * a.S;
     int expert = 0, item;
     if (a.order) {
         const int xcd = blockIdx.x % kNumXcd;
@@ -184,9 +180,10 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
         item = (blockIdx.x % kNumXcd) * each + blockIdx.x / kNumXcd;
         if (item >= per_e) return;
     }
-    const int slice = item / (nrt * nct);
-    const int rt = item % (nrt * nct) / nct;
-    const int ct = item % nct;
+    const int slice = item / (nrt * ngr);
+    const int rt = item % (nrt * ngr) / ngr;
+    const int ct0 = item % ngr * a.G;
+    const int ct1 = min(nct, ct0 + a.G);
     int row0, last;
     expert_rows(a, expert, &row0, &last);
     if (a.S > 1) {
@@ -200,12 +197,8 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wr = NW == 8 ? wave >> 1 : wave;  // 64-row block of the tile
-    const int wc = NW == 8 ? wave & 1 : 0;      // 128-column block
-    const int wq = wave % (NW / 2);
-    const int krow = P::kWaveRows * wq;         // its first K row of a step
-    // blocks past the matrix: their wavefronts only load
-    const bool active = rt * BM + wr * WM < a.n_out && ct * BN + wc * WN < a.n_in;
+    const int wr = wave >> 1, wc = wave & 1;    // 64-row and 128-column block of the tile
+    const int krow = 8 * (wave & 3);            // first K row of a step that it loads
 
     // dy: copy i moves K rows krow + 2 i (lanes 0-31) and + 1 (lanes 32-63); chunk c of K row
     // kr is stored at c ^ 4 (kr & 3).  (Columns past the matrix read its first: they reach
@@ -218,37 +211,22 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
         doff[i] = 2u * (uint32_t)(hi * a.n_out + (rt * BM + c < a.n_out ? c : 0));
     }
     const bf16_t* const dy = (const bf16_t*)a.dy + (int64_t)(row0 + krow) * a.n_out + rt * BM;
-    // packed rows: piece p of a lane is 16 columns of K row krow + p kWaveRows / 2 + lane / kPer,
-    // stored as chunks pchunk and pchunk ^ 1
-    constexpr int kPer = BN / 16;               // lanes per row
-    const int prow = lane / kPer;
-    const int pcol = ct * BN + 16 * (lane % kPer);
-    const bool pin = pcol < a.n_in;
-    const int8_t* const qcol = a.q + (pin ? pcol : 0);
-    const uint8_t* const scol = a.scale + (pin ? pcol / 32 : 0);
-    const int pchunk = (2 * (lane % kPer)) ^ (4 * (prow & 3));
-
-    f32x16 acc[MI][NJ];
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    // packed rows: piece p of a lane is 16 columns of K row krow + 4 p + lane / 16, stored as
+    // chunks pchunk and pchunk ^ 1
+    const int prow = lane >> 4;
+    const int pchunk = (2 * (lane & 15)) ^ (4 * prow);
 
     // MFMA fragments by two transposing reads each
     const int s16 = lane & 15, g4 = lane >> 4;
     const int nl = 16 * (g4 & 1) + 4 * (s16 & 3);
     const int kl = 8 * (g4 >> 1) + (s16 >> 2);
     const int tsw = (nl >> 3) ^ (4 * (kl & 3));
-    auto tr_pos = [&](int cb, int pitch) {
-        return kl * pitch + ((((cb >> 3) ^ tsw)) << 4) + ((nl & 4) << 1);
-    };
+    auto tr_pos = [&](int cb) { return kl * kPitch + ((((cb >> 3) ^ tsw)) << 4) + ((nl & 4) << 1); };
     int a_pos[MI], b_pos[NJ];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) a_pos[i] = tr_pos(wr * WM + i * 32, 512);
+    for (int i = 0; i < MI; ++i) a_pos[i] = tr_pos(wr * WM + i * 32);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) b_pos[j] = kOpA + tr_pos(wc * WN + j * 32, kPitch);
+    for (int j = 0; j < NJ; ++j) b_pos[j] = kOpB + tr_pos(wc * WN + j * 32);
 
     auto barrier = [&]() __attribute__((always_inline)) {
         // a plain barrier: __syncthreads() would wait for every load in flight
@@ -259,13 +237,16 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("" ::: "memory");
     };
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
 
-    for (int kc = 0; kc < klen; kc += P::kRows) {
-        const int clen = min(P::kRows, klen - kc);
-        const int nh = (clen + kBK - 1) / kBK;
-        if (kc > 0) barrier();       // the last chunk's readers of src and of the stages are done
+    int kc = 0, nh = 0, whole = 0;      // the rows whose indexes are in LDS: first, steps, whole steps
+    auto hold_rows = [&](int first) __attribute__((always_inline)) {
+        kc = first;
+        const int clen = min(kRowsHeld, klen - kc);
+        nh = (clen + kBK - 1) / kBK;
         bool none = false;
-        for (int i = tid; i < nh * kBK; i += P::kThreads) {
+        for (int i = tid; i < nh * kBK; i += kMfmaThreads) {
             const uint32_t r = i < clen ? (uint32_t)source_row(a, row0 + kc + i) : kNoRow;
             none |= i < clen && r == kNoRow;
             src[i] = r;
@@ -275,200 +256,239 @@ __device__ __forceinline__ void wgrad_tile(const WgradArgs& a, unsigned char* ld
         barrier();
         int any = 0;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) any |= s_bad[w];
+        for (int w = 0; w < kMfmaThreads / 64; ++w) any |= s_bad[w];
         // steps before this one have a source for every row
-        const int whole = __builtin_amdgcn_readfirstlane(any) ? 0 : clen / kBK;
-
-        auto stage_of = [&](int h) __attribute__((always_inline)) { return lds + (h % kStages) * kStageB; };
-        auto copy_dy = [&](int h, int i) __attribute__((always_inline)) {
-            unsigned char* dst = stage_of(h) + krow * 512 + i * 1024;
-            const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
-            if (h < whole) {
-                dma16_at(p, doff[i & 1], dst);
-            } else {
-                const bool ok = src[h * kBK + krow + 2 * i + hi] != kNoRow;
-                dma16(ok ? (const unsigned char*)p + doff[i & 1] : (const unsigned char*)kZeros, dst);
-            }
-        };
-        // Packed pieces in flight: two steps' worth.  Nothing is computed from them on arrival
-        // (a row that is none reads row 0, and its scale is masked when it is opened) and a step past
-        // the end reads the last one again, so that the wait for a piece leaves the later ones
-        // in flight.
-        u32x4 q[2][2];
-        uint32_t sb[2][2], mask[2][2];
-        auto load_packed = [&](auto S_, int h) __attribute__((always_inline)) {
-            constexpr int S = decltype(S_)::value;
-            const int k0 = min(h, nh - 1) * kBK + krow + prow;
+        whole = __builtin_amdgcn_readfirstlane(any) ? 0 : clen / kBK;
+    };
+    auto stage_of = [&](int h) __attribute__((always_inline)) { return lds + (h % kStages) * kStageB; };
+    auto copy_dy = [&](int h, int i) __attribute__((always_inline)) {
+        unsigned char* dst = stage_of(h) + krow * kPitch + i * 1024;
+        const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
+        if (h < whole) {
+            dma16_at(p, doff[i & 1], dst);
+        } else {
+            const bool ok = src[h * kBK + krow + 2 * i + hi] != kNoRow;
+            dma16(ok ? (const unsigned char*)p + doff[i & 1] : (const unsigned char*)kZeros, dst);
+        }
+    };
+    // Packed pieces in flight: two steps' worth.  Nothing is computed from them on arrival
+    // (a row that is none reads row 0, and its scale is masked when it is opened) and a step past
+    // the end reads the last one again, so that the wait for a piece leaves the later ones
+    // in flight.
+    u32x4 q[2][2];
+    uint32_t sb[2][2], mask[2][2];
+    auto load_packed = [&](auto S_, int ct, int h) __attribute__((always_inline)) {
+        constexpr int S = decltype(S_)::value;
+        int c = ct * BN + 16 * (lane & 15);
+        c = c < a.n_in ? c : 0;             // (as dy's columns)
+        const int k0 = min(h, nh - 1) * kBK + krow + prow;
 #pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                const uint32_t t = src[k0 + p * (P::kWaveRows / 2)];
-                const uint32_t row = t == kNoRow ? 0u : t;
-                mask[S][p] = t == kNoRow ? 0u : 255u << 23;
-                q[S][p] = *(const u32x4*)(qcol + (uint64_t)row * (uint32_t)a.n_in);
-                sb[S][p] = scol[(uint64_t)row * (uint32_t)a.groups];
-            }
-        };
-        // quarter i of a step's packed values
-        auto write_packed = [&](auto S_, int h, int i) __attribute__((always_inline)) {
-            constexpr int S = decltype(S_)::value;
-            const int p = i >> 1;
-            const int k = krow + p * (P::kWaveRows / 2) + prow;
-            unsigned char* dst = stage_of(h) + kOpA + k * kPitch;
-            const float step = __uint_as_float((sb[S][p] << 23) & mask[S][p]);
-            if (i & 1) *(u32x4*)(dst + (pchunk ^ 1) * 16) = open_packed(q[S][p][2], q[S][p][3], step);
-            else *(u32x4*)(dst + pchunk * 16) = open_packed(q[S][p][0], q[S][p][1], step);
-        };
-        using C0 = std::integral_constant<int, 0>;
-        using C1 = std::integral_constant<int, 1>;
-        // at most n steps' copies may still be in flight
-        auto wait_steps = [&](int n) __attribute__((always_inline)) {
-            if (n >= 3) wait_vmcnt<3 * P::kCopies>();
-            else if (n == 2) wait_vmcnt<2 * P::kCopies>();
-            else if (n == 1) wait_vmcnt<P::kCopies>();
-            else wait_vmcnt<0>();
-        };
-        // dy's first steps are copied, the packed steps 0 and 1 written, 2 and 3 in flight
+        for (int p = 0; p < 2; ++p) {
+            const uint32_t t = src[k0 + 4 * p];
+            const uint32_t row = t == kNoRow ? 0u : t;
+            mask[S][p] = t == kNoRow ? 0u : 255u << 23;
+            q[S][p] = *(const u32x4*)(a.q + (uint64_t)row * (uint32_t)a.n_in + c);
+            sb[S][p] = a.scale[(uint64_t)row * (uint32_t)a.groups + c / 32];
+        }
+    };
+    // quarter i of a step's packed values
+    auto write_packed = [&](auto S_, int h, int i) __attribute__((always_inline)) {
+        constexpr int S = decltype(S_)::value;
+        const int p = i >> 1;
+        unsigned char* dst = stage_of(h) + kOpB + (krow + 4 * p + prow) * kPitch;
+        const float step = __uint_as_float((sb[S][p] << 23) & mask[S][p]);
+        if (i & 1) *(u32x4*)(dst + (pchunk ^ 1) * 16) = open_packed(q[S][p][2], q[S][p][3], step);
+        else *(u32x4*)(dst + pchunk * 16) = open_packed(q[S][p][0], q[S][p][1], step);
+    };
+    // at most n steps' copies may still be in flight
+    auto wait_steps = [&](int n) __attribute__((always_inline)) {
+        if (n >= 3) wait_vmcnt<3 * kCopies>();
+        else if (n == 2) wait_vmcnt<2 * kCopies>();
+        else if (n == 1) wait_vmcnt<kCopies>();
+        else wait_vmcnt<0>();
+    };
+    // The first steps, in two parts: into registers and stages 0 and 1, which the stores of
+    // the tile before leave alone, and the rest.  Then dy's steps 0..3 are copied, the
+    // packed steps 0 and 1 written, 2 and 3 in flight.
+    auto fetch = [&](int ct) __attribute__((always_inline)) {
         if (PACKS) {
-            load_packed(C0{}, 0);
-            load_packed(C1{}, 1);
+            load_packed(C0{}, ct, 0);
+            load_packed(C1{}, ct, 1);
+        } else {
+            for (int h = 0; h < min(nh, 2); ++h) {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i) copy_dy(h, i);
+            }
+        }
+    };
+    auto start = [&](int ct) __attribute__((always_inline)) {
+        if (PACKS) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) write_packed(C0{}, 0, i);
             if (nh > 1) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) write_packed(C1{}, 1, i);
             }
-            load_packed(C0{}, 2);
-            load_packed(C1{}, 3);
+            load_packed(C0{}, ct, 2);
+            load_packed(C1{}, ct, 3);
         } else {
-            for (int h = 0; h < min(nh, kStages); ++h) {
+            for (int h = 2; h < min(nh, kStages); ++h) {
 #pragma unroll
-                for (int i = 0; i < P::kCopies; ++i) copy_dy(h, i);
+                for (int i = 0; i < kCopies; ++i) copy_dy(h, i);
             }
             wait_steps(min(nh, kStages) - 1);
         }
         barrier();
+    };
 
-        bf16x8 fa[2][MI], fb[2][NJ];
-        auto tr_frag = [&](const unsigned char* p, int pitch) __attribute__((always_inline)) {
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
-            const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * pitch));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the
-        // other set, and part(0..3)
-        auto phase = [&](auto S_, int stage, int ks, auto part) __attribute__((always_inline)) {
-            constexpr int S = decltype(S_)::value;
-            const unsigned char* base = lds + stage * kStageB;
+    if (klen > 0) {
+        hold_rows(0);
+        fetch(ct0);
+    }
+    for (int ct = ct0; ct < ct1; ++ct) {
+        // blocks past the matrix: their wavefronts only load
+        const bool active = rt * BM + wr * WM < a.n_out && ct * BN + wc * WN < a.n_in;
+        f32x16 acc[MI][NJ];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
-                __builtin_amdgcn_sched_barrier(0);
-                if (j == 0) {
-                    fa[S ^ 1][0] = tr_frag(base + ks * (16 * 512) + a_pos[0], 512);
-                    fa[S ^ 1][1] = tr_frag(base + ks * (16 * 512) + a_pos[1], 512);
-                } else if (j < 3) {
-                    fb[S ^ 1][2 * j - 2] = tr_frag(base + ks * (16 * kPitch) + b_pos[2 * j - 2], kPitch);
-                    fb[S ^ 1][2 * j - 1] = tr_frag(base + ks * (16 * kPitch) + b_pos[2 * j - 1], kPitch);
-                }
-                part(j);
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+
+        for (int k = 0; k < klen; k += kRowsHeld) {
+            if (klen > kRowsHeld && (k > 0 || ct > ct0)) {
+                barrier();           // the last readers of src and of the stages are done
+                hold_rows(k);
+                fetch(ct);
             }
-        };
-        // Step h.  Behind the barrier between its sub-steps every wavefront holds the step's
-        // last fragments, so its stage takes dy's step h + kStages; the packed step h + 2 goes
-        // into a stage whose last reader was a step earlier at least, and h + 4 is fetched.
-        // (Past the last step the reads fetch an old stage; unused.)
-        auto nothing = [](int) __attribute__((always_inline)) {};
-        auto step = [&](auto S_, int h) __attribute__((always_inline)) {
-            if (active) phase(C0{}, h % kStages, 1, nothing);
-            if (!PACKS) wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
-            barrier();
-            const bool more = h + (PACKS ? 2 : kStages) < nh;
-            auto part = [&](int j) __attribute__((always_inline)) {
-                if (PACKS) {
-                    if (more) write_packed(S_, h + 2, j);
-                    if (j == 3) load_packed(S_, h + 4);
-                } else if (more) {
+            start(ct);
+
+            bf16x8 fa[2][MI], fb[2][NJ];
+            auto tr_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
+                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
+                const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * kPitch));
+                return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the
+            // other set, and part(0..3)
+            auto phase = [&](auto S_, int stage, int ks, auto part) __attribute__((always_inline)) {
+                constexpr int S = decltype(S_)::value;
+                const unsigned char* base = lds + stage * kStageB + ks * (16 * kPitch);
 #pragma unroll
-                    for (int i = 0; i < P::kCopies / 4; ++i)
-                        copy_dy(h + kStages, j * (P::kCopies / 4) + i);
+                for (int j = 0; j < NJ; ++j) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (j == 0) {
+                        fa[S ^ 1][0] = tr_frag(base + a_pos[0]);
+                        fa[S ^ 1][1] = tr_frag(base + a_pos[1]);
+                    } else if (j < 3) {
+                        fb[S ^ 1][2 * j - 2] = tr_frag(base + b_pos[2 * j - 2]);
+                        fb[S ^ 1][2 * j - 1] = tr_frag(base + b_pos[2 * j - 1]);
+                    }
+                    part(j);
+                }
+            };
+            // Step h.  Behind the barrier between its sub-steps every wavefront holds the step's
+            // last fragments, so its stage takes dy's step h + kStages; the packed step h + 2 goes
+            // into a stage whose last reader was a step earlier at least, and h + 4 is fetched.
+            // (Past the last step the reads fetch an old stage; unused.)
+            auto step = [&](auto S_, int h) __attribute__((always_inline)) {
+                if (active) phase(C0{}, h % kStages, 1, [](int) __attribute__((always_inline)) {});
+                if (!PACKS) wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
+                barrier();
+                const bool more = h + (PACKS ? 2 : kStages) < nh;
+                auto part = [&](int j) __attribute__((always_inline)) {
+                    if (PACKS) {
+                        if (more) write_packed(S_, h + 2, j);
+                        if (j == 3) load_packed(S_, ct, h + 4);
+                    } else if (more) {
+                        copy_dy(h + kStages, j);
+                    }
+                };
+                if (active) {
+                    phase(C1{}, (h + 1) % kStages, 0, part);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) part(j);
                 }
             };
             if (active) {
-                phase(C1{}, (h + 1) % kStages, 0, part);
-            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) part(j);
+                for (int i = 0; i < MI; ++i) fa[0][i] = tr_frag(lds + a_pos[i]);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
             }
-        };
+            int h = 0;
+            for (; h + 1 < nh; h += 2) {
+                step(C0{}, h);
+                step(C1{}, h + 1);
+            }
+            if (h < nh) step(C0{}, h);
+        }
+        // (no wavefront reads a stage any more: all hold the last step's fragments)
+        barrier();
+        if (ct + 1 < ct1 && klen > 0 && klen <= kRowsHeld) fetch(ct + 1);
+
+        // Lane l holds output row l % 32 of each 32-row block and columns 8 (v / 4) + 4 (l / 32)
+        // + v % 4 of each 32-column block.  The rows are staged through this wavefront's share of
+        // stages 2 and 3, 32 rows of 64 columns at a time, and stored 16 bytes per lane along
+        // whole row segments, non-temporally: gradients are not read again here.
         if (active) {
+            float* const out = (a.S > 1 ? a.part : a.dW) + ct * BN + wc * WN +
+                ((int64_t)(slice * a.N + expert) * a.n_out + rt * BM + wr * WM) * a.n_in;
+            constexpr int RB = 64 * 4, NCH = RB / 16;
+            static_assert(kMfmaThreads / 64 * 32 * RB <= 2 * kStageB, "staged rows");
+            unsigned char* sw = lds + 2 * kStageB + wave * (32 * RB);
+            const int rows_left = a.n_out - rt * BM - wr * WM;
+            const int cols_left = a.n_in - ct * BN - wc * WN;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) fa[0][i] = tr_frag(lds + a_pos[i], 512);
+            for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j], kPitch);
+                for (int jh = 0; jh < NJ / 2; ++jh) {
+                    const int row = lane & 31;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int a4 = 0; a4 < 4; ++a4) {
+                            const int chunk = j * 8 + 2 * a4 + hi;
+                            const f32x16& v = acc[i][2 * jh + j];
+                            *(f32x4*)(sw + row * RB + ((chunk ^ (row & (NCH - 1))) << 4)) =
+                                f32x4{v[4 * a4], v[4 * a4 + 1], v[4 * a4 + 2], v[4 * a4 + 3]};
+                        }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    __builtin_amdgcn_wave_barrier();
+                    int row2 = lane / NCH;
+                    const int ch = lane % NCH;
+                    float* to = out + (int64_t)(i * 32 + row2) * a.n_in + jh * 64 + ch * 4;
+                    const int rows = jh * 64 + ch * 4 < cols_left ? min(32, rows_left - i * 32) : 0;
+#pragma unroll
+                    for (int p = 0; p < 32 / (64 / NCH); ++p) {
+                        if (row2 < rows)
+                            __builtin_nontemporal_store(
+                                *(const u32x4*)(sw + row2 * RB + ((ch ^ (row2 & (NCH - 1))) << 4)), (u32x4*)to);
+                        row2 += 64 / NCH;
+                        to += (int64_t)(64 / NCH) * a.n_in;
+                    }
+                    // the next block overwrites the region
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    __builtin_amdgcn_wave_barrier();
+                }
         }
-        int h = 0;
-        for (; h + 1 < nh; h += 2) {
-            step(C0{}, h);
-            step(C1{}, h + 1);
-        }
-        if (h < nh) step(C0{}, h);
-    }
-    // Lane l holds output row l % 32 of each 32-row block and columns 8 (v / 4) + 4 (l / 32) +
-    // v % 4 of each 32-column block.  The rows are staged through this wavefront's share of
-    // the freed stages, one 32-row block at a time, and stored 16 bytes per lane along whole
-    // row segments, non-temporally: gradients are not read again here.
-    const int ncol0 = 4 * (lane >> 5);
-    __syncthreads();
-    if (!active) return;
-    float* const out = a.S > 1 ? a.part + (int64_t)slice * a.N * a.n_out * a.n_in : a.dW;
-    constexpr int RB = WN * 4, NCH = RB / 16;
-    static_assert(NW * 32 * RB <= kStages * kStageB, "staged rows");
-    unsigned char* sw = lds + wave * (32 * RB);
-    const int rows_left = a.n_out - rt * BM - wr * WM;
-    const int cols_left = a.n_in - ct * BN - wc * WN;
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int row = lane & 31;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-            for (int a4 = 0; a4 < 4; ++a4) {
-                const int col = j * 32 + 8 * a4 + ncol0;
-                const int v0 = 4 * a4;
-                *(f32x4*)(sw + row * RB + (((col >> 2) ^ (row & (NCH - 1))) << 4)) =
-                    f32x4{acc[i][j][v0], acc[i][j][v0 + 1], acc[i][j][v0 + 2], acc[i][j][v0 + 3]};
-            }
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        __builtin_amdgcn_wave_barrier();
-        const int ch = lane % NCH;
-#pragma unroll
-        for (int p = 0; p < 32 / (64 / NCH); ++p) {
-            const int row2 = p * (64 / NCH) + lane / NCH;
-            const int o = i * 32 + row2;
-            if (o < rows_left && ch * 4 < cols_left) {
-                float* orow = out + ((int64_t)expert * a.n_out + rt * BM + wr * WM + o) * a.n_in;
-                __builtin_nontemporal_store(*(const u32x4*)(sw + row2 * RB + ((ch ^ (row2 & (NCH - 1))) << 4)),
-                                            (u32x4*)(orow + ct * BN + wc * WN + ch * 4));
-            }
-        }
-        // the next block overwrites the region
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        __builtin_amdgcn_wave_barrier();
+        barrier();                  // stages 2 and 3 are free again
     }
 }
 
-template <int NW>
-__global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ void __launch_bounds__(kMfmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 wgrad_mfma_kernel(WgradArgs a) {
-    using P = Shape<NW>;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[P::kStages * P::kStageB];
-    __shared__ __attribute__((aligned(16))) uint32_t src[P::kRows];
-    __shared__ int s_bad[NW];
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= NW / 2) wgrad_tile<NW, true>(a, lds, src, s_bad);
-    else wgrad_tile<NW, false>(a, lds, src, s_bad);
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStageB];
+    __shared__ __attribute__((aligned(16))) uint32_t src[kRowsHeld];
+    __shared__ int s_bad[kMfmaThreads / 64];
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= 4) wgrad_tiles<true>(a, lds, src, s_bad);
+    else wgrad_tiles<false>(a, lds, src, s_bad);
 }
 
 // dW = the slices' partial sums in slice order, four elements per thread
@@ -507,24 +527,27 @@ bool mfma_ok(const pr2_wgrad_desc& d) {
     return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % 16 == 0;
 }
 
-#ifndef WG_NW
-#define WG_NW 8
-#endif
-constexpr int kWaves = WG_NW;
 int64_t mfma_tiles(const pr2_wgrad_desc& d) {
-    constexpr int BN = Shape<kWaves>::BN;
     return (int64_t)((d.n_out + BM - 1) / BM) * ((d.n_in + BN - 1) / BN);
 }
 
 // Slices of the rows: with fewer tiles than CUs, as many as fill them once, each of at least
 // 256 rows (which pay for a tile's start, its stores and the join).
-constexpr int kCus = kWaves == 8 ? 256 : 512;
+constexpr int kCus = 256;
 int mfma_slices(const pr2_wgrad_desc& d) {
     const int64_t tiles = mfma_tiles(d) * d.N;
     const int64_t rows = d.R / d.N / 256;
     int64_t s = kCus / tiles;
     if (s > rows) s = rows;
     return s < 1 ? 1 : (int)s;
+}
+
+#ifndef WG_G
+#define WG_G 2
+#endif
+int mfma_group(const pr2_wgrad_desc& d) {
+    int64_t g = mfma_tiles(d) * d.N / (4 * kCus);
+    return g < 1 ? 1 : g > WG_G ? WG_G : (int)g;
 }
 
 struct WgradWs {
@@ -546,22 +569,24 @@ WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
 }
 
 hipError_t launch_mfma(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
-    const int64_t tiles = mfma_tiles(d);
     a.S = mfma_slices(d);
+    a.G = mfma_group(d);
     a.part = w.part;
+    const int64_t nct = (d.n_in + BN - 1) / BN;
+    const int64_t items = (int64_t)((d.n_out + BM - 1) / BM) * ((nct + a.G - 1) / a.G) * a.S;
     int64_t grid;
     hipError_t e;
     if (d.N > 1) {
         e = launch_expert_order(a.offsets, d.N, w.order, st);
         if (e != hipSuccess) return e;
         a.order = w.order;
-        grid = tiles * a.S * ((d.N + kNumXcd - 1) / kNumXcd) * kNumXcd;
+        grid = items * ((d.N + kNumXcd - 1) / kNumXcd) * kNumXcd;
     } else {
-        grid = (tiles * a.S + kNumXcd - 1) / kNumXcd * kNumXcd;
+        grid = (items + kNumXcd - 1) / kNumXcd * kNumXcd;
     }
     {
         LaunchScope scope("wgrad_mfma", st);
-        hipLaunchKernelGGL(wgrad_mfma_kernel<kWaves>, dim3((unsigned)grid), dim3(64 * kWaves), 0, st, a);
+        hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
@@ -615,7 +640,7 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
     drop_split_records(ws, ws_bytes);
     const hipStream_t st = (hipStream_t)stream;
     WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
-                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1};
+                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1};
     hipError_t e;
     if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
         e = launch_mfma(d, a, wgrad_ws(d, ws), st);
