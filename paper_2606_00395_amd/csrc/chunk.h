@@ -46,13 +46,24 @@ template <> struct Chunk<float> {
     }
 };
 
+// 16 bytes at any element's address; NT: not to be kept in the caches
+template <bool NT>
+__device__ __forceinline__ u32x4 load16(const void* p) {
+    return NT ? __builtin_nontemporal_load((const u32x4_any*)p) : *(const u32x4_any*)p;
+}
+template <bool NT>
+__device__ __forceinline__ void store16(void* p, const u32x4& w) {
+    if (NT) __builtin_nontemporal_store(w, (u32x4_any*)p);
+    else *(u32x4_any*)p = w;
+}
+
 // chunk c of a row of `full` whole chunks and `rem` more elements; past the end `pad`, two
 // bf16 or one fp32 value
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ u32x4 load_chunk(const T* row, int c, int full, int rem,
                                             uint32_t pad = 0) {
     constexpr int E = Chunk<T>::E;
-    if (c < full) return *(const u32x4_any*)(row + (int64_t)c * E);
+    if (c < full) return load16<NT>(row + (int64_t)c * E);
     u32x4 w = {pad, pad, pad, pad};
     if (c == full) {
 #pragma unroll
@@ -67,11 +78,11 @@ __device__ __forceinline__ u32x4 load_chunk(const T* row, int c, int full, int r
 }
 
 // the bits of a chunk as they are
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ void copy_chunk(T* row, int c, int full, int rem, const u32x4& w) {
     constexpr int E = Chunk<T>::E;
     if (c < full) {
-        *(u32x4_any*)(row + (int64_t)c * E) = w;
+        store16<NT>(row + (int64_t)c * E, w);
     } else if (c == full) {
 #pragma unroll
         for (int i = 0; i < E; ++i)
@@ -81,11 +92,11 @@ __device__ __forceinline__ void copy_chunk(T* row, int c, int full, int rem, con
     }
 }
 
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ void store_chunk(T* row, int c, int full, int rem, const float* v) {
     constexpr int E = Chunk<T>::E;
     if (c < full) {
-        *(u32x4_any*)(row + (int64_t)c * E) = Chunk<T>::close(v);
+        store16<NT>(row + (int64_t)c * E, Chunk<T>::close(v));
     } else if (c == full) {
 #pragma unroll
         for (int i = 0; i < E; ++i)

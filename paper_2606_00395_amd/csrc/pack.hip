@@ -44,13 +44,13 @@ __device__ __forceinline__ Unit unit_of(const Tiling& t, int i) {
 }
 
 // 16 elements at p, the first n of them inside the row (zeros for the others)
-template <typename T>
+template <typename T, bool NT = false>
 __device__ __forceinline__ void load_unit(const T* p, int n, float (&v)[kUnit]) {
     constexpr int E = Chunk<T>::E;
     if (n >= kUnit) {
         u32x4 w[kUnit / E];
 #pragma unroll
-        for (int i = 0; i < kUnit / E; ++i) w[i] = *(const u32x4_any*)(p + i * E);
+        for (int i = 0; i < kUnit / E; ++i) w[i] = load16<NT>(p + i * E);
 #pragma unroll
         for (int i = 0; i < kUnit / E; ++i) Chunk<T>::open(w[i], v + i * E);
     } else {
@@ -64,7 +64,7 @@ __device__ __forceinline__ void store_unit(T* p, int n, const float (&v)[kUnit])
     constexpr int E = Chunk<T>::E;
     if (n >= kUnit) {
 #pragma unroll
-        for (int i = 0; i < kUnit / E; ++i) *(u32x4_any*)(p + i * E) = Chunk<T>::close(v + i * E);
+        for (int i = 0; i < kUnit / E; ++i) store16<false>(p + i * E, Chunk<T>::close(v + i * E));
     } else {
 #pragma unroll
         for (int i = 0; i < kUnit; ++i)
@@ -145,7 +145,7 @@ act_pack_kernel(Tiling t, int C, int64_t groups, const T* x, int8_t* q, uint8_t*
         if (at.row >= t.R) continue;
         const int c = at.u * kUnit, n = C - c;
         float v[kUnit];
-        load_unit(x + at.row * C + c, n, v);
+        load_unit<T, true>(x + at.row * C + c, n, v);      // read once
         const uint32_t byte = group_scale(v);
         if (n > 0) store_q(q + at.row * C + c, n, quantise(v, byte));
         if ((at.u & 1) == 0) scale[at.row * groups + at.u / 2] = (uint8_t)byte;
