@@ -21,11 +21,10 @@ struct WgradArgs {
     int64_t R, Rx;
     int n_out, n_in, N, k;
     int groups;
-    // MFMA form
     const int* order;           // [N] experts by decreasing row count; null with one weight
     float* part;                // [S, N, n_out, n_in] partial sums of S > 1 slices of the rows
     int S;
-    int G;                      // column tiles per workgroup
+    int G;                      // 256 x 256 tiles: column tiles per workgroup
 };
 
 // rows of expert e, clamped to the R that there are
@@ -33,6 +32,13 @@ __device__ __forceinline__ void expert_rows(const WgradArgs& a, int e, int* firs
     const int R = (int)a.R;
     *first = a.offsets ? min(max(a.offsets[e], 0), R) : 0;
     *last = a.offsets ? max(min(a.offsets[e + 1], R), *first) : R;
+}
+
+// slice s of a.S of them, whole steps of 32
+__device__ __forceinline__ void slice_rows(const WgradArgs& a, int s, int* first, int* last) {
+    const int len = ((*last - *first + a.S - 1) / a.S + 31) / 32 * 32;
+    *first = (int)min((int64_t)*last, *first + (int64_t)s * len);
+    *last = (int)min((int64_t)*last, (int64_t)*first + len);
 }
 
 // packed row of dy's row r, -1 if it has none
@@ -43,63 +49,100 @@ __device__ __forceinline__ int source_row(const WgradArgs& a, int r) {
     return q >= 0 && t < a.Rx ? t : -1;
 }
 
-// Any type, width and row count: 64 x 64 outputs per workgroup, 4 x 4 per thread, 16 rows of
-// both operands staged in LDS as fp32.  Bound by its vector FMAs and LDS reads.
+// Any type, width and row count: 64 x 64 outputs per workgroup, four wavefronts of 32 x 32 on
+// v_mfma_f32_32x32x2_f32 (fp32 products and sums), 32 rows of both operands staged in LDS as
+// fp32 at a time, the next 32 fetched meanwhile.  Small layers are bound by the latency of
+// that chain (15 us at 1226 rows, 7 experts of 135 x 203; one FMA per lane at a time took 24),
+// large ones by the fp32 MFMA and the LDS (111 TFLOP/s at 4096 x 4096 over 32768 rows, where
+// the library's fp32 product reaches 154; with FMAs 74).
 constexpr int kTile = 64;
-constexpr int kStep = 16;
+constexpr int kStep = 32;
+constexpr int kTilePitch = kTile + 32;      // the two halves of a wavefront read other banks
+
+// 8 columns of a row, the first n of them inside the matrix
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
+    constexpr int E = Chunk<T>::E;
+    if (n >= 8) {
+        u32x4 w[8 / E];
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) w[i] = load16<false>(p + i * E);
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) Chunk<T>::open(w[i], v + i * E);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? Act<T>::to_f32(p[i]) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ void load8_packed(const int8_t* p, int n, float step, float (&v)[8]) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef u32x2 u32x2_byte __attribute__((aligned(1)));
+    if (n >= 8) {
+        const u32x2 w = *(const u32x2_byte*)p;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)((int)(w[i / 4] << (24 - 8 * (i % 4))) >> 24) * step;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] * step : 0.0f;
+    }
+}
 
 template <typename T>
 __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
-    __shared__ float A[kStep][kTile + 4], B[kStep][kTile + 4];
+    __shared__ __attribute__((aligned(16))) float A[kStep * kTilePitch], B[kStep * kTilePitch];
     const int tid = threadIdx.x;
+    const int lane = tid & 63, wave = tid >> 6;
     const int nct = (a.n_in + kTile - 1) / kTile;
     const int o0 = (int)(blockIdx.x / nct) * kTile, c0 = (int)(blockIdx.x % nct) * kTile;
     const int e = blockIdx.y;
     int first, last;
     expert_rows(a, e, &first, &last);
-    const int sr = tid / 16, sc = (tid % 16) * 4;       // row and columns this thread stages
-    const int tr = (tid / 16) * 4, tc = (tid % 16) * 4; // outputs it owns
-    float acc[4][4] = {};
-    for (int r0 = first; r0 < last; r0 += kStep) {
+    slice_rows(a, blockIdx.z, &first, &last);
+    const int sr = tid / 8, sc = (tid % 8) * 8;         // row and columns this thread stages
+    const int no = a.n_out - o0 - sc, nc = a.n_in - c0 - sc;
+    f32x16 acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
+    float va[8], vb[8];
+    auto fetch = [&](int r0) __attribute__((always_inline)) {
         const int r = r0 + sr;
-        const bool in = r < last;
-        const int x = in ? source_row(a, r) : -1;
-        const T* dy = (const T*)a.dy + (int64_t)(in ? r : 0) * a.n_out;
-        const int8_t* q = a.q + (int64_t)max(x, 0) * a.n_in;
-        const uint8_t* s = a.scale + (int64_t)max(x, 0) * a.groups;
-        float va[4], vb[4];
+        const int x = r < last ? source_row(a, r) : -1;
+        // a row without a source is zeros in both operands: nothing of it multiplies
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int o = o0 + sc + j, c = c0 + sc + j;
-            // a row without a source is zeros in both operands: nothing of it multiplies
-            va[j] = x >= 0 && o < a.n_out ? Act<T>::to_f32(dy[o]) : 0.0f;
-            vb[j] = x >= 0 && c < a.n_in ? (float)q[c] * __uint_as_float((uint32_t)s[c / 32] << 23) : 0.0f;
-        }
+        for (int i = 0; i < 8; ++i) va[i] = vb[i] = 0.0f;
+        if (x < 0) return;
+        if (no > 0) load8((const T*)a.dy + (int64_t)r * a.n_out + o0 + sc, no, va);
+        if (nc > 0)
+            load8_packed(a.q + (int64_t)x * a.n_in + c0 + sc, nc,
+                         __uint_as_float((uint32_t)a.scale[(int64_t)x * a.groups + (c0 + sc) / 32] << 23), vb);
+    };
+    const int ao = 32 * (wave >> 1) + (lane & 31), bo = 32 * (wave & 1) + (lane & 31), k2 = lane >> 5;
+    if (first < last) fetch(first);
+    for (int r0 = first; r0 < last; r0 += kStep) {
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            A[sr][sc + j] = va[j];
-            B[sr][sc + j] = vb[j];
+        for (int i = 0; i < 8; i += 4) {
+            *(f32x4*)(A + sr * kTilePitch + sc + i) = f32x4{va[i], va[i + 1], va[i + 2], va[i + 3]};
+            *(f32x4*)(B + sr * kTilePitch + sc + i) = f32x4{vb[i], vb[i + 1], vb[i + 2], vb[i + 3]};
         }
         __syncthreads();
+        if (r0 + kStep < last) fetch(r0 + kStep);
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) {
-            const float4 p = *(const float4*)&A[i][tr], w = *(const float4*)&B[i][tc];
-            const float pa[4] = {p.x, p.y, p.z, p.w}, wb[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(pa[u], wb[v], acc[u][v]);
-        }
+        for (int k = 0; k < kStep; k += 2)
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(B[(k + k2) * kTilePitch + bo], A[(k + k2) * kTilePitch + ao],
+                                                       acc, 0, 0, 0);
     }
+    // lane l holds output row l % 32 and columns 8 (v / 4) + 4 (l / 32) + v % 4
+    const int o = o0 + ao;
+    if (o >= a.n_out) return;
+    float* to = (a.S > 1 ? a.part : a.dW) +
+        (((int64_t)blockIdx.z * a.N + e) * a.n_out + o) * a.n_in;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            const int o = o0 + tr + u, c = c0 + tc + v;
-            if (o < a.n_out && c < a.n_in)
-                a.dW[((int64_t)e * a.n_out + o) * a.n_in + c] = acc[u][v];
-        }
+    for (int v = 0; v < 16; ++v) {
+        const int c = c0 + 32 * (wave & 1) + 8 * (v / 4) + 4 * k2 + v % 4;
+        if (c < a.n_in) to[c] = acc[v];
+    }
 }
 
 // bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs at a time, eight
@@ -186,11 +229,7 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
     const int ct1 = min(nct, ct0 + a.G);
     int row0, last;
     expert_rows(a, expert, &row0, &last);
-    if (a.S > 1) {
-        const int len = (((last - row0 + a.S - 1) / a.S) + kBK - 1) / kBK * kBK;
-        row0 = min(last, row0 + slice * len);
-        last = min(last, row0 + len);
-    }
+    slice_rows(a, slice, &row0, &last);
     row0 = __builtin_amdgcn_readfirstlane(row0);
     const int klen = __builtin_amdgcn_readfirstlane(last) - row0;
 
@@ -493,11 +532,19 @@ wgrad_mfma_kernel(WgradArgs a) {
 
 // dW = the slices' partial sums in slice order, four elements per thread
 __global__ void __launch_bounds__(256) wgrad_join_kernel(const float* part, int64_t n, int S, float* dW) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));        // a slice starts at any float
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    f32x4 v = *(const f32x4*)(part + i);
-    for (int s = 1; s < S; ++s) v += *(const f32x4*)(part + s * n + i);
-    *(f32x4*)(dW + i) = v;
+    if (i + 4 <= n) {
+        f32x4 v = *(const f32x4_any*)(part + i);
+        for (int s = 1; s < S; ++s) v += *(const f32x4_any*)(part + s * n + i);
+        *(f32x4*)(dW + i) = v;
+    } else {
+        for (int64_t j = i; j < n; ++j) {
+            float v = part[j];
+            for (int s = 1; s < S; ++s) v += part[s * n + j];
+            dW[j] = v;
+        }
+    }
 }
 
 // ------------------------------------------------------------------ host ----
@@ -518,8 +565,8 @@ pr2_status check_wgrad(const pr2_wgrad_desc* desc) {
                     (long long)d.R, (long long)d.Rx);
     if (d.n_out > (1 << 20) || d.n_in > (1 << 20))
         return fail(PR2_ERR_UNSUPPORTED, "n_out = %d or n_in = %d > 2^20", d.n_out, d.n_in);
-    if (((int64_t)(d.n_out + 63) / 64) * ((d.n_in + 63) / 64) * d.N > 0x7fffffff / 64)
-        return fail(PR2_ERR_UNSUPPORTED, "N n_out n_in is too large");
+    if ((int64_t)d.N * d.n_out * d.n_in > (int64_t)1 << 36)
+        return fail(PR2_ERR_UNSUPPORTED, "N n_out n_in > 2^36");
     return PR2_OK;
 }
 
@@ -527,27 +574,29 @@ bool mfma_ok(const pr2_wgrad_desc& d) {
     return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % 16 == 0;
 }
 
-int64_t mfma_tiles(const pr2_wgrad_desc& d) {
-    return (int64_t)((d.n_out + BM - 1) / BM) * ((d.n_in + BN - 1) / BN);
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Output tiles over all experts.
+int64_t wgrad_tile_count(const pr2_wgrad_desc& d, int tile) {
+    return ceil_div(d.n_out, tile) * ceil_div(d.n_in, tile) * d.N;
 }
 
-// Slices of the rows: with fewer tiles than CUs, as many as fill them once, each of at least
-// 256 rows (which pay for a tile's start, its stores and the join).
+// Slices of the rows: where the output tiles leave the chip idle, as many as fill it once (one
+// 256 x 256 tile per CU, or four of 64 x 64), each with enough rows to pay for a tile's start,
+// its stores and the join.
 constexpr int kCus = 256;
-int mfma_slices(const pr2_wgrad_desc& d) {
-    const int64_t tiles = mfma_tiles(d) * d.N;
-    const int64_t rows = d.R / d.N / 256;
-    int64_t s = kCus / tiles;
-    if (s > rows) s = rows;
+int wgrad_slices(const pr2_wgrad_desc& d) {
+    const bool big = mfma_ok(d);
+    const int64_t fill = big ? kCus : 4 * kCus;
+    int64_t s = fill / wgrad_tile_count(d, big ? BM : kTile);
+    const int64_t most = d.R / d.N / (big ? 256 : 128);
+    if (s > most) s = most;
     return s < 1 ? 1 : (int)s;
 }
 
-#ifndef WG_G
-#define WG_G 2
-#endif
-int mfma_group(const pr2_wgrad_desc& d) {
-    int64_t g = mfma_tiles(d) * d.N / (4 * kCus);
-    return g < 1 ? 1 : g > WG_G ? WG_G : (int)g;
+// Column tiles per workgroup: two where that leaves each CU eight workgroups.
+int wgrad_group(const pr2_wgrad_desc& d) {
+    return wgrad_tile_count(d, BM) >= 16 * kCus ? 2 : 1;
 }
 
 struct WgradWs {
@@ -558,42 +607,45 @@ struct WgradWs {
 
 WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
     WgradWs w{};
-    if (!mfma_ok(d)) return w;
     char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
     const size_t order = (sizeof(int) * (size_t)d.N + 255) & ~(size_t)255;
-    const int S = mfma_slices(d);
+    const int S = wgrad_slices(d);
     w.order = (int*)p;
     w.part = (float*)(p ? p + order : nullptr);
     w.bytes = order + (S > 1 ? sizeof(float) * (size_t)S * d.N * d.n_out * d.n_in : 0) + 256;
     return w;
 }
 
-hipError_t launch_mfma(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
-    a.S = mfma_slices(d);
-    a.G = mfma_group(d);
+hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
+    a.S = d.R > 0 ? wgrad_slices(d) : 1;
     a.part = w.part;
-    const int64_t nct = (d.n_in + BN - 1) / BN;
-    const int64_t items = (int64_t)((d.n_out + BM - 1) / BM) * ((nct + a.G - 1) / a.G) * a.S;
-    int64_t grid;
     hipError_t e;
-    if (d.N > 1) {
-        e = launch_expert_order(a.offsets, d.N, w.order, st);
-        if (e != hipSuccess) return e;
-        a.order = w.order;
-        grid = items * ((d.N + kNumXcd - 1) / kNumXcd) * kNumXcd;
-    } else {
-        grid = (items + kNumXcd - 1) / kNumXcd * kNumXcd;
-    }
-    {
+    if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
+        a.G = wgrad_group(d);
+        const int64_t items = ceil_div(d.n_out, BM) * ceil_div(ceil_div(d.n_in, BN), a.G) * a.S;
+        int64_t grid = ceil_div(items, kNumXcd) * kNumXcd;
+        if (d.N > 1) {
+            e = launch_expert_order(a.offsets, d.N, w.order, st);
+            if (e != hipSuccess) return e;
+            a.order = w.order;
+            grid = items * ceil_div(d.N, kNumXcd) * kNumXcd;
+        }
         LaunchScope scope("wgrad_mfma", st);
         hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
+    } else {
+        const dim3 grid((unsigned)(wgrad_tile_count(d, kTile) / d.N), d.N, a.S);
+        LaunchScope scope("wgrad_tile", st);
+        if (d.act_dtype == PR2_BF16)
+            hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, grid, dim3(256), 0, st, a);
+        else
+            hipLaunchKernelGGL(wgrad_tile_kernel<float>, grid, dim3(256), 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
     const int64_t n = (int64_t)d.N * d.n_out * d.n_in;
     LaunchScope scope("wgrad_join", st);
-    hipLaunchKernelGGL(wgrad_join_kernel, dim3((unsigned)((n / 4 + 255) / 256)), dim3(256), 0, st,
-                       a.part, n, a.S, a.dW);
+    hipLaunchKernelGGL(wgrad_join_kernel, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, st, a.part,
+                       n, a.S, a.dW);
     return hipGetLastError();
 }
 
@@ -641,18 +693,7 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
     const hipStream_t st = (hipStream_t)stream;
     WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
                 d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1};
-    hipError_t e;
-    if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
-        e = launch_mfma(d, a, wgrad_ws(d, ws), st);
-    } else {
-        const int64_t tiles = (int64_t)((d.n_out + kTile - 1) / kTile) * ((d.n_in + kTile - 1) / kTile);
-        LaunchScope scope("wgrad_tile", st);
-        if (d.act_dtype == PR2_BF16)
-            hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, dim3((unsigned)tiles, d.N), dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL(wgrad_tile_kernel<float>, dim3((unsigned)tiles, d.N), dim3(256), 0, st, a);
-        e = hipGetLastError();
-    }
+    const hipError_t e = launch_wgrad(d, a, wgrad_ws(d, ws), st);
     if (e != hipSuccess) return hip_fail(e, "weight_grad_packed launch");
     return ok();
 }
