@@ -390,6 +390,9 @@ constexpr int64_t kMaxRows = 0x7fffffff / kMaxParts;    // the grid is T x parts
 constexpr int64_t kFillWgs = 2048;      // workgroups of 256 that fill the chip
 constexpr size_t kPartBytes = sizeof(float4) * 2 * kFillWgs;
 
+// Rows of up to this many chunks fit the registers of 512 threads.
+constexpr int kShortRow = 512 * 18;
+
 int row_chunks(const pr2_policy_desc& d) {
     const int e = d.act_dtype == PR2_BF16 ? 8 : 4;
     return (int)(((int64_t)d.V + e - 1) / e);
@@ -408,8 +411,13 @@ int row_parts(const pr2_policy_desc& d) {
 // read are still there (104 MB of each: both passes 68 -> 57 us).  The eight L2s hold 32 MiB.
 constexpr int64_t kStreamBytes = 32 << 20;
 
-// Below this many rows the fused kernel leaves CUs idle and its rows are read twice instead.
-constexpr int64_t kFusedRows = 192;
+// Long rows, a whole CU each in the fused form, are better read twice by many workgroups while
+// they are few: loss and gradient of 151936 bf16 logits take 16, 23 and 38.5 us in 1, 64 and
+// 191 rows that way, 25, 32 and 40 fused; 256 rows 46 and 46, 2048 rows 343 and 266.  Shorter
+// rows are faster fused at any count (32000 logits: 13 against 16 us for one row, 63 against
+// 77 for 2048).
+constexpr int64_t kFewRows = 192;
+bool fuse_rows(const pr2_policy_desc& d) { return d.T >= kFewRows || row_chunks(d) <= kShortRow; }
 
 struct PolicyWs {
     float4* rowsum;
@@ -527,7 +535,7 @@ hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, hipStream
         hipLaunchKernelGGL((policy_fused_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
     else if (n <= 256 * 16)
         hipLaunchKernelGGL((policy_fused_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
-    else if (n <= 512 * 18)
+    else if (n <= kShortRow)
         hipLaunchKernelGGL((policy_fused_kernel<T, 512, 18>), grid, dim3(512), 0, s, a);
     else
         hipLaunchKernelGGL((policy_fused_kernel<T, 1024, 20>), grid, dim3(1024), 0, s, a);
@@ -620,7 +628,7 @@ pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, cons
         a.dz = dlogits;
         const bool bf = d.act_dtype == PR2_BF16;
         hipError_t e;
-        if (grad && d.T >= kFusedRows) {
+        if (grad && fuse_rows(d)) {
             e = bf ? launch_fused<bf16_t>(d, a, st) : launch_fused<float>(d, a, st);
         } else {
             const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
