@@ -439,12 +439,11 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
                 if (active) phase(C0{}, h % kStages, 1, [](int) __attribute__((always_inline)) {});
                 if (!PACKS) wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
                 barrier();
-                const bool more = h + (PACKS ? 2 : kStages) < nh;
                 auto part = [&](int j) __attribute__((always_inline)) {
                     if (PACKS) {
-                        if (more) write_packed(S_, h + 2, j);
+                        write_packed(S_, h + 2, j);     // (past the end into a stage nobody reads)
                         if (j == 3) load_packed(S_, ct, h + 4);
-                    } else if (more) {
+                    } else if (h + kStages < nh) {
                         copy_dy(h + kStages, j);
                     }
                 };
