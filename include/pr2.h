@@ -426,11 +426,11 @@ pr2_status pr2_predictor_loss(const pr2_moe_desc* desc, const void* h, const flo
  * be sampled) has probability 0.  NaN or +infinity in a row that counts make that row's
  * results NaN.
  *
- * T rows (>= 0, below 2^25), V vocabulary size (>= 1), ldl and ldd (>= V) the row strides in
- * elements of logits and dlogits (ldd is read only by calls that write dlogits), act_dtype of
- * both, token_dtype PR2_I32 or PR2_I64 of the ids, inv_temp > 0, clip_low, clip_high and
- * kl_coef >= 0, all finite.  Logits and gradients need only their element's alignment, rows
- * may start anywhere.
+ * T rows (>= 0, below 2^25), V vocabulary size (>= 1), ldl and ldd (>= V, at most 2^35) the row
+ * strides in elements of logits and dlogits (ldd is read only by calls that write dlogits),
+ * act_dtype of both, token_dtype PR2_I32 or PR2_I64 of the ids, inv_temp > 0, clip_low,
+ * clip_high and kl_coef >= 0, all finite.  Logits and gradients need only their element's
+ * alignment, rows may start anywhere.
  * Per-token tensors are [T] fp32, contiguous.
  */
 typedef struct {

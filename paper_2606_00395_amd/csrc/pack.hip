@@ -24,7 +24,7 @@ typedef u32x4 u32x4_byte __attribute__((aligned(1)));    // int8 rows start anyw
 struct Tiling {
     int64_t R;
     int rows, per;
-    uint32_t magic;         // ceil(2^32 / per); 0 with one row per workgroup
+    uint32_t magic;         // ceil(2^32 / per); 0 with one row per workgroup (and unused at per = 1)
 };
 
 Tiling tiling(int64_t R, int64_t per) {
@@ -33,7 +33,6 @@ Tiling tiling(int64_t R, int64_t per) {
     t.per = (int)per;
     t.rows = per >= kUnits ? 1 : (int)(kUnits / per);
     t.magic = t.rows == 1 ? 0 : (uint32_t)(((1ull << 32) + per - 1) / per);
-    if (per == 1) t.magic = 0xffffffffu;        // floor(i (2^32 - 1) / 2^32) would be i - 1
     return t;
 }
 

@@ -7,7 +7,11 @@
 // and with the gradient's coefficient c = d loss / d logp, which depends on logp alone,
 //   dlogits_v = c s ([v = y] - 2^(k (z_v - M)) / S).
 // Bound by HBM: V elements read per row, and V written where the gradient is wanted;
-// two exponentials per element (a quarter-rate instruction each) come next.
+// two exponentials per element (a quarter-rate instruction each) come next.  Loss and gradient
+// of 4096 x 151936 bf16 logits take 484 us, 5.15 TB/s (a large copy reaches 5.2); of 517 x
+// 50257 fp32 in two calls 58 us, 5.3 TB/s; log-probabilities of 8 rows 12 us, two launches.
+#include <type_traits>
+
 #include "chunk.h"
 
 namespace pr2 {
@@ -62,27 +66,31 @@ __device__ __forceinline__ void join_lanes(Stat& a, float k) {
     }
 }
 
+// What the wavefronts of a workgroup exchange.
+template <int W>
+struct Exchange {
+    float m[W], s[W], e[W];
+};
+
 // all threads get the workgroup's statistics, joined in the same order every time
-template <int NT>
-__device__ __forceinline__ void join_block(Stat& a, float k) {
-    constexpr int W = NT / 64;
-    __shared__ float sm[W], ss[W], se[W];
+template <int W>
+__device__ __forceinline__ void join_block(Stat& a, float k, Exchange<W>& x) {
     join_lanes(a, k);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     if (lane == 0) {
-        sm[wave] = a.m;
-        ss[wave] = a.s;
-        se[wave] = a.e;
+        x.m[wave] = a.m;
+        x.s[wave] = a.s;
+        x.e[wave] = a.e;
     }
     __syncthreads();
-    Stat r{sm[0], ss[0], se[0]};
+    Stat r{x.m[0], x.s[0], x.e[0]};
     float m = r.m;
 #pragma unroll
-    for (int w = 1; w < W; ++w) m = fmaxf(m, sm[w]);
+    for (int w = 1; w < W; ++w) m = fmaxf(m, x.m[w]);
     rebase(r, m, k);
 #pragma unroll
     for (int w = 1; w < W; ++w) {
-        Stat b{sm[w], ss[w], se[w]};
+        Stat b{x.m[w], x.s[w], x.e[w]};
         rebase(b, m, k);
         r.s += b.s;
         r.e += b.e;
@@ -189,6 +197,7 @@ __global__ void __launch_bounds__(kStatThreads) policy_stats_kernel(PolicyArgs a
     constexpr int E = Chunk<T>::E;
     const int64_t t = blockIdx.x / a.S;
     const int part = (int)(blockIdx.x - t * a.S);
+    __shared__ Exchange<kStatThreads / 64> x;
     const Row r = open_row(a, t);
     Stat st{kLowest, 0.0f, 0.0f};
     const T* z = (const T*)a.z + t * a.ldl;
@@ -217,7 +226,7 @@ __global__ void __launch_bounds__(kStatThreads) policy_stats_kernel(PolicyArgs a
             Chunk<T>::open(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), v);
             add_terms<E>(st, v, a.k);
         }
-        join_block<kStatThreads>(st, a.k);
+        join_block(st, a.k, x);
     }
     if (a.S > 1) {
         if (threadIdx.x == 0) a.part[blockIdx.x] = make_float4(st.m, st.s, st.e, 0.0f);
@@ -296,65 +305,114 @@ __global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
     }
 }
 
-// Loss and gradient of one row per workgroup.  The row's first NT * NCH chunks stay in
+// Loss and gradient, one row at a time per workgroup.  The row's first NT * NCH chunks stay in
 // registers between the two passes (a CU's register file is 512 KiB, a row of 151936 bf16
-// logits 297 KiB), the rest is read again.
-template <typename T, int NT, int NCH>
-__global__ void __launch_bounds__(NT) policy_fused_kernel(PolicyArgs a) {
+// logits 297 KiB), the rest is read again; the elements after its last whole chunk go one to
+// a thread.  A workgroup that fills a CU (NEXT) takes rows from a counter until they are used
+// up, and loads each piece of the next row into the registers that the piece of this one
+// has just left, so that the memory does not wait for a row's statistics; the others take
+// one row, and hide behind each other.
+template <typename T, int NT, int NCH, bool NEXT>
+__global__ void __launch_bounds__(NT) policy_fused_kernel(PolicyArgs a, int* counter) {
     constexpr int E = Chunk<T>::E;
-    const int64_t t = blockIdx.x;
-    const int tid = threadIdx.x;
-    const Row r = open_row(a, t);
-    const T* z = (const T*)a.z + t * a.ldl;
-    T* dz = (T*)a.dz + t * a.ldd;
+    __shared__ Exchange<NT / 64> x[2];
+    __shared__ int s_next[2];
+    int tid = threadIdx.x;
     const int full = a.V / E, rem = a.V % E;
-    const int n = full + (rem != 0);
-    Stat st{kLowest, 0.0f, 0.0f};
-    float zy = 0.0f;
+    int64_t t = blockIdx.x;
+    Row r = open_row(a, t);
     u32x4 w[NCH];
-    if (r.on) {
-        zy = Act<T>::to_f32(z[r.y]);
-#pragma unroll
-        for (int i = 0; i < NCH; ++i)
-            w[i] = load_chunk(z, i * NT + tid, full, rem, Chunk<T>::kNegInf);
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-            float v[E];
-            Chunk<T>::open(w[i], v);
-            add_terms<E>(st, v, a.k);
-        }
-        for (int c = NCH * NT + tid; c < n; c += NT) {
-            float v[E];
-            Chunk<T>::open(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), v);
-            add_terms<E>(st, v, a.k);
-        }
-        // every thread holds z_y before the barrier behind which it may be overwritten
-        asm volatile("" ::"v"(zy));
-        join_block<NT>(st, a.k);
-    }
-    const Result res = close_row(a, t, r, zy, st, tid == 0);
-    if (res.coef == 0.0f) {
-        zero_chunks(dz, tid, n, NT, full, rem);
-        return;
-    }
-    const float g = res.coef * a.it;
-    const float gs = -g / st.s;
-    const float gy = -g * expm1f(res.logp);       // c s (1 - p_y) without the cancellation
-    const int yc = (int)(r.y / E), ye = (int)(r.y % E);
-    auto put = [&](const u32x4& raw, int c) __attribute__((always_inline)) {
-        float v[E];
-        Chunk<T>::open(raw, v);
-#pragma unroll
-        for (int j = 0; j < E; ++j) v[j] = gs * exp2_native((v[j] - st.m) * a.k);
-        if (c == yc) {
-#pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = j == ye ? gy : v[j];
-        }
-        store_chunk(dz, c, full, rem, v);
+    auto load_piece = [&](const T* z, int i) __attribute__((always_inline)) {
+        const int c = i * NT + tid;
+        constexpr uint32_t p = Chunk<T>::kNegInf;
+        w[i] = c < full ? load16<false>(z + (int64_t)c * E) : u32x4{p, p, p, p};
     };
+    if (r.on) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) put(w[i], i * NT + tid);
-    for (int c = NCH * NT + tid; c < n; c += NT) put(load_chunk(z, c, full, rem, Chunk<T>::kNegInf), c);
+        for (int i = 0; i < NCH; ++i) load_piece((const T*)a.z + t * a.ldl, i);
+    }
+    for (int turn = 0;; turn ^= 1) {
+        // (a new number each time: kept over the turns, the pieces' addresses fill the registers)
+        if (NEXT) asm volatile("" : "+v"(tid));
+        const T* z = (const T*)a.z + t * a.ldl;
+        T* dz = (T*)a.dz + t * a.ldd;
+        if (NEXT && tid == 0) s_next[turn] = gridDim.x + atomicAdd(counter, 1);
+        Stat st{kLowest, 0.0f, 0.0f};
+        float zy = 0.0f, zt = 0.0f;
+        if (r.on) {
+            zy = Act<T>::to_f32(z[r.y]);
+            if (tid < rem) {
+                zt = Act<T>::to_f32(z[(int64_t)full * E + tid]);
+                add_terms<1>(st, &zt, a.k);
+            }
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                float v[E];
+                Chunk<T>::open(w[i], v);
+                add_terms<E>(st, v, a.k);
+            }
+            for (int c = NCH * NT + tid; c < full; c += NT) {
+                float v[E];
+                Chunk<T>::open(load16<false>(z + (int64_t)c * E), v);
+                add_terms<E>(st, v, a.k);
+            }
+            // every thread holds z_y before the barrier behind which it may be overwritten
+            asm volatile("" ::"v"(zy));
+            join_block(st, a.k, x[turn]);
+        } else if (NEXT) {
+            __syncthreads();
+        }
+        const int64_t t1 = NEXT ? s_next[turn] : a.T;
+        const Row r1 = NEXT && t1 < a.T ? open_row(a, t1) : Row{0, 0.0f, false};
+        const T* z1 = (const T*)a.z + (NEXT && t1 < a.T ? t1 * a.ldl : 0);
+        const Result res = close_row(a, t, r, zy, st, tid == 0);
+        const float g = res.coef * a.it;
+        const float gy = -g * expm1f(res.logp);       // c s (1 - p_y) without the cancellation
+        const int yc = (int)(r.y / E), ye = (int)(r.y % E);
+        const bool some = res.coef != 0.0f;
+        const float gs = some ? -g / st.s : 0.0f;
+        auto open_piece = [&](const u32x4& raw, int c, float (&v)[E]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = 0.0f;
+            if (!some) return;
+            Chunk<T>::open(raw, v);
+#pragma unroll
+            for (int j = 0; j < E; ++j) v[j] = gs * exp2_native((v[j] - st.m) * a.k);
+            if (c == yc) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[j] = j == ye ? gy : v[j];
+            }
+        };
+        auto pieces = [&](auto more) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < NCH; ++i) {
+                const int c = i * NT + tid;
+                float v[E];
+                open_piece(w[i], c, v);
+                const u32x4 o = Chunk<T>::close(v);
+                if (decltype(more)::value) load_piece(z1, i);
+                if (c < full) store16<false>(dz + (int64_t)c * E, o);
+                if (NEXT) __builtin_amdgcn_sched_barrier(0);    // one piece's values at a time
+            }
+        };
+        if (NEXT && r1.on) pieces(std::true_type{});
+        else pieces(std::false_type{});
+        for (int c = NCH * NT + tid; c < full; c += NT) {
+            u32x4 raw = {};
+            float v[E];
+            if (some) raw = load16<false>(z + (int64_t)c * E);
+            open_piece(raw, c, v);
+            store16<false>(dz + (int64_t)c * E, Chunk<T>::close(v));
+        }
+        if (tid < rem) {
+            float v = some ? gs * exp2_native((zt - st.m) * a.k) : 0.0f;
+            if (some && full == yc && tid == ye) v = gy;
+            dz[(int64_t)full * E + tid] = Act<T>::from_f32(v);
+        }
+        if (t1 >= a.T) return;
+        t = t1;
+        r = r1;
+    }
 }
 
 // the four sums over the tokens, in fp64 and a fixed order
@@ -385,13 +443,18 @@ policy_sums_kernel(const float4* rows, int64_t T, float* out) {
 }
 
 // ------------------------------------------------------------------ host ----
+constexpr int kCus = 256;
 constexpr int kMaxParts = 64;
 constexpr int64_t kMaxRows = 0x7fffffff / kMaxParts;    // the grid is T x parts
+constexpr int64_t kMaxStride = (int64_t)1 << 35;        // T x stride in bytes stays below 2^63
 constexpr int64_t kFillWgs = 2048;      // workgroups of 256 that fill the chip
 constexpr size_t kPartBytes = sizeof(float4) * 2 * kFillWgs;
 
 // Rows of up to this many chunks fit the registers of 512 threads.
 constexpr int kShortRow = 512 * 18;
+
+// Chunks per thread that 1024 threads hold of a longer one.
+constexpr int kLongHeld = 19;
 
 int row_chunks(const pr2_policy_desc& d) {
     const int e = d.act_dtype == PR2_BF16 ? 8 : 4;
@@ -420,6 +483,7 @@ constexpr int64_t kFewRows = 192;
 bool fuse_rows(const pr2_policy_desc& d) { return d.T >= kFewRows || row_chunks(d) <= kShortRow; }
 
 struct PolicyWs {
+    int* counter;
     float4* rowsum;
     float4* part;
     size_t bytes;
@@ -428,7 +492,8 @@ struct PolicyWs {
 PolicyWs policy_ws(const pr2_policy_desc& d, void* base) {
     char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
     PolicyWs w{};
-    w.part = (float4*)p;
+    w.part = (float4*)p;            // (split rows and the counter exclude each other)
+    w.counter = (int*)p;
     const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
     w.rowsum = (float4*)(p ? p + kPartBytes : nullptr);
     w.bytes = kPartBytes + 3 * stats + 256;
@@ -459,6 +524,9 @@ pr2_status check_policy(const pr2_policy_desc* desc, bool loss, bool grad) {
                     (long long)kMaxRows);
     if (d.V > 0x7fffffff - 65536)
         return fail(PR2_ERR_UNSUPPORTED, "V = %d is too large", d.V);
+    if (d.ldl > kMaxStride || (grad && d.ldd > kMaxStride))
+        return fail(PR2_ERR_UNSUPPORTED, "ldl = %lld or ldd = %lld exceeds %lld", (long long)d.ldl,
+                    (long long)d.ldd, (long long)kMaxStride);
     return PR2_OK;
 }
 
@@ -527,18 +595,29 @@ hipError_t launch_grad(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
 }
 
 template <typename T>
-hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, hipStream_t s) {
+hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, int* counter, hipStream_t s) {
     const int n = row_chunks(d);
     const dim3 grid((unsigned)d.T);
+    // Rows that are held whole, eight a CU or more: the counter's turns (4096 rows of 151936
+    // bf16 logits, a tenth of them without weight, 519 -> 484 us; without it 2048 rows took
+    // 266 and 1024 rows 148 us, with it 267 and 149; 2048 fp32 rows, half of each read
+    // again, 529 and 559).
+    if (n > kShortRow && n <= 1024 * kLongHeld && d.T >= 8 * kCus) {
+        const hipError_t e = launch_zero_i32(counter, 1, s);
+        if (e != hipSuccess) return e;
+        LaunchScope scope("policy_fused", s);
+        hipLaunchKernelGGL((policy_fused_kernel<T, 1024, kLongHeld, true>), dim3(kCus), dim3(1024), 0, s, a, counter);
+        return hipGetLastError();
+    }
     LaunchScope scope("policy_fused", s);
     if (n <= 256 * 4)
-        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 4>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 4, false>), grid, dim3(256), 0, s, a, nullptr);
     else if (n <= 256 * 16)
-        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 16>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((policy_fused_kernel<T, 256, 16, false>), grid, dim3(256), 0, s, a, nullptr);
     else if (n <= kShortRow)
-        hipLaunchKernelGGL((policy_fused_kernel<T, 512, 18>), grid, dim3(512), 0, s, a);
+        hipLaunchKernelGGL((policy_fused_kernel<T, 512, 18, false>), grid, dim3(512), 0, s, a, nullptr);
     else
-        hipLaunchKernelGGL((policy_fused_kernel<T, 1024, 20>), grid, dim3(1024), 0, s, a);
+        hipLaunchKernelGGL((policy_fused_kernel<T, 1024, kLongHeld, false>), grid, dim3(1024), 0, s, a, nullptr);
     return hipGetLastError();
 }
 
@@ -629,7 +708,7 @@ pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, cons
         const bool bf = d.act_dtype == PR2_BF16;
         hipError_t e;
         if (grad && fuse_rows(d)) {
-            e = bf ? launch_fused<bf16_t>(d, a, st) : launch_fused<float>(d, a, st);
+            e = bf ? launch_fused<bf16_t>(d, a, w.counter, st) : launch_fused<float>(d, a, w.counter, st);
         } else {
             const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
             if (grad && !a.lse) a.lse = (float*)((char*)w.rowsum + stats);

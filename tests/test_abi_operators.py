@@ -60,7 +60,7 @@ def loss_backward(d, **kw):
     (dict(act_dtype=9), "PR2_ERR_DTYPE"), (dict(token_dtype=B.PR2_I16), "PR2_ERR_DTYPE"),
     (dict(inv_temp=0.0), "PR2_ERR_SHAPE"), (dict(inv_temp=-1.0), "PR2_ERR_SHAPE"),
     (dict(inv_temp=float("nan")), "PR2_ERR_SHAPE"), (dict(inv_temp=float("inf")), "PR2_ERR_SHAPE"),
-    (dict(T=1 << 40), "PR2_ERR_UNSUPPORTED"), (dict(V=2 ** 31 - 1, ldl=2 ** 31), "PR2_ERR_UNSUPPORTED"),
+    (dict(T=1 << 40), "PR2_ERR_UNSUPPORTED"), (dict(ldl=1 << 40), "PR2_ERR_UNSUPPORTED"), (dict(V=2 ** 31 - 1, ldl=2 ** 31), "PR2_ERR_UNSUPPORTED"),
 ])
 def test_policy_descriptor(kw, status):
     d = policy_desc(**kw)
@@ -215,6 +215,13 @@ def test_weight_grad_arguments():
     for kw in (dict(N=1025), dict(R=2 ** 31, Rx=2 ** 31), dict(n_in=2 ** 21)):
         assert wg(**kw) == "PR2_ERR_UNSUPPORTED", kw
     assert wg(R=0, Rx=0, ptr=dict(dy=0, q=0, e=0, off=0)) in READY      # zeros are still written
+    # few tiles and many rows: the workspace holds the slices' partial sums
+    long = dict(R=8192, Rx=8192, n_out=2048, n_in=2048, N=1)
+    need = B.lib().pr2_weight_grad_workspace_bytes(byref(B.WgradDesc(k=1, act_dtype=B.PR2_BF16, **long)))
+    assert need > 2 * 4 * 2048 * 2048
+    assert wg(ptr={"off": 0}, **long) in READY
+    assert wg(ptr={"off": 0}, ws_bytes=need - 1, **long) == "PR2_ERR_WORKSPACE"
+    assert wg(ptr={"off": 0, "ws": 0}, **long) == "PR2_ERR_NULL"
 
 
 def test_null_descriptors():

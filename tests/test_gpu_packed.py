@@ -168,6 +168,57 @@ def test_weight_gradients_of_experts(case, bf16):
     assert torch.all(dW[torch.from_numpy(empty).cuda()] == 0)
 
 
+def test_many_experts_and_long_ones():
+    """1024 experts in 6144 tiles (two column tiles per workgroup), one expert with more rows
+    than a workgroup holds the indexes of, one with none; sampled experts against float64."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    N, n_out, n_in, T = 1024, 264, 528, 1500
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows = torch.randint(0, 6, (N,), generator=g, device="cuda")
+    rows[7], rows[8], rows[1023] = 17000, 0, 33
+    R = int(rows.sum())
+    off = torch.cat([rows.new_zeros(1), rows.cumsum(0)]).to(torch.int32)
+    route = torch.randint(0, 2 * T, (R,), generator=g, device="cuda", dtype=torch.int32)
+    dy = torch.randn((R, n_out), generator=g, device="cuda").to(torch.bfloat16)
+    x = torch.randn((T, n_in), generator=g, device="cuda").to(torch.bfloat16)
+    q, e = do_pack(x)
+    dW = torch.full((N, n_out, n_in), float("nan"), device="cuda")
+    B.weight_grad_packed(dy, q, e, dW, offsets=off, route_of_row=route, k=2)
+    v = torch.empty_like(x)
+    B.act_unpack(q, e, v)
+    ends = off.tolist()
+    for i in [0, 1, 2, 6, 7, 8, 9, 500, 1022, 1023]:
+        a = dy[ends[i]:ends[i + 1]].double()
+        b = v[(route[ends[i]:ends[i + 1]] // 2).long()].double()
+        want, mag = a.T @ b, a.abs().T @ b.abs()
+        assert torch.all((dW[i].double() - want).abs() <= (len(a) + 2) * 2.0 ** -23 * mag + 1e-37), i
+    assert torch.isfinite(dW).all() and torch.all(dW[8] == 0)
+    again = torch.empty_like(dW)
+    B.weight_grad_packed(dy, q, e, again, offsets=off, route_of_row=route, k=2)
+    assert torch.equal(again, dW)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_weight_gradient_over_many_rows(bf16):
+    """Slices of the rows, each in several parts, and their join; an odd number of outputs."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    for R, n_out, n_in in ((70001, 248, 240), (20011, 77, 35)):
+        g = torch.Generator(device="cuda").manual_seed(R)
+        dt = torch.bfloat16 if bf16 else torch.float32
+        dy = torch.randn((R, n_out), generator=g, device="cuda").to(dt)
+        x = torch.randn((R, n_in), generator=g, device="cuda").to(dt)
+        q, e = do_pack(x)
+        v = torch.empty_like(x)
+        B.act_unpack(q, e, v)
+        dW = torch.full((1, n_out, n_in), float("nan"), device="cuda")
+        B.weight_grad_packed(dy, q, e, dW)
+        want, mag = dy.double().T @ v.double(), dy.double().abs().T @ v.double().abs()
+        # (sums of slices: the longest chain is shorter than R)
+        assert torch.all((dW[0].double() - want).abs() <= 2.0 ** -23 * 2000 * mag)
+
+
 @pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
 def test_rows_without_a_source_add_nothing(bf16):
     import torch

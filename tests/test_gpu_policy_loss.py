@@ -366,3 +366,42 @@ def test_refusals_of_the_binding():
     with pytest.raises(B.Pr2Error, match="overlaps"):
         wide = torch.zeros((4, 20), device="cuda")
         B.policy_loss(wide[:, :10], y, f, f, torch.zeros(4, device="cuda"), dlogits=wide[:, 5:15])
+
+
+def test_many_long_rows_taken_in_turns():
+    """2300 rows that take a CU each, a third of them without weight: the rows' results are
+    those of the same rows in batches too small for turns, bit for bit, whatever order the
+    turns came in; and rows of a sample against the definition."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    T, V = 2300, 80003
+    g = torch.Generator(device="cuda").manual_seed(11)
+    z = torch.empty((T, V), dtype=torch.bfloat16, device="cuda")
+    for t0 in range(0, T, 100):
+        z[t0:t0 + 100] = torch.randn((100, V), generator=g, device="cuda").mul_(3).to(torch.bfloat16)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda")
+    old = torch.full((T,), -12.0, device="cuda")
+    adv = torch.randn(T, generator=g, device="cuda")
+    w = (torch.rand(T, generator=g, device="cuda") > 0.33).float() / T
+    logp, coef, sums = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty(4, device="cuda")
+    grad = torch.empty_like(z)
+    for _ in range(3):
+        for t in (logp, coef, sums, grad):
+            t.fill_(float("nan"))
+        B.policy_loss(z, y, old, adv, sums, weight=w, logp_out=logp, coef_out=coef, dlogits=grad)
+    for t0 in range(0, T, 575):
+        sl = slice(t0, t0 + 575)
+        lp, cf, gr = torch.empty(575, device="cuda"), torch.empty(575, device="cuda"), torch.empty_like(grad[sl])
+        B.policy_loss(z[sl], y[sl], old[sl], adv[sl], torch.empty(4, device="cuda"), weight=w[sl], logp_out=lp,
+                      coef_out=cf, dlogits=gr)
+        assert torch.equal(lp, logp[sl]) and torch.equal(cf, coef[sl]) and torch.equal(gr, grad[sl])
+    pick = torch.cat([torch.arange(6, device="cuda"), torch.arange(T - 6, T, device="cuda")])
+    host = dict(logits=z[pick].float().cpu().numpy(), token=y[pick].cpu().numpy(), logp_old=old[pick].cpu().numpy(),
+                adv=adv[pick].cpu().numpy(), logp_ref=None, weight=w[pick].cpu().numpy(), kl_coef=0.0, inv_temp=1.0)
+    ref = O.policy_loss(**host, clip_low=np.float32(0.2), clip_high=np.float32(0.28))
+    got = grad[pick].double().cpu().numpy()
+    assert np.all(np.abs(logp[pick].cpu().numpy() - ref["logp"]) <= 1e-5 + 4e-7 * np.abs(ref["logp"]))
+    assert np.all(np.abs(got - ref["dlogits"]) <= 2.0 ** -7 * np.abs(ref["dlogits"]) + 1e-37)
+    in_place = z
+    B.policy_loss(in_place, y, old, adv, sums, weight=w, dlogits=in_place)
+    assert torch.equal(in_place, grad)
