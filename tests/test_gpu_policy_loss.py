@@ -99,7 +99,7 @@ def compare(got, host, bf16, factor=1.0):
     return ref
 
 
-SIZES = [(1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 1000), (9, 4097), (2, 33001), (1, 165001),
+SIZES = [(17, 20001), (16, 9001), (1, 1), (3, 2), (2, 7), (5, 8), (4, 9), (1, 1000), (9, 4097), (2, 33001), (1, 165001),
          (200, 1030), (195, 4200), (193, 33100), (192, 70001), (192, 165000)]
 
 
