@@ -163,17 +163,31 @@ def check(status: int):
 # ----------------------------------------------------------- torch glue ----
 # A decode step's route call is bound by this module's work on the host, so each
 # check first tests everything at once and names the fault only when there is one
-# (256 tokens: 10.9 us per call before the library was entered, now 6.5).
+# (256 tokens: 10.9 us per call before the library was entered, then 6.5).  With torch
+# loaded, compiled forms of the two checks (_args, if built) take the place of _need and
+# _need_act and come back to these for everything that they would refuse.
 
 _torch_module = None
 _raw_stream = None      # (device index) -> raw handle of its current stream
+_raw_device = None      # () -> current device
+_ACT_CODES = {}         # torch dtype -> dtype code of an activation
 
 
 def _torch():
-    global _torch_module, _raw_stream
+    global _torch_module, _raw_stream, _raw_device, _need, _need_act
     if _torch_module is None:
         import torch
-        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+            _raw_stream = torch._C._cuda_getCurrentRawStream
+            _raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        try:
+            from . import _args
+        except ImportError:
+            pass
+        else:
+            _args.refuse_with(_need, _need_act)
+            _need, _need_act = _args.need, _args.need_act
+        _ACT_CODES.update({torch.bfloat16: PR2_BF16, torch.float32: PR2_F32})
         _torch_module = torch
     return _torch_module
 
@@ -183,13 +197,11 @@ def _ptr(t):
 
 
 def _act_code(t):
-    torch = _torch()
-    dt = t.dtype
-    if dt == torch.bfloat16:
-        return PR2_BF16
-    if dt == torch.float32:
-        return PR2_F32
-    raise TypeError(f"activations must be bfloat16 or float32, got {dt}")
+    _torch()
+    code = _ACT_CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"activations must be bfloat16 or float32, got {t.dtype}")
+    return code
 
 
 def _idx_code(t):
@@ -207,7 +219,7 @@ def _stream(stream):
         return stream.cuda_stream
     torch = _torch()
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -222,17 +234,18 @@ def _row_stride(idx):
 
 def _need(t, name, shape, dtype=None, device=None, optional=False):
     """Checks that tensor ``t`` is what the C ABI will read or write through its
-    pointer: the given shape, dtype and device, row-major and contiguous."""
+    pointer: the given shape, dtype and device, row-major and contiguous.  Returns the
+    pointer (None for no tensor)."""
     if t is None:
         if optional:
-            return
+            return None
         raise ValueError(f"{name} is required")
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if (t.shape == shape and (dtype is None or t.dtype == dtype) and t.is_contiguous()
             and (device is None or t.device == device)):
-        return
+        return t.data_ptr()
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
@@ -241,6 +254,7 @@ def _need(t, name, shape, dtype=None, device=None, optional=False):
         raise ValueError(f"{name} must be contiguous (row-major)")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
+    return t.data_ptr()
 
 
 def _need_ids(idx, name, T, k, device):
@@ -270,10 +284,11 @@ def _need_act(x, name="x"):
 
 def _need_ws(ws, device):
     if ws is None:
-        return
+        return None
     torch = _torch()
     if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
         raise ValueError("ws must be a contiguous uint8 tensor on the inputs' device")
+    return ws
 
 
 def _new_ws(nbytes, device, stream):
@@ -668,18 +683,19 @@ def _logit_rows(t, name, device=None, shape=None, dtype=None):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
     T, V = t.shape
-    if V > 1 and t.stride(1) != 1:
+    rows, columns = t.stride()
+    if V > 1 and columns != 1:
         raise ValueError(f"{name} must have unit stride along V")
     if T <= 1:
         return V
-    if t.stride(0) < V:
+    if rows < V:
         raise ValueError(f"rows of {name} overlap: row stride below V")
-    return t.stride(0)
+    return rows
 
 
 def _policy_desc(logits, token, inv_temp, clip_low=0.0, clip_high=0.0, kl_coef=0.0, dlogits=None):
@@ -689,12 +705,13 @@ def _policy_desc(logits, token, inv_temp, clip_low=0.0, clip_high=0.0, kl_coef=0
     T, V = logits.shape
     if token.shape != (T,):
         raise ValueError(f"token has shape {tuple(token.shape)}, expected {(T,)}")
-    if token.dtype == torch.int64:
+    ids = token.dtype
+    if ids == torch.int64:
         code = PR2_I64
-    elif token.dtype == torch.int32:
+    elif ids == torch.int32:
         code = PR2_I32
     else:
-        raise TypeError(f"token must be int32 or int64, got {token.dtype}")
+        raise TypeError(f"token must be int32 or int64, got {ids}")
     if not token.is_contiguous() or token.device != dev:
         raise ValueError("token must be contiguous, on the logits' device")
     ldd = 0
@@ -717,15 +734,16 @@ def token_logprob(logits, token, logp_out, lse_out=None, entropy_out=None, inv_t
     (logits [T, V], rows at any stride; token int32/int64 [T])."""
     torch = _torch()
     desc, T, dev = _policy_desc(logits, token, inv_temp)
-    _need(logp_out, "logp_out", (T,), torch.float32, dev)
-    _need(lse_out, "lse_out", (T,), torch.float32, dev, optional=True)
-    _need(entropy_out, "entropy_out", (T,), torch.float32, dev, optional=True)
-    _need_ws(ws, dev)
+    f = torch.float32
+    logp_out = _need(logp_out, "logp_out", (T,), f, dev)
+    lse_out = _need(lse_out, "lse_out", (T,), f, dev, True)
+    entropy_out = _need(entropy_out, "entropy_out", (T,), f, dev, True)
+    L, desc = lib(), byref(desc)
+    ws = _need_ws(ws, dev)
     if ws is None:
-        ws = policy_workspace(logits, stream)
-    check(lib().pr2_token_logprob(byref(desc), _ptr(logits), _ptr(token), _ptr(logp_out),
-                                  _ptr(lse_out), _ptr(entropy_out), _ptr(ws), ws.numel(),
-                                  _stream(stream)))
+        ws = _new_ws(L.pr2_policy_workspace_bytes(desc), dev, stream)
+    check(L.pr2_token_logprob(desc, logits.data_ptr(), token.data_ptr(), logp_out, lse_out,
+                              entropy_out, ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def policy_loss(logits, token, logp_old, adv, sums_out, logp_ref=None, weight=None, logp_out=None,
@@ -738,19 +756,23 @@ def policy_loss(logits, token, logp_old, adv, sums_out, logp_ref=None, weight=No
     torch = _torch()
     desc, T, dev = _policy_desc(logits, token, inv_temp, clip_low, clip_high, kl_coef, dlogits)
     f = torch.float32
-    _need(logp_old, "logp_old", (T,), f, dev)
-    _need(adv, "adv", (T,), f, dev)
-    _need(sums_out, "sums_out", (4,), f, dev)
-    for t, name in ((logp_ref, "logp_ref"), (weight, "weight"), (logp_out, "logp_out"),
-                    (lse_out, "lse_out"), (entropy_out, "entropy_out"), (coef_out, "coef_out")):
-        _need(t, name, (T,), f, dev, optional=True)
-    _need_ws(ws, dev)
+    row = (T,)
+    logp_old = _need(logp_old, "logp_old", row, f, dev)
+    adv = _need(adv, "adv", row, f, dev)
+    sums_out = _need(sums_out, "sums_out", (4,), f, dev)
+    logp_ref = _need(logp_ref, "logp_ref", row, f, dev, True)
+    weight = _need(weight, "weight", row, f, dev, True)
+    logp_out = _need(logp_out, "logp_out", row, f, dev, True)
+    lse_out = _need(lse_out, "lse_out", row, f, dev, True)
+    entropy_out = _need(entropy_out, "entropy_out", row, f, dev, True)
+    coef_out = _need(coef_out, "coef_out", row, f, dev, True)
+    L, desc = lib(), byref(desc)
+    ws = _need_ws(ws, dev)
     if ws is None:
-        ws = policy_workspace(logits, stream)
-    check(lib().pr2_policy_loss(byref(desc), _ptr(logits), _ptr(token), _ptr(logp_old),
-                                _ptr(logp_ref), _ptr(adv), _ptr(weight), _ptr(sums_out),
-                                _ptr(logp_out), _ptr(lse_out), _ptr(entropy_out), _ptr(coef_out),
-                                _ptr(dlogits), _ptr(ws), ws.numel(), _stream(stream)))
+        ws = _new_ws(L.pr2_policy_workspace_bytes(desc), dev, stream)
+    check(L.pr2_policy_loss(desc, logits.data_ptr(), token.data_ptr(), logp_old, logp_ref, adv,
+                            weight, sums_out, logp_out, lse_out, entropy_out, coef_out,
+                            _ptr(dlogits), ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 def policy_loss_backward(logits, token, lse, coef, dlogits, grad_loss=None, inv_temp=1.0,
@@ -761,13 +783,13 @@ def policy_loss_backward(logits, token, lse, coef, dlogits, grad_loss=None, inv_
     desc, T, dev = _policy_desc(logits, token, inv_temp, dlogits=dlogits)
     if dlogits is None:
         raise ValueError("dlogits is required")
-    _need(lse, "lse", (T,), torch.float32, dev)
-    _need(coef, "coef", (T,), torch.float32, dev)
+    lse = _need(lse, "lse", (T,), torch.float32, dev)
+    coef = _need(coef, "coef", (T,), torch.float32, dev)
     if grad_loss is not None and (grad_loss.numel() != 1 or grad_loss.dtype != torch.float32
                                   or grad_loss.device != dev):
         raise ValueError("grad_loss must be one fp32 element on the logits' device")
-    check(lib().pr2_policy_loss_backward(byref(desc), _ptr(logits), _ptr(token), _ptr(lse),
-                                         _ptr(coef), _ptr(grad_loss), _ptr(dlogits),
+    check(lib().pr2_policy_loss_backward(byref(desc), logits.data_ptr(), token.data_ptr(), lse,
+                                         coef, _ptr(grad_loss), dlogits.data_ptr(),
                                          _stream(stream)))
 
 
@@ -787,57 +809,61 @@ def dispatch_plan(idx, N, offsets, row_of_route, route_of_row, ws=None, stream=N
         raise ValueError("idx must be 2-D [T, k]")
     T, k = idx.shape
     dev = idx.device
-    if dev.type != "cuda":
+    if not idx.is_cuda:
         raise ValueError("idx must be a CUDA (HIP) tensor")
     ldi = _need_ids(idx, "idx", T, k, dev)
     if T <= 1:
         ldi = k
-    _need(offsets, "offsets", (N + 1,), torch.int32, dev)
-    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
-    _need(route_of_row, "route_of_row", (T * k,), torch.int32, dev)
-    _need_ws(ws, dev)
-    desc = make_desc(T, 1, N, k, idx=_idx_code(idx))
+    i32 = torch.int32
+    offsets = _need(offsets, "offsets", (N + 1,), i32, dev)
+    row_of_route = _need(row_of_route, "row_of_route", (T, k), i32, dev)
+    route_of_row = _need(route_of_row, "route_of_row", (T * k,), i32, dev)
+    L, desc = lib(), byref(MoeDesc(T, 1, N, k, 0, 0, PR2_BF16, _idx_code(idx), 1))
+    ws = _need_ws(ws, dev)
     if ws is None:
-        ws = _new_ws(workspace_bytes(desc, OP_DISPATCH_PLAN), dev, stream)
-    check(lib().pr2_dispatch_plan(byref(desc), _ptr(idx), ldi, _ptr(offsets), _ptr(row_of_route),
-                                  _ptr(route_of_row), _ptr(ws), ws.numel(), _stream(stream)))
+        ws = _new_ws(L.pr2_workspace_bytes(desc, OP_DISPATCH_PLAN), dev, stream)
+    check(L.pr2_dispatch_plan(desc, idx.data_ptr(), ldi, offsets, row_of_route, route_of_row,
+                              ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
-def _plan_shape(row_of_route, offsets, device):
-    """k and N of a plan; without offsets (the call reads none) N is k, the least allowed."""
+def _plan(row_of_route, offsets, T, device):
+    """k, N and the addresses of row_of_route and offsets; without offsets (the call reads
+    none) N is k, the least allowed."""
     torch = _torch()
-    if row_of_route.dim() != 2:
+    shape = row_of_route.shape
+    if len(shape) != 2:
         raise ValueError("row_of_route must be 2-D [T, k]")
-    k = row_of_route.shape[1]
+    k = N = shape[1]
+    row = _need(row_of_route, "row_of_route", (T, k), torch.int32, device)
     if offsets is None:
-        return k, k
-    if offsets.dim() != 1 or offsets.shape[0] < 2:
+        return k, N, row, None
+    shape = offsets.shape
+    if len(shape) != 1 or shape[0] < 2:
         raise ValueError("offsets must be 1-D [N + 1]")
-    _need(offsets, "offsets", offsets.shape, torch.int32, device)
-    return k, offsets.shape[0] - 1
+    return k, shape[0] - 1, row, _need(offsets, "offsets", shape, torch.int32, device)
+
+
+def _rows_desc(T, d, N, k, dtype):
+    return byref(MoeDesc(T, d, N, k, 0, 0, _ACT_CODES[dtype], PR2_I32, 1))
 
 
 def dispatch(x, offsets, row_of_route, xs, stream=None):
     """pr2_dispatch on torch tensors: the rows of x [T, d] sorted by expert into xs [T * k, d]."""
-    torch = _torch()
     T, d, adt, dev = _need_act(x)
-    k, N = _plan_shape(row_of_route, offsets, dev)
-    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
-    _need(xs, "xs", (T * k, d), adt, dev)
-    desc = make_desc(T, d, N, k, act=_act_code(x))
-    check(lib().pr2_dispatch(byref(desc), _ptr(x), _ptr(offsets), _ptr(row_of_route), _ptr(xs),
+    if offsets is None:
+        raise ValueError("offsets is required")
+    k, N, row, offsets = _plan(row_of_route, offsets, T, dev)
+    xs = _need(xs, "xs", (T * k, d), adt, dev)
+    check(lib().pr2_dispatch(_rows_desc(T, d, N, k, adt), x.data_ptr(), offsets, row, xs,
                              _stream(stream)))
 
 
 def dispatch_backward(dxs, row_of_route, dx, stream=None):
     """pr2_dispatch_backward on torch tensors: dx [T, d] = the sum of each token's rows of dxs."""
-    torch = _torch()
     T, d, adt, dev = _need_act(dx, "dx")
-    k, N = _plan_shape(row_of_route, None, dev)
-    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
-    _need(dxs, "dxs", (T * k, d), adt, dev)
-    desc = make_desc(T, d, N, k, act=_act_code(dx))
-    check(lib().pr2_dispatch_backward(byref(desc), _ptr(dxs), _ptr(row_of_route), _ptr(dx),
+    k, N, row, _ = _plan(row_of_route, None, T, dev)
+    dxs = _need(dxs, "dxs", (T * k, d), adt, dev)
+    check(lib().pr2_dispatch_backward(_rows_desc(T, d, N, k, adt), dxs, row, dx.data_ptr(),
                                       _stream(stream)))
 
 
@@ -845,12 +871,10 @@ def combine(o, row_of_route, gate, y, stream=None):
     """pr2_combine on torch tensors: y [T, d] = the rows of o [T * k, d] under ``gate`` [T, k]."""
     torch = _torch()
     T, d, adt, dev = _need_act(y, "y")
-    k, N = _plan_shape(row_of_route, None, dev)
-    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
-    _need(gate, "gate", (T, k), torch.float32, dev)
-    _need(o, "o", (T * k, d), adt, dev)
-    desc = make_desc(T, d, N, k, act=_act_code(y))
-    check(lib().pr2_combine(byref(desc), _ptr(o), _ptr(row_of_route), _ptr(gate), _ptr(y),
+    k, N, row, _ = _plan(row_of_route, None, T, dev)
+    gate = _need(gate, "gate", (T, k), torch.float32, dev)
+    o = _need(o, "o", (T * k, d), adt, dev)
+    check(lib().pr2_combine(_rows_desc(T, d, N, k, adt), o, row, gate, y.data_ptr(),
                             _stream(stream)))
 
 
@@ -858,40 +882,38 @@ def combine_backward(dy, o, offsets, row_of_route, gate, d_o, dgate, stream=None
     """pr2_combine_backward on torch tensors: d_o [T * k, d] (may be ``o``) and dgate [T, k]."""
     torch = _torch()
     T, d, adt, dev = _need_act(dy, "dy")
-    k, N = _plan_shape(row_of_route, offsets, dev)
-    _need(row_of_route, "row_of_route", (T, k), torch.int32, dev)
-    _need(gate, "gate", (T, k), torch.float32, dev)
-    _need(o, "o", (T * k, d), adt, dev)
-    _need(d_o, "d_o", (T * k, d), adt, dev)
-    _need(dgate, "dgate", (T, k), torch.float32, dev)
-    desc = make_desc(T, d, N, k, act=_act_code(dy))
-    check(lib().pr2_combine_backward(byref(desc), _ptr(dy), _ptr(o), _ptr(offsets),
-                                     _ptr(row_of_route), _ptr(gate), _ptr(d_o), _ptr(dgate),
-                                     _stream(stream)))
+    if offsets is None:
+        raise ValueError("offsets is required")
+    k, N, row, offsets = _plan(row_of_route, offsets, T, dev)
+    gate = _need(gate, "gate", (T, k), torch.float32, dev)
+    o = _need(o, "o", (T * k, d), adt, dev)
+    d_o = _need(d_o, "d_o", (T * k, d), adt, dev)
+    dgate = _need(dgate, "dgate", (T, k), torch.float32, dev)
+    check(lib().pr2_combine_backward(_rows_desc(T, d, N, k, adt), dy.data_ptr(), o, offsets, row,
+                                     gate, d_o, dgate, _stream(stream)))
 
 
 # ------------------------------------------------- activations kept in 8 bits --
 
 def _packed(q, scale, R, C, device):
     torch = _torch()
-    _need(q, "q", (R, C), torch.int8, device)
-    _need(scale, "scale", (R, -(-C // PACK_GROUP)), torch.uint8, device)
+    return (_need(q, "q", (R, C), torch.int8, device),
+            _need(scale, "scale", (R, -(-C // PACK_GROUP)), torch.uint8, device))
 
 
 def act_pack(x, q, scale, stream=None):
     """pr2_act_pack on torch tensors: x [R, C] to q int8 [R, C] and scale uint8
     [R, ceil(C / 32)]."""
-    R, C, _, dev = _need_act(x)
-    _packed(q, scale, R, C, dev)
-    check(lib().pr2_act_pack(R, C, _act_code(x), _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+    R, C, adt, dev = _need_act(x)
+    q, scale = _packed(q, scale, R, C, dev)
+    check(lib().pr2_act_pack(R, C, _ACT_CODES[adt], x.data_ptr(), q, scale, _stream(stream)))
 
 
 def act_unpack(q, scale, x, stream=None):
     """pr2_act_unpack on torch tensors: the values of (q, scale) into x [R, C]."""
-    R, C, _, dev = _need_act(x)
-    _packed(q, scale, R, C, dev)
-    check(lib().pr2_act_unpack(R, C, _act_code(x), _ptr(q), _ptr(scale), _ptr(x),
-                               _stream(stream)))
+    R, C, adt, dev = _need_act(x)
+    q, scale = _packed(q, scale, R, C, dev)
+    check(lib().pr2_act_unpack(R, C, _ACT_CODES[adt], q, scale, x.data_ptr(), _stream(stream)))
 
 
 def swiglu_pack(au, h, q, scale, stream=None):
@@ -900,9 +922,9 @@ def swiglu_pack(au, h, q, scale, stream=None):
     R, C, adt, dev = _need_act(au, "au")
     if C % 2:
         raise ValueError("au must hold a and u, [R, 2m]")
-    _need(h, "h", (R, C // 2), adt, dev)
-    _packed(q, scale, R, C, dev)
-    check(lib().pr2_swiglu_pack(R, C // 2, _act_code(au), _ptr(au), _ptr(h), _ptr(q), _ptr(scale),
+    h = _need(h, "h", (R, C // 2), adt, dev)
+    q, scale = _packed(q, scale, R, C, dev)
+    check(lib().pr2_swiglu_pack(R, C // 2, _ACT_CODES[adt], au.data_ptr(), h, q, scale,
                                 _stream(stream)))
 
 
@@ -910,11 +932,11 @@ def swiglu_backward_packed(q, scale, dh, d_au, h_out=None, stream=None):
     """pr2_swiglu_backward_packed on torch tensors: d_au [R, 2m] from the packed au and
     dh [R, m]; h_out [R, m] also receives silu(a) u."""
     R, m, adt, dev = _need_act(dh, "dh")
-    _packed(q, scale, R, 2 * m, dev)
-    _need(d_au, "d_au", (R, 2 * m), adt, dev)
-    _need(h_out, "h_out", (R, m), adt, dev, optional=True)
-    check(lib().pr2_swiglu_backward_packed(R, m, _act_code(dh), _ptr(q), _ptr(scale), _ptr(dh),
-                                           _ptr(d_au), _ptr(h_out), _stream(stream)))
+    q, scale = _packed(q, scale, R, 2 * m, dev)
+    d_au = _need(d_au, "d_au", (R, 2 * m), adt, dev)
+    h_out = _need(h_out, "h_out", (R, m), adt, dev, True)
+    check(lib().pr2_swiglu_backward_packed(R, m, _ACT_CODES[adt], q, scale, dh.data_ptr(), d_au,
+                                           h_out, _stream(stream)))
 
 
 def weight_grad_packed(dy, q, scale, dW, offsets=None, route_of_row=None, k=1, ws=None,
@@ -923,26 +945,25 @@ def weight_grad_packed(dy, q, scale, dW, offsets=None, route_of_row=None, k=1, w
     packed x [Rx, n_in]; ``offsets`` [N + 1] and ``route_of_row`` [R] (with the layer's ``k``)
     as dispatch_plan writes them."""
     torch = _torch()
-    R, n_out, _, dev = _need_act(dy, "dy")
+    R, n_out, adt, dev = _need_act(dy, "dy")
     if q.dim() != 2:
         raise ValueError("q must be 2-D [Rx, n_in]")
     Rx, n_in = q.shape
-    _packed(q, scale, Rx, n_in, dev)
+    q, scale = _packed(q, scale, Rx, n_in, dev)
     N = 1
     if offsets is not None:
         if offsets.dim() != 1 or offsets.shape[0] < 2:
             raise ValueError("offsets must be 1-D [N + 1]")
         N = offsets.shape[0] - 1
-        _need(offsets, "offsets", (N + 1,), torch.int32, dev)
-    _need(route_of_row, "route_of_row", (R,), torch.int32, dev, optional=True)
-    _need(dW, "dW", (N, n_out, n_in), torch.float32, dev)
-    _need_ws(ws, dev)
-    desc = WgradDesc(R, Rx, n_out, n_in, N, k, _act_code(dy))
+        offsets = _need(offsets, "offsets", (N + 1,), torch.int32, dev)
+    route_of_row = _need(route_of_row, "route_of_row", (R,), torch.int32, dev, True)
+    dW = _need(dW, "dW", (N, n_out, n_in), torch.float32, dev)
+    L, desc = lib(), byref(WgradDesc(R, Rx, n_out, n_in, N, k, _ACT_CODES[adt]))
+    ws = _need_ws(ws, dev)
     if ws is None:
-        ws = _new_ws(int(lib().pr2_weight_grad_workspace_bytes(byref(desc))), dev, stream)
-    check(lib().pr2_weight_grad_packed(byref(desc), _ptr(dy), _ptr(q), _ptr(scale), _ptr(offsets),
-                                       _ptr(route_of_row), _ptr(dW), _ptr(ws), ws.numel(),
-                                       _stream(stream)))
+        ws = _new_ws(L.pr2_weight_grad_workspace_bytes(desc), dev, stream)
+    check(L.pr2_weight_grad_packed(desc, dy.data_ptr(), q, scale, offsets, route_of_row, dW,
+                                   ws.data_ptr(), ws.numel(), _stream(stream)))
 
 
 # ------------------------------------------------------ measurement hooks --

@@ -1,7 +1,8 @@
 """Builds libpr2.so (HIP for gfx950) in-tree with hipcc.
 
 Each translation unit compiles to an object under ``_build/`` in parallel,
-then one shared library is linked next to this file.  Always recompiles.
+then one shared library is linked next to this file, and beside it the binding's
+compiled argument checks (``_args``, against the installed torch).  Always recompiles.
 """
 from __future__ import annotations
 
@@ -15,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpr2.so")
+ARGS = os.path.join(HERE, "_args.so")
 SOURCES = ["api.hip", "router.hip", "permute.hip", "gemm.hip", "tile.hip", "backward.hip",
            "predictor.hip", "noalloc.hip", "policy.hip", "dispatch.hip", "pack.hip", "wgrad.hip"]
 
@@ -34,6 +36,19 @@ def _run(cmd):
     return p.returncode, out
 
 
+def _args_command(out: str):
+    """The binding's argument checks: host code on the interpreter's and torch's C++ API."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-isystem", sysconfig.get_paths()["include"],
+            "-isystem", os.path.join(root, "include"), os.path.join(CSRC, "args.cpp"),
+            "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", out]
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     objs = []
@@ -42,6 +57,7 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(BUILD, src.replace(".hip", ".o"))
         objs.append(obj)
         cmds.append([HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
+    cmds.append(_args_command(ARGS + ".tmp"))
     with ThreadPoolExecutor(len(cmds)) as ex:
         results = list(ex.map(_run, cmds))
     for cmd, (rc, out) in zip(cmds, results):
@@ -49,7 +65,8 @@ def build(verbose: bool = False) -> str:
             if out.strip():
                 print(out, file=sys.stderr)
         if rc != 0:
-            raise RuntimeError("hipcc failed: " + " ".join(cmd))
+            raise RuntimeError("compilation failed: " + " ".join(cmd))
+    os.replace(ARGS + ".tmp", ARGS)
     tmp = LIB + ".tmp"
     rc, out = _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs])
     if rc != 0:

@@ -1,0 +1,99 @@
+"""The binding's compiled argument checks give the pointers, results and refusals of the
+Python ones that they stand in for."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+from paper_2606_00395_amd import binding as B
+
+pytestmark = pytest.mark.skipif(
+    not os.path.exists(os.path.join(B.HERE, "_args.so")), reason="_args.so not built")
+
+
+@pytest.fixture(scope="module")
+def plain():
+    """The binding outside its package, where no compiled module is found."""
+    spec = importlib.util.spec_from_file_location("plain_binding", B.__file__)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    m._torch()
+    B._torch()
+    assert m._need.__module__ == "plain_binding"
+    assert type(B._need).__name__ == "builtin_function_or_method"
+    return m
+
+
+def outcome(f, *args, **kw):
+    try:
+        return f(*args, **kw)
+    except Exception as e:
+        return type(e), str(e)
+
+
+X = torch.arange(12.0).reshape(3, 4)
+CPU, GPU = torch.device("cpu"), torch.device("cuda", 0)
+NEED = [
+    ((X, "x", (3, 4)), {}),
+    ((X, "x", (3, 4), torch.float32, CPU), {}),
+    ((X, "x", X.shape, torch.float32, CPU, True), {}),
+    ((X, "x", (3, 4), torch.float32, CPU), dict(optional=True)),
+    ((X, "x", (3, 4)), dict(dtype=torch.float32, device=CPU)),
+    ((X[1:], "x", (2, 4), None, CPU), {}),
+    ((torch.empty(0), "x", (0,), torch.float32, CPU), {}),
+    ((torch.tensor(1.0), "x", ()), {}),
+    ((torch.empty(4, 0, dtype=torch.int8), "x", (4, 0), torch.int8), {}),
+    # refused
+    ((X, "x", (4, 3)), {}),
+    ((X, "x", (3, 4, 1)), {}),
+    ((X, "x", (3, -1)), {}),
+    ((X, "x", (3, 1 << 70)), {}),
+    ((X, "x", (3, 4), torch.bfloat16), {}),
+    ((X, "x", (3, 4), torch.float32, GPU), {}),
+    ((X.t(), "x", (4, 3)), {}),
+    ((X[:, :2], "x", (3, 2)), {}),
+    ((X.numpy(), "x", (3, 4)), {}),
+    (([1.0], "x", (1,)), {}),
+    ((None, "x", (3, 4)), {}),
+    ((None, "x", (3, 4), None, None, False), {}),
+    # absent where it may be
+    ((None, "x", (3, 4), torch.float32, CPU, True), {}),
+    ((None, "x", (3, 4)), dict(optional=True)),
+]
+
+
+@pytest.mark.parametrize("args,kw", NEED)
+def test_need(plain, args, kw):
+    assert outcome(B._need, *args, **kw) == outcome(plain._need, *args, **kw)
+
+
+def test_need_returns_the_address(plain):
+    assert B._need(X[1:], "x", (2, 4), torch.float32, CPU) == X.data_ptr() + 16
+
+
+@pytest.mark.parametrize("args", [(), (X,), (X, "x")])
+def test_need_without_its_arguments(plain, args):
+    with pytest.raises(TypeError):
+        B._need(*args)
+    with pytest.raises(TypeError):
+        plain._need(*args)
+
+
+@pytest.mark.parametrize("x", [X, X.t(), X.to(torch.float16), X[0], X.to(torch.bfloat16),
+                               torch.empty(2, 3, dtype=torch.int8)])
+def test_need_act_refusals(plain, x):
+    kind, text = outcome(B._need_act, x, "dy")
+    assert issubclass(kind, (TypeError, ValueError)) and text
+    assert (kind, text) == outcome(plain._need_act, x, "dy")
+    assert outcome(B._need_act, x) == outcome(plain._need_act, x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_need_act(plain, dtype):
+    x = torch.empty((3, 5), dtype=dtype, device="cuda")
+    for m in (B, plain):
+        assert m._need_act(x, "x") == (3, 5, dtype, x.device)
+        assert m._need(x, "x", (3, 5), dtype, x.device) == x.data_ptr()
+        assert outcome(m._need, x, "x", (3, 5), dtype, CPU)[0] is ValueError
