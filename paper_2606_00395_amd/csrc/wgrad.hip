@@ -346,15 +346,15 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         else if (n == 1) wait_vmcnt<kCopies>();
         else wait_vmcnt<0>();
     };
-    // The first steps, in two parts: into registers and stages 0 and 1, which the stores of
-    // the tile before leave alone, and the rest.  Then dy's steps 0..3 are copied, the
-    // packed steps 0 and 1 written, 2 and 3 in flight.
+    // The first steps, in two parts, with the stores of the tile before in between: dy's steps
+    // 0..3 into the stages, the packed steps 0 and 1 into registers; then these are written and
+    // 2 and 3 fetched.
     auto fetch = [&](int ct) __attribute__((always_inline)) {
         if (PACKS) {
             load_packed(C0{}, ct, 0);
             load_packed(C1{}, ct, 1);
         } else {
-            for (int h = 0; h < min(nh, 2); ++h) {
+            for (int h = 0; h < min(nh, kStages); ++h) {
 #pragma unroll
                 for (int i = 0; i < kCopies; ++i) copy_dy(h, i);
             }
@@ -371,10 +371,6 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
             load_packed(C0{}, ct, 2);
             load_packed(C1{}, ct, 3);
         } else {
-            for (int h = 2; h < min(nh, kStages); ++h) {
-#pragma unroll
-                for (int i = 0; i < kCopies; ++i) copy_dy(h, i);
-            }
             wait_steps(min(nh, kStages) - 1);
         }
         barrier();
@@ -419,7 +415,7 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < MI; ++i)
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[S][i], fb[S][j], acc[i][j], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                     if (j == 0) {
                         fa[S ^ 1][0] = tr_frag(base + a_pos[0]);
@@ -467,59 +463,34 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
             }
             if (h < nh) step(C0{}, h);
         }
-        // (no wavefront reads a stage any more: all hold the last step's fragments)
-        barrier();
+        barrier();          // (no wavefront reads a stage any more: all hold the last step's fragments)
         if (ct + 1 < ct1 && klen > 0 && klen <= kRowsHeld) fetch(ct + 1);
 
-        // Lane l holds output row l % 32 of each 32-row block and columns 8 (v / 4) + 4 (l / 32)
-        // + v % 4 of each 32-column block.  The rows are staged through this wavefront's share of
-        // stages 2 and 3, 32 rows of 64 columns at a time, and stored 16 bytes per lane along
-        // whole row segments: gradients, which are not read again here, past the caches (at
-        // 128 experts 1057 us against 1082), partial sums not.
+        // Lane l holds column l % 32 of each 32-column block and rows 8 (v / 4) + 4 (l / 32) + v % 4
+        // of each 32-row block: a store writes whole 128-byte pieces of two rows, straight from
+        // the accumulators (128 experts of 1536 x 2048: 1002 -> 973 us against rows of 256 bytes
+        // put together in LDS; past the caches 976).
         if (active) {
-            float* const out = (a.S > 1 ? a.part : a.dW) + ct * BN + wc * WN +
-                ((int64_t)(slice * a.N + expert) * a.n_out + rt * BM + wr * WM) * a.n_in;
-            constexpr int RB = 64 * 4, NCH = RB / 16;
-            static_assert(kMfmaThreads / 64 * 32 * RB <= 2 * kStageB, "staged rows");
-            unsigned char* sw = lds + 2 * kStageB + wave * (32 * RB);
-            const int rows_left = a.n_out - rt * BM - wr * WM;
-            const int cols_left = a.n_in - ct * BN - wc * WN;
+            const int rows_left = a.n_out - rt * BM - wr * WM - 4 * hi;
+            const int cols_left = a.n_in - ct * BN - wc * WN - (lane & 31);
+            float* const out = (a.S > 1 ? a.part : a.dW) + ct * BN + wc * WN + (lane & 31) +
+                ((int64_t)(slice * a.N + expert) * a.n_out + rt * BM + wr * WM + 4 * hi) * a.n_in;
+            auto store = [&](auto whole_) __attribute__((always_inline)) {
+                constexpr bool W = decltype(whole_)::value;
 #pragma unroll
-            for (int i = 0; i < MI; ++i)
+                for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int jh = 0; jh < NJ / 2; ++jh) {
-                    const int row = lane & 31;
+                    for (int v = 0; v < 16; ++v) {
+                        const int row = i * 32 + 8 * (v / 4) + v % 4;
+                        float* to = out + (int64_t)row * a.n_in;
 #pragma unroll
-                    for (int j = 0; j < 2; ++j)
-#pragma unroll
-                        for (int a4 = 0; a4 < 4; ++a4) {
-                            const int chunk = j * 8 + 2 * a4 + hi;
-                            const f32x16& v = acc[i][2 * jh + j];
-                            *(f32x4*)(sw + row * RB + ((chunk ^ (row & (NCH - 1))) << 4)) =
-                                f32x4{v[4 * a4], v[4 * a4 + 1], v[4 * a4 + 2], v[4 * a4 + 3]};
-                        }
-                    __builtin_amdgcn_s_waitcnt(0xc07f);
-                    __builtin_amdgcn_wave_barrier();
-                    int row2 = lane / NCH;
-                    const int ch = lane % NCH;
-                    float* to = out + (int64_t)(i * 32 + row2) * a.n_in + jh * 64 + ch * 4;
-                    const int rows = jh * 64 + ch * 4 < cols_left ? min(32, rows_left - i * 32) : 0;
-#pragma unroll
-                    for (int p = 0; p < 32 / (64 / NCH); ++p) {
-                        if (row2 < rows) {
-                            const u32x4 w = *(const u32x4*)(sw + row2 * RB + ((ch ^ (row2 & (NCH - 1))) << 4));
-                            if (a.S > 1) *(u32x4*)to = w;
-                            else __builtin_nontemporal_store(w, (u32x4*)to);
-                        }
-                        row2 += 64 / NCH;
-                        to += (int64_t)(64 / NCH) * a.n_in;
+                        for (int j = 0; j < NJ; ++j)
+                            if (W || (row < rows_left && j * 32 < cols_left)) to[j * 32] = acc[i][j][v];
                     }
-                    // the next block overwrites the region
-                    __builtin_amdgcn_s_waitcnt(0xc07f);
-                    __builtin_amdgcn_wave_barrier();
-                }
+            };
+            if (rt * BM + wr * WM + WM <= a.n_out && ct * BN + wc * WN + WN <= a.n_in) store(std::true_type{});
+            else store(std::false_type{});
         }
-        barrier();                  // stages 2 and 3 are free again
     }
 }
 
