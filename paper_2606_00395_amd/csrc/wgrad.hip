@@ -51,41 +51,42 @@ __device__ __forceinline__ int source_row(const WgradArgs& a, int r) {
 
 // Any type, width and row count: 64 x 64 outputs per workgroup, four wavefronts of 32 x 32 on
 // v_mfma_f32_32x32x2_f32 (fp32 products and sums), 32 rows of both operands staged in LDS as
-// fp32 at a time, the next 32 fetched meanwhile.  Small layers are bound by the latency of
-// that chain (15 us at 1226 rows, 7 experts of 135 x 203; one FMA per lane at a time took 24),
-// large ones by the fp32 MFMA and the LDS (111 TFLOP/s at 4096 x 4096 over 32768 rows, where
-// the library's fp32 product reaches 154; with FMAs 74).
+// fp32 at a time, the next 32 in flight meanwhile.  Small layers are bound by the latency of
+// that chain (with the packing 15.5 us at 1226 rows, 7 experts of 135 x 203; 17.7 where the
+// operands were opened on arrival), large ones by the fp32 MFMA and the LDS (112 TFLOP/s at
+// 4096 x 4096 over 32768 rows, where the library's fp32 product reaches 154).
 constexpr int kTile = 64;
 constexpr int kStep = 32;
 constexpr int kTilePitch = kTile + 32;      // the two halves of a wavefront read other banks
 
-// 8 columns of a row, the first n of them inside the matrix
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
+// 8 elements of a row from column c on, their bits as they lie there; those past the row's n
+// stand in for others of it (WHOLE: there are none)
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void load8(const T* row, int c, int n, u32x4 (&w)[8 / Chunk<T>::E]) {
     constexpr int E = Chunk<T>::E;
-    if (n >= 8) {
-        u32x4 w[8 / E];
+    if (WHOLE) {
 #pragma unroll
-        for (int i = 0; i < 8 / E; ++i) w[i] = load16<false>(p + i * E);
+        for (int i = 0; i < 8 / E; ++i) w[i] = load16<false>(row + c + i * E);
+        return;
+    }
 #pragma unroll
-        for (int i = 0; i < 8 / E; ++i) Chunk<T>::open(w[i], v + i * E);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? Act<T>::to_f32(p[i]) : 0.0f;
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t b = __builtin_bit_cast(typename Chunk<T>::Bits, row[min(c + i, n - 1)]);
+        if (E == 4) w[i / 4][i % 4] = b;
+        else w[0][i / 2] = i & 1 ? w[0][i / 2] | b << 16 : b;
     }
 }
 
-__device__ __forceinline__ void load8_packed(const int8_t* p, int n, float step, float (&v)[8]) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    typedef u32x2 u32x2_byte __attribute__((aligned(1)));
+// the same of a packed row, 8 bytes (shifted into place: the ones past the row's end are 0)
+__device__ __forceinline__ uint64_t load8_packed(const int8_t* row, int c, int n) {
+    typedef uint64_t u64_byte __attribute__((aligned(1)));
     if (n >= 8) {
-        const u32x2 w = *(const u32x2_byte*)p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)((int)(w[i / 4] << (24 - 8 * (i % 4))) >> 24) * step;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] * step : 0.0f;
+        const int at = min(c, n - 8);
+        return *(const u64_byte*)(row + at) >> min(8 * (c - at), 63);
     }
+    uint64_t w = 0;
+    for (int i = 0; i < n - c; ++i) w |= (uint64_t)(uint8_t)row[c + i] << (8 * i);
+    return w;
 }
 
 template <typename T>
@@ -100,26 +101,43 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
     expert_rows(a, e, &first, &last);
     slice_rows(a, blockIdx.z, &first, &last);
     const int sr = tid / 8, sc = (tid % 8) * 8;         // row and columns this thread stages
-    const int no = a.n_out - o0 - sc, nc = a.n_in - c0 - sc;
     f32x16 acc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
-    float va[8], vb[8];
+    // A step's operands as they come: nothing is computed from them before the products of the
+    // step before.  Columns past the matrix hold anything, they reach only outputs that are
+    // not stored.
+    constexpr int E = Chunk<T>::E;
+    const bool whole = o0 + kTile <= a.n_out;
+    u32x4 wa[8 / E];
+    uint64_t wb;
+    uint32_t byte;
+    bool on;
     auto fetch = [&](int r0) __attribute__((always_inline)) {
-        const int r = r0 + sr;
-        const int x = r < last ? source_row(a, r) : -1;
-        // a row without a source is zeros in both operands: nothing of it multiplies
-#pragma unroll
-        for (int i = 0; i < 8; ++i) va[i] = vb[i] = 0.0f;
-        if (x < 0) return;
-        if (no > 0) load8((const T*)a.dy + (int64_t)r * a.n_out + o0 + sc, no, va);
-        if (nc > 0)
-            load8_packed(a.q + (int64_t)x * a.n_in + c0 + sc, nc,
-                         __uint_as_float((uint32_t)a.scale[(int64_t)x * a.groups + (c0 + sc) / 32] << 23), vb);
+        const int r = min(r0 + sr, last - 1);
+        const int x = source_row(a, r);
+        on = r0 + sr < last && x >= 0;
+        const int64_t xr = max(x, 0);
+        const T* row = (const T*)a.dy + (int64_t)r * a.n_out;
+        if (whole) load8<T, true>(row, o0 + sc, a.n_out, wa);
+        else load8<T, false>(row, o0 + sc, a.n_out, wa);
+        wb = load8_packed(a.q + xr * a.n_in, c0 + sc, a.n_in);
+        byte = a.scale[xr * a.groups + min(c0 + sc, a.n_in - 1) / 32];
     };
     const int ao = 32 * (wave >> 1) + (lane & 31), bo = 32 * (wave & 1) + (lane & 31), k2 = lane >> 5;
+    if (a.Rx == 0) last = first;        // no row has a source
     if (first < last) fetch(first);
     for (int r0 = first; r0 < last; r0 += kStep) {
+        // a row without a source is zeros in both operands: nothing of it multiplies
+        float va[8], vb[8];
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) Chunk<T>::open(wa[i], va + i * E);
+        const float step = on ? __uint_as_float(byte << 23) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            va[i] = on ? va[i] : 0.0f;
+            vb[i] = (float)(int8_t)(wb >> (8 * i)) * step;
+        }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
