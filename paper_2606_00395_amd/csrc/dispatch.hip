@@ -8,9 +8,10 @@
 // Every one is bound by HBM and goes token by token: the token's row is read (or written)
 // once and its k sorted rows, each contiguous, are written or read as whole segments; no
 // row is read for a route that was dropped.  The sums over the slots run in slot order in
-// fp32, so no atomics and the same bits every time.  16384 tokens of 2048 bf16, k 8:
-// dispatch 90 us (6.7 TB/s, mostly writes), combine 137 (4.4, mostly reads), combine backward
-// 200 (5.7), dispatch backward 128 (4.7); a large copy reaches 5.2.
+// fp32, so no atomics and the same bits every time.  16384 tokens of 2048 bf16, k 8: dispatch
+// 119 us (5.1 TB/s), combine 110 (5.5), combine backward 222 (5.2), dispatch backward 106 (5.7);
+// a large copy reaches 5.2.  A token's row indexes are read together, before its pieces go out
+// (dispatch and combine with their plan 244.6 -> 240.5 us).
 #include "chunk.h"
 
 namespace pr2 {
@@ -38,13 +39,14 @@ struct RowArgs {
     int d, k, N;
 };
 
-// sorted rows that belong to no route are zeros; workgroup b of `wgs` takes every wgs-th
+// sorted rows from `filled` on belong to no route: zeros; workgroup b of `wgs` takes every wgs-th
 template <typename T, bool NT>
-__device__ __forceinline__ void zero_rest(const RowArgs& a, int lanes, int lane, int64_t b, int64_t wgs) {
+__device__ __forceinline__ void zero_rest(const RowArgs& a, int filled, int lanes, int lane, int64_t b,
+                                          int64_t wgs) {
     const int full = a.d / Chunk<T>::E, rem = a.d % Chunk<T>::E;
     const int n = full + (rem != 0);
     const float v[Chunk<T>::E] = {};
-    for (int64_t r = max(a.offsets[a.N], 0) + b; r < a.Tk; r += wgs)
+    for (int64_t r = max(filled, 0) + b; r < a.Tk; r += wgs)
         for (int c = lane; c < n; c += lanes)
             store_chunk<T, NT>((T*)a.rows_out + r * a.d, c, full, rem, v);
 }
@@ -57,18 +59,23 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(RowArgs a) {
     const int y = __builtin_amdgcn_readfirstlane(threadIdx.y);
     const int64_t b = (int64_t)blockIdx.x * blockDim.y + y;
     const int64_t wgs = (int64_t)gridDim.x * blockDim.y;
+    const int filled = a.offsets[a.N];
     for (int64_t t = b; t < a.T; t += wgs) {
         const T* x = (const T*)a.tok + t * a.d;
         for (int c = threadIdx.x; c < n; c += blockDim.x) {
             const u32x4 w = load_chunk<T, true>(x, c, full, rem);
-            for (int s = 0; s < a.k; ++s) {
-                const int r = a.row[t * a.k + s];
-                if ((uint32_t)r < (uint64_t)a.Tk)
-                    copy_chunk<T, NT>((T*)a.rows_out + (int64_t)r * a.d, c, full, rem, w);
+            for (int s0 = 0; s0 < a.k; s0 += kSlots) {
+                int r[kSlots];
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j) r[j] = s0 + j < a.k ? a.row[t * a.k + s0 + j] : -1;
+#pragma unroll
+                for (int j = 0; j < kSlots; ++j)
+                    if ((uint32_t)r[j] < (uint64_t)a.Tk)
+                        copy_chunk<T, NT>((T*)a.rows_out + (int64_t)r[j] * a.d, c, full, rem, w);
             }
         }
     }
-    zero_rest<T, NT>(a, blockDim.x, threadIdx.x, b, wgs);
+    zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
 }
 
 // y[t] = sum_s [gate] row: combine (GATED) and the gradient of dispatch.  (Two tokens at a
@@ -145,6 +152,7 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(RowArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) + y * waves;
     const int64_t b = (int64_t)blockIdx.x * blockDim.y + y;
     const int64_t wgs = (int64_t)gridDim.x * blockDim.y;
+    const int filled = a.offsets[a.N];
     const int64_t turns = (a.T + wgs - 1) / wgs;        // the same for all: barriers inside
     for (int64_t turn = 0; turn < turns; ++turn) {
         const int64_t t = turn * wgs + b;
@@ -199,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(RowArgs a) {
             }
         }
     }
-    zero_rest<T, NT>(a, blockDim.x, threadIdx.x, b, wgs);
+    zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
 }
 
 // ------------------------------------------------------------------ host ----

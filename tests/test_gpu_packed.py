@@ -361,3 +361,22 @@ def test_refusals_of_the_binding():
         B.weight_grad_packed(x, q, e, torch.zeros((2, 64, 64), device="cuda"))
     with pytest.raises(B.Pr2Error, match="R = 8"):
         B.weight_grad_packed(torch.zeros((8, 4), device="cuda"), q, e, torch.zeros((1, 4, 64), device="cuda"))
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n_out,n_in", [(3, 5), (63, 7), (65, 8), (9, 9), (1, 15), (71, 33), (8, 66), (130, 71)])
+def test_weight_gradients_at_the_edges_of_narrow_tiles(n_out, n_in, bf16):
+    """Rows shorter than a thread's piece, pieces that end outside the row, dropped routes and
+    rows past the last expert's."""
+    import torch
+    T, N, k = 90, 3, 2
+    g = np.random.default_rng([n_out, n_in])
+    idx = np.sort(np.stack([g.choice(N, k, replace=False) for _ in range(T)]), 1)
+    idx[g.random((T, k)) < 0.2] = -1
+    from paper_2606_00395_amd import binding as B
+    i32 = dict(dtype=torch.int32, device="cuda")
+    offsets, row, route = torch.empty(N + 1, **i32), torch.empty((T, k), **i32), torch.empty(T * k, **i32)
+    B.dispatch_plan(torch.from_numpy(idx.astype(np.int32)).cuda(), N, offsets, row, route)
+    assert int(offsets[N]) < T * k
+    check_wgrad(act(g.standard_normal((T * k, n_out)), bf16), act(g.standard_normal((T, n_in)), bf16),
+                offsets, route, k, N)
