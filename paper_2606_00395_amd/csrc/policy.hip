@@ -9,7 +9,7 @@
 // Bound by HBM: V elements read per row, and V written where the gradient is wanted;
 // two exponentials per element (a quarter-rate instruction each) come next.  Loss and gradient
 // of 4096 x 151936 bf16 logits take 484 us, 5.15 TB/s (a large copy reaches 5.2); of 517 x
-// 50257 fp32 in two calls 58 us, 5.3 TB/s; log-probabilities of 8 rows 12 us, two launches.
+// 50257 fp32 in two calls 59 us, 5.3 TB/s; log-probabilities of 8 rows 10 us, two launches.
 #include <type_traits>
 
 #include "chunk.h"

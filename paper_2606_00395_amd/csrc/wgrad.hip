@@ -148,19 +148,17 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         if (r0 + kStep < last) fetch(r0 + kStep);
 #pragma unroll
         for (int k = 0; k < kStep; k += 2)
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(B[(k + k2) * kTilePitch + bo], A[(k + k2) * kTilePitch + ao],
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(A[(k + k2) * kTilePitch + ao], B[(k + k2) * kTilePitch + bo],
                                                        acc, 0, 0, 0);
     }
-    // lane l holds output row l % 32 and columns 8 (v / 4) + 4 (l / 32) + v % 4
-    const int o = o0 + ao;
-    if (o >= a.n_out) return;
-    float* to = (a.S > 1 ? a.part : a.dW) +
-        (((int64_t)blockIdx.z * a.N + e) * a.n_out + o) * a.n_in;
+    // lane l holds column l % 32 and rows 8 (v / 4) + 4 (l / 32) + v % 4
+    const int c = c0 + bo;
+    if (c >= a.n_in) return;
+    const int o = o0 + 32 * (wave >> 1) + 4 * k2;
+    float* to = (a.S > 1 ? a.part : a.dW) + (((int64_t)blockIdx.z * a.N + e) * a.n_out + o) * a.n_in + c;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const int c = c0 + 32 * (wave & 1) + 8 * (v / 4) + 4 * k2 + v % 4;
-        if (c < a.n_in) to[c] = acc[v];
-    }
+    for (int v = 0; v < 16; ++v)
+        if (o + 8 * (v / 4) + v % 4 < a.n_out) to[(int64_t)(8 * (v / 4) + v % 4) * a.n_in] = acc[v];
 }
 
 // bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs at a time, eight
@@ -489,25 +487,35 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         // the accumulators (128 experts of 1536 x 2048: 1002 -> 973 us against rows of 256 bytes
         // put together in LDS; past the caches 976).
         if (active) {
-            const int rows_left = a.n_out - rt * BM - wr * WM - 4 * hi;
-            const int cols_left = a.n_in - ct * BN - wc * WN - (lane & 31);
+            const int rows_left = a.n_out - rt * BM - wr * WM;      // multiples of 8 and 16
+            const int cols_left = a.n_in - ct * BN - wc * WN;
             float* const out = (a.S > 1 ? a.part : a.dW) + ct * BN + wc * WN + (lane & 31) +
                 ((int64_t)(slice * a.N + expert) * a.n_out + rt * BM + wr * WM + 4 * hi) * a.n_in;
-            auto store = [&](auto whole_) __attribute__((always_inline)) {
-                constexpr bool W = decltype(whole_)::value;
+            if (rows_left >= WM && cols_left >= WN) {
 #pragma unroll
                 for (int i = 0; i < MI; ++i)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int row = i * 32 + 8 * (v / 4) + v % 4;
-                        float* to = out + (int64_t)row * a.n_in;
+                        float* to = out + (int64_t)(i * 32 + 8 * (v / 4) + v % 4) * a.n_in;
 #pragma unroll
-                        for (int j = 0; j < NJ; ++j)
-                            if (W || (row < rows_left && j * 32 < cols_left)) to[j * 32] = acc[i][j][v];
+                        for (int j = 0; j < NJ; ++j) to[j * 32] = acc[i][j][v];
                     }
-            };
-            if (rt * BM + wr * WM + WM <= a.n_out && ct * BN + wc * WN + WN <= a.n_in) store(std::true_type{});
-            else store(std::false_type{});
+            } else {
+                // (one condition per lane and column block, one for all lanes per 8 rows)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) {
+                    if (j * 32 + (lane & 31) >= cols_left) continue;
+#pragma unroll
+                    for (int i = 0; i < MI; ++i)
+#pragma unroll
+                        for (int v0 = 0; v0 < 16; v0 += 4) {
+                            if (i * 32 + 2 * v0 >= rows_left) continue;
+#pragma unroll
+                            for (int v = v0; v < v0 + 4; ++v)
+                                out[(int64_t)(i * 32 + 2 * v0 + v - v0) * a.n_in + j * 32] = acc[i][j][v];
+                        }
+                }
+            }
         }
     }
 }
