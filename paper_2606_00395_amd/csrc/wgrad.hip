@@ -4,6 +4,7 @@
 //
 // A packed value is an int8 times a power of two, exact in bf16 and fp32, so nothing is
 // rounded on the way into the products.
+#include <algorithm>
 #include <type_traits>
 
 #include "chunk.h"
@@ -25,6 +26,7 @@ struct WgradArgs {
     float* part;                // [S, N, n_out, n_in] partial sums of S > 1 slices of the rows
     int S;
     int G;                      // 256 x 256 tiles: column tiles per workgroup
+    bool split;                 // each expert's tiles on all XCDs
 };
 
 // rows of expert e, clamped to the R that there are
@@ -219,26 +221,26 @@ __device__ __forceinline__ u32x4 open_packed(uint32_t q0, uint32_t q1, float ste
 template <bool PACKS>
 __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* lds, uint32_t* src,
                                             int* s_bad) {
-    // Work items (expert, slice, row tile, group of column tiles); experts are dealt to the
-    // XCDs round-robin in decreasing row count and an expert's items run on one XCD, whose L2
-    // then holds its rows.  One weight's items are dealt to the XCDs in contiguous ranges.
+    // Work items (expert, slice, row tile, group of column tiles), experts in decreasing row
+    // count.  Many experts are dealt to the XCDs round-robin and an expert's items run on one
+    // XCD, whose L2 then holds its rows; of few experts (SPLIT) each XCD takes an eighth of each
+    // one's items, a contiguous range, every expert's ranges beginning at another XCD.
     const int nct = (a.n_in + BN - 1) / BN;
     const int ngr = (nct + a.G - 1) / a.G;
     const int nrt = (a.n_out + BM - 1) / BM;
     const int per_e = nrt * ngr * a.S;
-    int expert = 0, item;
-    if (a.order) {
-        const int xcd = blockIdx.x % kNumXcd;
-        const int local = blockIdx.x / kNumXcd;
-        const int slot = xcd + kNumXcd * (local / per_e);
-        if (slot >= a.N) return;
-        expert = __builtin_amdgcn_readfirstlane(a.order[slot]);
-        item = local % per_e;
-    } else {
+    const int xcd = blockIdx.x % kNumXcd, local = blockIdx.x / kNumXcd;
+    int slot, item;
+    if (a.split) {
         const int each = (per_e + kNumXcd - 1) / kNumXcd;
-        item = (blockIdx.x % kNumXcd) * each + blockIdx.x / kNumXcd;
-        if (item >= per_e) return;
+        slot = local / each;
+        item = (xcd + slot) % kNumXcd * each + local % each;
+    } else {
+        slot = xcd + kNumXcd * (local / per_e);
+        item = local % per_e;
     }
+    if (slot >= a.N || item >= per_e) return;
+    const int expert = __builtin_amdgcn_readfirstlane(a.order ? a.order[slot] : slot);
     const int slice = item / (nrt * ngr);
     const int rt = item % (nrt * ngr) / ngr;
     const int ct0 = item % ngr * a.G;
@@ -535,6 +537,7 @@ __global__ void __launch_bounds__(256) wgrad_join_kernel(const float* part, int6
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i + 4 <= n) {
         f32x4 v = *(const f32x4_any*)(part + i);
+#pragma unroll 8
         for (int s = 1; s < S; ++s) v += *(const f32x4_any*)(part + s * n + i);
         *(f32x4*)(dW + i) = v;
     } else {
@@ -580,23 +583,43 @@ int64_t wgrad_tile_count(const pr2_wgrad_desc& d, int tile) {
     return ceil_div(d.n_out, tile) * ceil_div(d.n_in, tile) * d.N;
 }
 
-// Slices of the rows: where the output tiles leave the chip idle, as many as fill it once (one
-// 256 x 256 tile per CU, or four of 64 x 64), each with enough rows to pay for a tile's start,
-// its stores and the join.
+// Slices of the rows: where the output tiles leave the chip idle, as many as are expected to
+// take the least time, up to what fills it once (one 256 x 256 tile per CU, or four of 64 x 64).
+// More slices take fewer steps of 32 rows each, but write and read partial sums and need the
+// join.  In us, as measured: a step of a chip full of tiles 0.9 and 1.2, the join's launch 6, its
+// traffic and the slices' writes at 6.5 TB/s.  Against a fixed 256 and 128 rows a slice at
+// least, with the packing: 700 rows of 2048 x 2048 outputs 33.0 -> 30.3, 32768 of 64 x 128
+// 48.6 -> 26.1, 8192 of 512 x 512 35.7 -> 31.0, 20 fp32 experts of 33 x 50 25.9 -> 13.6.
 constexpr int kCus = 256;
+constexpr int kMaxSlices = 64;
 int wgrad_slices(const pr2_wgrad_desc& d) {
     const bool big = mfma_ok(d);
-    const int64_t fill = big ? kCus : 4 * kCus;
-    int64_t s = fill / wgrad_tile_count(d, big ? BM : kTile);
-    const int64_t most = d.R / d.N / (big ? 256 : 128);
-    if (s > most) s = most;
-    return s < 1 ? 1 : (int)s;
+    const int64_t tiles = wgrad_tile_count(d, big ? BM : kTile);
+    const int64_t rows = d.R / d.N;
+    const int64_t most = std::min<int64_t>({(big ? kCus : 4 * kCus) / tiles, ceil_div(rows, kBK), kMaxSlices});
+    const float step = big ? 0.9f : 1.2f;
+    const float part = 2.0f * sizeof(float) * (float)((int64_t)d.N * d.n_out * d.n_in) / 6.5e6f;
+    int best = 1;
+    float least = step * (float)ceil_div(rows, kBK);
+    for (int s = 2; s <= most; ++s) {
+        const float t = step * (float)ceil_div(rows, (int64_t)s * kBK) + 6.0f + (float)s * part;
+        if (t < least) {
+            least = t;
+            best = s;
+        }
+    }
+    return best;
 }
 
 // Column tiles per workgroup: two where that leaves each CU eight workgroups.
 int wgrad_group(const pr2_wgrad_desc& d) {
     return wgrad_tile_count(d, BM) >= 16 * kCus ? 2 : 1;
 }
+
+// Experts from which on one runs on one XCD: 2, 4, 9, 25 and 33 of them took 53, 135, 107, 174 and
+// 400 us that way and 30, 80, 79, 154 and 366 on all XCDs, 64 and 128 took 705 and 975 against 737
+// and 1025 (1536 x 2048 outputs, 64: 2816, 2: 2288 x 1376).
+constexpr int kManyExperts = 64;
 
 struct WgradWs {
     int* order;
@@ -622,12 +645,12 @@ hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, 
     if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
         a.G = wgrad_group(d);
         const int64_t items = ceil_div(d.n_out, BM) * ceil_div(ceil_div(d.n_in, BN), a.G) * a.S;
-        int64_t grid = ceil_div(items, kNumXcd) * kNumXcd;
+        a.split = d.N < kManyExperts;
+        const int64_t grid = kNumXcd * (a.split ? ceil_div(items, kNumXcd) * d.N : items * ceil_div(d.N, kNumXcd));
         if (d.N > 1) {
             e = launch_expert_order(a.offsets, d.N, w.order, st);
             if (e != hipSuccess) return e;
             a.order = w.order;
-            grid = items * ceil_div(d.N, kNumXcd) * kNumXcd;
         }
         LaunchScope scope("wgrad_mfma", st);
         hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
@@ -691,7 +714,7 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
     drop_split_records(ws, ws_bytes);
     const hipStream_t st = (hipStream_t)stream;
     WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
-                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1};
+                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1, false};
     const hipError_t e = launch_wgrad(d, a, wgrad_ws(d, ws), st);
     if (e != hipSuccess) return hip_fail(e, "weight_grad_packed launch");
     return ok();

@@ -380,3 +380,18 @@ def test_weight_gradients_at_the_edges_of_narrow_tiles(n_out, n_in, bf16):
     assert int(offsets[N]) < T * k
     check_wgrad(act(g.standard_normal((T * k, n_out)), bf16), act(g.standard_normal((T, n_in)), bf16),
                 offsets, route, k, N)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,n_out,n_in,N", [(20000, 8, 16, 1), (9973, 24, 48, 1), (6001, 40, 32, 5), (900, 520, 272, 2),
+                                            (300, 264, 512, 9)])
+def test_weight_gradients_in_many_slices_and_of_few_experts(R, n_out, n_in, N, bf16):
+    """Small outputs over many rows, the rows of an expert in up to 64 slices (some empty where
+    another expert has most of the rows), and experts whose tiles go to all XCDs."""
+    import torch
+    g = np.random.default_rng([R, n_out, N])
+    offsets = None
+    if N > 1:
+        cuts = np.sort(g.integers(0, R // 3, N - 1))        # the last one has most
+        offsets = torch.from_numpy(np.concatenate([[0], cuts, [R]]).astype(np.int32)).cuda()
+    check_wgrad(act(g.standard_normal((R, n_out)), bf16), act(g.standard_normal((R, n_in)), bf16), offsets, N=N)
