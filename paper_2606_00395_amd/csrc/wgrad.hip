@@ -22,7 +22,7 @@ struct WgradArgs {
     int64_t R, Rx;
     int n_out, n_in, N, k;
     int groups;
-    const int* order;           // [N] experts by decreasing row count; null with one weight
+    const int* order;           // [N] experts by decreasing row count; null: as they come
     float* part;                // [S, N, n_out, n_in] partial sums of S > 1 slices of the rows
     int S;
     int G;                      // 256 x 256 tiles: column tiles per workgroup
@@ -226,10 +226,10 @@ __device__ __forceinline__ u32x4 open_packed(uint32_t q0, uint32_t q1, float ste
 template <bool PACKS>
 __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* lds, uint32_t* src,
                                             int* s_bad) {
-    // Work items (expert, slice, row tile, group of column tiles), experts in decreasing row
-    // count.  Many experts are dealt to the XCDs round-robin and an expert's items run on one
-    // XCD, whose L2 then holds its rows; of few experts (SPLIT) each XCD takes an eighth of each
-    // one's items, a contiguous range, every expert's ranges beginning at another XCD.
+    // Work items (expert, slice, row tile, group of column tiles).  Many experts are dealt to the
+    // XCDs round-robin and an expert's items run on one XCD, whose L2 then holds its rows; of
+    // few experts (split) each XCD takes an eighth of each one's items, a contiguous range,
+    // every expert's ranges beginning at another XCD.
     const int nct = (a.n_in + BN - 1) / BN;
     const int ngr = (nct + a.G - 1) / a.G;
     const int nrt = (a.n_out + BM - 1) / BM;
@@ -626,6 +626,13 @@ int wgrad_group(const pr2_wgrad_desc& d) {
 // and 1025 (1536 x 2048 outputs, 64: 2816, 2: 2288 x 1376).
 constexpr int kManyExperts = 64;
 
+// Whether longest experts first is worth its launch of 5 us: not where all work items run at
+// once, and not where the longest expert could take little longer than that (2 experts of 2288 x
+// 1376 over 89 rows 16.3 -> 14.2 us without, 25 of 736 x 1600 over 312 32.7 -> 30.2).
+bool order_pays(const pr2_wgrad_desc& d, int64_t items) {
+    return d.N > 1 && d.N * items > kCus && d.R > 512;
+}
+
 struct WgradWs {
     int* order;
     float* part;
@@ -652,7 +659,7 @@ hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, 
         const int64_t items = ceil_div(d.n_out, BM) * ceil_div(ceil_div(d.n_in, BN), a.G) * a.S;
         a.split = d.N < kManyExperts;
         const int64_t grid = kNumXcd * (a.split ? ceil_div(items, kNumXcd) * d.N : items * ceil_div(d.N, kNumXcd));
-        if (d.N > 1) {
+        if (order_pays(d, items)) {
             e = launch_expert_order(a.offsets, d.N, w.order, st);
             if (e != hipSuccess) return e;
             a.order = w.order;
