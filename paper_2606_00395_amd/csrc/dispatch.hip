@@ -12,6 +12,8 @@
 // 119 us (5.1 TB/s), combine 110 (5.5), combine backward 222 (5.2), dispatch backward 106 (5.7);
 // a large copy reaches 5.2.  A token's row indexes are read together, before its pieces go out
 // (dispatch and combine with their plan 244.6 -> 240.5 us).
+#include <algorithm>
+
 #include "chunk.h"
 
 namespace pr2 {
@@ -51,7 +53,9 @@ __device__ __forceinline__ void zero_rest(const RowArgs& a, int filled, int lane
             store_chunk<T, NT>((T*)a.rows_out + r * a.d, c, full, rem, v);
 }
 
-// blockDim = (lanes per token, tokens per workgroup); lanes is a multiple of 64
+// blockDim = (lanes per token, tokens per workgroup); lanes is a multiple of 64.  With few tokens a
+// token's pieces past the first lanes go to workgroups of their own (gridDim.y), in gather_sum
+// too.
 template <typename T, bool NT>
 __global__ void __launch_bounds__(kThreads) dispatch_kernel(RowArgs a) {
     const int full = a.d / Chunk<T>::E, rem = a.d % Chunk<T>::E;
@@ -62,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(RowArgs a) {
     const int filled = a.offsets[a.N];
     for (int64_t t = b; t < a.T; t += wgs) {
         const T* x = (const T*)a.tok + t * a.d;
-        for (int c = threadIdx.x; c < n; c += blockDim.x) {
+        for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < n; c += gridDim.y * blockDim.x) {
             const u32x4 w = load_chunk<T, true>(x, c, full, rem);
             for (int s0 = 0; s0 < a.k; s0 += kSlots) {
                 int r[kSlots];
@@ -75,7 +79,7 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(RowArgs a) {
             }
         }
     }
-    zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
+    if (blockIdx.y == 0) zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
 }
 
 // y[t] = sum_s [gate] row: combine (GATED) and the gradient of dispatch.  (Two tokens at a
@@ -88,7 +92,7 @@ __global__ void __launch_bounds__(kThreads) gather_sum_kernel(RowArgs a) {
     const int y = __builtin_amdgcn_readfirstlane(threadIdx.y);
     const int64_t wgs = (int64_t)gridDim.x * blockDim.y;
     for (int64_t t = (int64_t)blockIdx.x * blockDim.y + y; t < a.T; t += wgs) {
-        for (int c = threadIdx.x; c < n; c += blockDim.x) {
+        for (int c = blockIdx.y * blockDim.x + threadIdx.x; c < n; c += gridDim.y * blockDim.x) {
             float acc[E] = {};
             for (int s0 = 0; s0 < a.k; s0 += kSlots) {
                 u32x4 w[kSlots];
@@ -139,7 +143,8 @@ __device__ __forceinline__ float sum_slots(const float (&v)[kSlots], int lane) {
     return r;
 }
 
-// d_o may be o: a thread reads its piece of a row before it writes it.
+// d_o may be o: a thread reads its piece of a row before it writes it.  With few tokens a
+// token's groups of slots go to workgroups of their own (gridDim.y).
 template <typename T, bool NT>
 __global__ void __launch_bounds__(kThreads) combine_backward_kernel(RowArgs a) {
     constexpr int E = Chunk<T>::E;
@@ -157,7 +162,7 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(RowArgs a) {
     for (int64_t turn = 0; turn < turns; ++turn) {
         const int64_t t = turn * wgs + b;
         const bool in = t < a.T;
-        for (int s0 = 0; s0 < a.k; s0 += kSlots) {
+        for (int s0 = blockIdx.y * kSlots; s0 < a.k; s0 += gridDim.y * kSlots) {
             int r[kSlots];
             float g[kSlots];
             float dot[kSlots] = {};
@@ -207,7 +212,7 @@ __global__ void __launch_bounds__(kThreads) combine_backward_kernel(RowArgs a) {
             }
         }
     }
-    zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
+    if (blockIdx.y == 0) zero_rest<T, NT>(a, filled, blockDim.x, threadIdx.x, b, wgs);
 }
 
 // ------------------------------------------------------------------ host ----
@@ -228,12 +233,26 @@ dim3 row_grid(const RowArgs& a, dim3 block) {
 // Whether the sorted rows that a call writes pass the caches by.
 bool stream_rows(const RowArgs& a, int elem) { return a.Tk * a.d * elem > kStreamBytes; }
 
+// Where the tokens alone leave the chip idle, more workgroups per token: for each eight slots in
+// combine backward, for each 256 pieces of a row in the others (9 tokens of 4058, k 11, both
+// directions 42.9 -> 32.1 us; 512 of 2988, k 10, the backward 49.5 -> 42.6; 300 of 4096, k 8,
+// plan, dispatch and combine 21.7 -> 19.1).
+constexpr int64_t kFewTokens = 512;
+unsigned slot_groups(const RowArgs& a) { return a.T <= kFewTokens ? (a.k + kSlots - 1) / kSlots : 1; }
+unsigned piece_groups(const RowArgs& a, int elem) {
+    const int64_t n = ((int64_t)a.d * elem + 15) / 16;
+    return a.T <= kFewTokens ? (unsigned)std::min<int64_t>((n + kThreads - 1) / kThreads, 16) : 1;
+}
+
 template <typename K>
-pr2_status launch_rows(K kernel, const RowArgs& a, int elem, const char* name, hipStream_t st) {
+pr2_status launch_rows(K kernel, const RowArgs& a, int elem, const char* name, hipStream_t st,
+                       unsigned groups = 1) {
     const dim3 block = row_block(a, elem);
     {
         LaunchScope scope(name, st);
-        hipLaunchKernelGGL(kernel, row_grid(a, block), block, 0, st, a);
+        dim3 grid = row_grid(a, block);
+        grid.y = groups;
+        hipLaunchKernelGGL(kernel, grid, block, 0, st, a);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? ok() : hip_fail(e, name);
@@ -365,9 +384,9 @@ pr2_status pr2_dispatch(const pr2_moe_desc* desc, const void* x, const int32_t* 
     a.rows_out = xs;
     if (d.act_dtype == PR2_F32)
         return launch_rows(stream_rows(a, 4) ? dispatch_kernel<float, true> : dispatch_kernel<float, false>,
-                           a, 4, "dispatch", st);
+                           a, 4, "dispatch", st, piece_groups(a, 4));
     return launch_rows(stream_rows(a, 2) ? dispatch_kernel<bf16_t, true> : dispatch_kernel<bf16_t, false>,
-                       a, 2, "dispatch", st);
+                       a, 2, "dispatch", st, piece_groups(a, 2));
 }
 
 pr2_status pr2_dispatch_backward(const pr2_moe_desc* desc, const void* dxs,
@@ -389,8 +408,8 @@ pr2_status pr2_dispatch_backward(const pr2_moe_desc* desc, const void* dxs,
     a.rows = dxs;
     a.tok_out = dx;
     if (d.act_dtype == PR2_F32)
-        return launch_rows(gather_sum_kernel<float, false>, a, 4, "dispatch_backward", st);
-    return launch_rows(gather_sum_kernel<bf16_t, false>, a, 2, "dispatch_backward", st);
+        return launch_rows(gather_sum_kernel<float, false>, a, 4, "dispatch_backward", st, piece_groups(a, 4));
+    return launch_rows(gather_sum_kernel<bf16_t, false>, a, 2, "dispatch_backward", st, piece_groups(a, 2));
 }
 
 pr2_status pr2_combine(const pr2_moe_desc* desc, const void* o, const int32_t* row_of_route,
@@ -413,8 +432,8 @@ pr2_status pr2_combine(const pr2_moe_desc* desc, const void* o, const int32_t* r
     a.gate = gate;
     a.tok_out = y;
     if (d.act_dtype == PR2_F32)
-        return launch_rows(gather_sum_kernel<float, true>, a, 4, "combine_rows", st);
-    return launch_rows(gather_sum_kernel<bf16_t, true>, a, 2, "combine_rows", st);
+        return launch_rows(gather_sum_kernel<float, true>, a, 4, "combine_rows", st, piece_groups(a, 4));
+    return launch_rows(gather_sum_kernel<bf16_t, true>, a, 2, "combine_rows", st, piece_groups(a, 2));
 }
 
 pr2_status pr2_combine_backward(const pr2_moe_desc* desc, const void* dy, const void* o,
@@ -448,10 +467,10 @@ pr2_status pr2_combine_backward(const pr2_moe_desc* desc, const void* dy, const 
     if (d.act_dtype == PR2_F32)
         return launch_rows(stream_rows(a, 4) ? combine_backward_kernel<float, true>
                                              : combine_backward_kernel<float, false>,
-                           a, 4, "combine_backward", st);
+                           a, 4, "combine_backward", st, slot_groups(a));
     return launch_rows(stream_rows(a, 2) ? combine_backward_kernel<bf16_t, true>
                                          : combine_backward_kernel<bf16_t, false>,
-                       a, 2, "combine_backward", st);
+                       a, 2, "combine_backward", st, slot_groups(a));
 }
 
 }  // extern "C"

@@ -642,7 +642,13 @@ hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, int* coun
         return hipGetLastError();
     }
     LaunchScope scope("policy_fused", s);
-    if (n <= 256 * 4)
+    // (short rows to one wavefront each, no barrier: 16384 rows of 1609 bf16 logits 82 -> 36 us,
+    // of 4000 85 -> 53; of 8000 104 with four wavefronts, 117 with one)
+    if (n <= 64 * 4)
+        hipLaunchKernelGGL((policy_fused_kernel<T, 64, 4, false>), grid, dim3(64), 0, s, a, nullptr);
+    else if (n <= 64 * 8)
+        hipLaunchKernelGGL((policy_fused_kernel<T, 64, 8, false>), grid, dim3(64), 0, s, a, nullptr);
+    else if (n <= 256 * 4)
         hipLaunchKernelGGL((policy_fused_kernel<T, 256, 4, false>), grid, dim3(256), 0, s, a, nullptr);
     else if (n <= 256 * 16)
         hipLaunchKernelGGL((policy_fused_kernel<T, 256, 16, false>), grid, dim3(256), 0, s, a, nullptr);

@@ -281,3 +281,12 @@ def test_refusals_of_the_binding():
     buf = torch.zeros((12, 16), device="cuda")
     with pytest.raises(B.Pr2Error, match="overlaps"):
         B.dispatch(buf[:4], off, row, buf[2:10])
+
+
+# around the token counts up to which a token's slots and pieces go to several workgroups, rows
+# of several hundred pieces, groups of slots that are not full
+@pytest.mark.parametrize("case", [(9, 4058, 30, 11, "bf16", 0.05), (1, 4100, 20, 17, "f32", 0.3),
+                                  (3, 40000, 9, 9, "bf16", 0.4), (512, 1033, 12, 9, "f32", 0.1),
+                                  (513, 1033, 12, 9, "f32", 0.1)], ids=str)
+def test_several_workgroups_per_token(case):
+    test_both_directions(case, "int32")

@@ -405,3 +405,10 @@ def test_many_long_rows_taken_in_turns():
     in_place = z
     B.policy_loss(in_place, y, old, adv, sums, weight=w, dlogits=in_place)
     assert torch.equal(in_place, grad)
+
+
+# the widths at which a row's threads and pieces change
+@pytest.mark.parametrize("act", [BF, "f32"])
+@pytest.mark.parametrize("T,V", [(3, 2041), (5, 2048), (2, 2049), (3, 4089), (1, 4096), (300, 1017), (2, 8192), (3, 8193)])
+def test_loss_and_gradient_of_short_rows(T, V, act):
+    test_loss_and_gradient(T, V, act)
