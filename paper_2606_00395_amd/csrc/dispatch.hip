@@ -233,11 +233,12 @@ dim3 row_grid(const RowArgs& a, dim3 block) {
 // Whether the sorted rows that a call writes pass the caches by.
 bool stream_rows(const RowArgs& a, int elem) { return a.Tk * a.d * elem > kStreamBytes; }
 
-// Where the tokens alone leave the chip idle, more workgroups per token: for each eight slots in
+// Up to a few thousand tokens, where the tokens alone do not fill the chip, more workgroups per token: for each eight slots in
 // combine backward, for each 256 pieces of a row in the others (9 tokens of 4058, k 11, both
-// directions 42.9 -> 32.1 us; 512 of 2988, k 10, the backward 49.5 -> 42.6; 300 of 4096, k 8,
-// plan, dispatch and combine 21.7 -> 19.1).
-constexpr int64_t kFewTokens = 512;
+// directions 42.9 -> 32.1 us; 1500 of 2988, k 10, the backward 105.5 -> 89.7, 4000 of 1000, k 12,
+// 64.5 -> 61.9; 300 and 3000 of 4096, k 8, plan, dispatch and combine 21.7 -> 19.1 and 108.9 ->
+// 105.0).
+constexpr int64_t kFewTokens = 4096;
 unsigned slot_groups(const RowArgs& a) { return a.T <= kFewTokens ? (a.k + kSlots - 1) / kSlots : 1; }
 unsigned piece_groups(const RowArgs& a, int elem) {
     const int64_t n = ((int64_t)a.d * elem + 15) / 16;
