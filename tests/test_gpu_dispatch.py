@@ -287,6 +287,7 @@ def test_refusals_of_the_binding():
 # of several hundred pieces, groups of slots that are not full
 @pytest.mark.parametrize("case", [(9, 4058, 30, 11, "bf16", 0.05), (1, 4100, 20, 17, "f32", 0.3),
                                   (3, 40000, 9, 9, "bf16", 0.4), (512, 1033, 12, 9, "f32", 0.1),
-                                  (4096, 24, 12, 9, "bf16", 0.1), (4097, 24, 12, 9, "f32", 0.1)], ids=str)
+                                  (513, 1033, 12, 9, "f32", 0.1), (4096, 24, 12, 9, "bf16", 0.1),
+                                  (4097, 24, 12, 9, "f32", 0.1)], ids=str)
 def test_several_workgroups_per_token(case):
     test_both_directions(case, "int32")
