@@ -71,7 +71,7 @@ PyObject* need(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwn
                 return PyLong_FromVoidPtr(t->data_ptr());
         }
     } catch (const std::exception&) {
-        // a tensor that has no such property (no storage, symbolic sizes): named over there
+        PyErr_Clear();      // a tensor that has no such property (no storage, symbolic sizes): named over there
     }
     return refuse(g_need, args, nargs, kwnames);
 }
@@ -90,6 +90,7 @@ PyObject* need_act(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject*
             return Py_BuildValue("(LLNN)", (long long)t->size(0), (long long)t->size(1), dtype, device);
         }
     } catch (const std::exception&) {
+        PyErr_Clear();
     }
     return refuse(g_need_act, args, nargs, kwnames);
 }

@@ -97,3 +97,12 @@ def test_need_act(plain, dtype):
         assert m._need_act(x, "x") == (3, 5, dtype, x.device)
         assert m._need(x, "x", (3, 5), dtype, x.device) == x.data_ptr()
         assert outcome(m._need, x, "x", (3, 5), dtype, CPU)[0] is ValueError
+
+
+def test_tensors_without_storage_or_strides(plain):
+    meta = torch.empty((3, 4), device="meta")
+    sparse = torch.eye(3).to_sparse()
+    for t, shape in ((meta, (3, 4)), (sparse, (3, 3))):
+        got, want = outcome(B._need, t, "x", shape, torch.float32, CPU), outcome(plain._need, t, "x", shape, torch.float32, CPU)
+        assert got == want and issubclass(got[0], Exception)
+        assert outcome(B._need_act, t, "x") == outcome(plain._need_act, t, "x")
