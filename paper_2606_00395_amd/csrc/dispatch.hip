@@ -9,7 +9,7 @@
 // once and its k sorted rows, each contiguous, are written or read as whole segments; no
 // row is read for a route that was dropped.  The sums over the slots run in slot order in
 // fp32, so no atomics and the same bits every time.  16384 tokens of 2048 bf16, k 8: dispatch
-// 119 us (5.1 TB/s), combine 110 (5.5), combine backward 222 (5.2), dispatch backward 106 (5.7);
+// 111 us (5.5 TB/s), combine 111 (5.4), combine backward 218 (5.3), dispatch backward 105 (5.8);
 // a large copy reaches 5.2.  A token's row indexes are read together, before its pieces go out
 // (dispatch and combine with their plan 244.6 -> 240.5 us).
 #include <algorithm>
