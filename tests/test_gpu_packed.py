@@ -395,3 +395,17 @@ def test_weight_gradients_in_many_slices_and_of_few_experts(R, n_out, n_in, N, b
         cuts = np.sort(g.integers(0, R // 3, N - 1))        # the last one has most
         offsets = torch.from_numpy(np.concatenate([[0], cuts, [R]]).astype(np.int32)).cuda()
     check_wgrad(act(g.standard_normal((R, n_out)), bf16), act(g.standard_normal((R, n_in)), bf16), offsets, N=N)
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+@pytest.mark.parametrize("R,n_out,n_in", [(70, 264, 272), (70, 135, 203), (300, 8, 64)])
+@pytest.mark.parametrize("top,slope", [(3.3e38, 1e-30), (1e-38, 1e30)], ids=["largest", "smallest"])
+def test_weight_gradients_of_the_largest_and_smallest_groups(top, slope, R, n_out, n_in, bf16):
+    """Groups at both ends of the scale's range, zeros among their values: every value is a
+    finite number, and the sums of products that are finite stay so, at every width."""
+    g = np.random.default_rng([R, n_out, n_in])
+    x = g.uniform(-1, 1, (R, n_in)) * top
+    x[g.random((R, n_in)) < 0.3] = 0.0
+    scale = O.pack(act(x, bf16).float().cpu().numpy())[1]
+    assert np.any(scale == (248 if top > 1 else 1))
+    check_wgrad(act(g.standard_normal((R, n_out)) * slope, bf16), act(x, bf16))
