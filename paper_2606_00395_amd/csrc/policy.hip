@@ -188,15 +188,17 @@ __device__ __forceinline__ void zero_chunks(T* row, int c0, int c1, int step, in
     for (int c = c0; c < c1; c += step) store_chunk(row, c, full, rem, v);
 }
 
-// Statistics of row blockIdx.x / S, part blockIdx.x % S (whole rows finish here).
+// Statistics of row b / S, part b % S for workgroup b (whole rows finish here).
 constexpr int kStatThreads = 256;
 constexpr int kStatDeep = 4;        // chunks in flight per thread
 
 template <typename T>
 __global__ void __launch_bounds__(kStatThreads) policy_stats_kernel(PolicyArgs a) {
     constexpr int E = Chunk<T>::E;
-    const int64_t t = blockIdx.x / a.S;
-    const int part = (int)(blockIdx.x - t * a.S);
+    const uint32_t b = block_number();
+    const int64_t t = b / (uint32_t)a.S;
+    const int part = (int)(b - t * a.S);
+    if (t >= a.T) return;
     __shared__ Exchange<kStatThreads / 64> x;
     const Row r = open_row(a, t);
     Stat st{kLowest, 0.0f, 0.0f};
@@ -229,7 +231,7 @@ __global__ void __launch_bounds__(kStatThreads) policy_stats_kernel(PolicyArgs a
         join_block(st, a.k, x);
     }
     if (a.S > 1) {
-        if (threadIdx.x == 0) a.part[blockIdx.x] = make_float4(st.m, st.s, st.e, 0.0f);
+        if (threadIdx.x == 0) a.part[b] = make_float4(st.m, st.s, st.e, 0.0f);
     } else {
         close_row(a, t, r, zy, st, threadIdx.x == 0);
     }
@@ -285,13 +287,15 @@ __global__ void __launch_bounds__(SUMS ? kSumThreads : 256) policy_finish_kernel
     }
 }
 
-// dlogits of row blockIdx.x / S, part blockIdx.x % S, from lse and coef.
+// dlogits of row b / S, part b % S for workgroup b, from lse and coef.
 // NT: the gradient passes the caches by.
 template <typename T, bool NT>
 __global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
     constexpr int E = Chunk<T>::E;
-    const int64_t t = blockIdx.x / a.S;
-    const int part = (int)(blockIdx.x - t * a.S);
+    const uint32_t b = block_number();
+    const int64_t t = b / (uint32_t)a.S;
+    const int part = (int)(b - t * a.S);
+    if (t >= a.T) return;
     const T* z = (const T*)a.z + t * a.ldl;
     T* dz = (T*)a.dz + t * a.ldd;
     const int full = a.V / E, rem = a.V % E;
@@ -352,7 +356,8 @@ __global__ void __launch_bounds__(NT) policy_fused_kernel(PolicyArgs a, int* cou
     __shared__ int s_next[2];
     int tid = threadIdx.x;
     const int full = a.V / E, rem = a.V % E;
-    int64_t t = blockIdx.x;
+    int64_t t = block_number();
+    if (t >= a.T) return;
     Row r = open_row(a, t);
     u32x4 w[NCH];
     auto load_piece = [&](const T* z, int i) __attribute__((always_inline)) {
@@ -456,7 +461,7 @@ policy_sums_kernel(const float4* rows, int64_t T, float* out) {
 // ------------------------------------------------------------------ host ----
 constexpr int kCus = 256;
 constexpr int kMaxParts = 64;
-constexpr int64_t kMaxRows = 0x7fffffff / kMaxParts;    // the grid is T x parts
+constexpr int64_t kMaxRows = 0x7fffffff / kMaxParts;    // T x parts are numbered in 32 bits
 constexpr int64_t kMaxStride = (int64_t)1 << 35;        // T x stride in bytes stays below 2^63
 constexpr int64_t kFillWgs = 2048;      // workgroups of 256 that fill the chip
 constexpr size_t kPartBytes = sizeof(float4) * 2 * kFillWgs;
@@ -595,7 +600,7 @@ hipError_t launch_stats(const pr2_policy_desc& d, PolicyArgs a, float* sums, hip
     a.S = row_parts(d);
     {
         LaunchScope scope("policy_stats", s);
-        hipLaunchKernelGGL(policy_stats_kernel<T>, dim3((unsigned)(d.T * a.S)), dim3(kStatThreads),
+        hipLaunchKernelGGL(policy_stats_kernel<T>, wide_grid(d.T * a.S, kStatThreads), dim3(kStatThreads),
                            0, s, a);
     }
     hipError_t e = hipGetLastError();
@@ -618,7 +623,7 @@ template <typename T>
 hipError_t launch_grad(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
     a.S = row_parts(d);
     LaunchScope scope("policy_grad", s);
-    const dim3 grid((unsigned)(d.T * a.S));
+    const dim3 grid = wide_grid(d.T * a.S, 256);
     if (d.T * d.V * (int64_t)sizeof(T) > kStreamBytes)
         hipLaunchKernelGGL((policy_grad_kernel<T, true>), grid, dim3(256), 0, s, a);
     else
@@ -629,7 +634,7 @@ hipError_t launch_grad(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
 template <typename T>
 hipError_t launch_fused(const pr2_policy_desc& d, const PolicyArgs& a, int* counter, hipStream_t s) {
     const int n = row_chunks(d);
-    const dim3 grid((unsigned)d.T);
+    const dim3 grid = wide_grid(d.T, 1024);
     // Rows that are held whole, eight a CU or more: the counter's turns (4096 rows of 151936
     // bf16 logits, a tenth of them without weight, 519 -> 484 us; without it 2048 rows took
     // 266 and 1024 rows 148 us, with it 267 and 149; 2048 fp32 rows, half of each read

@@ -412,3 +412,38 @@ def test_many_long_rows_taken_in_turns():
 @pytest.mark.parametrize("T,V", [(3, 2041), (5, 2048), (2, 2049), (3, 4089), (1, 4096), (300, 1017), (2, 8192), (3, 8193)])
 def test_loss_and_gradient_of_short_rows(T, V, act):
     test_loss_and_gradient(T, V, act)
+
+
+def test_more_rows_than_a_grid_of_one_dimension_holds():
+    """2^24 rows and more, as many workgroups of 256: the first and last rows' results are those
+    of the rows alone."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    T, V, n = 2 ** 24 + 5, 3, 1000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    z = torch.randn((T, V), generator=g, device="cuda").to(torch.bfloat16)
+    y = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    old = torch.full((T,), -1.0, device="cuda")
+    adv = torch.randn(T, generator=g, device="cuda")
+    nan = lambda *s, dt=torch.float32: torch.full(s, float("nan"), device="cuda", dtype=dt)
+
+    def run(z, y, old, adv):
+        T = len(y)
+        out = [nan(T) for _ in range(5)] + [nan(T, V, dt=z.dtype) for _ in range(2)]
+        lp, logp, lse, ent, coef, once, twice = out
+        sums = nan(4)
+        B.token_logprob(z, y, lp)
+        B.policy_loss(z, y, old, adv, sums, logp_out=logp, lse_out=lse, entropy_out=ent, coef_out=coef)
+        B.policy_loss_backward(z, y, lse, coef, twice)
+        B.policy_loss(z, y, old, adv, nan(4), dlogits=once)
+        return out, sums
+
+    whole, sums = run(z, y, old, adv)
+    for sl in (slice(0, n), slice(T - n, T)):
+        for a, b in zip(whole, run(z[sl], y[sl], old[sl], adv[sl])[0]):
+            assert torch.equal(a[sl], b)
+    lp, _, _, _, _, once, twice = whole
+    assert torch.isfinite(lp).all() and torch.isfinite(once).all() and torch.isfinite(twice).all()
+    want = torch.log_softmax(z.double(), 1).gather(1, y.long()[:, None])[:, 0]
+    assert torch.all((lp.double() - want).abs() <= 1e-5 + 4e-7 * want.abs())
+    assert torch.isfinite(sums).all()
