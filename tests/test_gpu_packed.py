@@ -409,3 +409,31 @@ def test_weight_gradients_of_the_largest_and_smallest_groups(top, slope, R, n_ou
     scale = O.pack(act(x, bf16).float().cpu().numpy())[1]
     assert np.any(scale == (248 if top > 1 else 1))
     check_wgrad(act(g.standard_normal((R, n_out)) * slope, bf16), act(x, bf16))
+
+
+def test_as_many_rows_as_are_allowed():
+    """2^31 - 1 rows: the first and last ones as packed alone, the others zeros."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    R, n = 2 ** 31 - 1, 700
+    x = torch.zeros((R, 1), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for sl in (slice(0, n), slice(R - n, R)):
+        x[sl] = torch.randn((n, 1), generator=g, device="cuda").to(torch.bfloat16)
+    q = torch.full((R, 1), 99, dtype=torch.int8, device="cuda")
+    e = torch.full((R, 1), 77, dtype=torch.uint8, device="cuda")
+    B.act_pack(x, q, e)
+    for sl in (slice(0, n), slice(R - n, R)):
+        sq, se = do_pack(x[sl].clone())
+        assert torch.equal(q[sl], sq) and torch.equal(e[sl], se)
+    for r in range(n, R - n, 2 ** 28):      # (in parts: the comparisons take memory too)
+        sl = slice(r, min(r + 2 ** 28, R - n))
+        assert not q[sl].any() and torch.all(e[sl] == 1)
+    x.fill_(float("nan"))
+    B.act_unpack(q, e, x)
+    for sl in (slice(0, n), slice(R - n, R)):
+        back = torch.full((n, 1), float("nan"), dtype=torch.bfloat16, device="cuda")
+        B.act_unpack(q[sl].clone(), e[sl].clone(), back)
+        assert torch.equal(x[sl], back)
+    for r in range(n, R - n, 2 ** 28):
+        assert not x[r:min(r + 2 ** 28, R - n)].any()
