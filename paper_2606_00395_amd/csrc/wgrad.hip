@@ -96,12 +96,12 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
     __shared__ __attribute__((aligned(16))) float A[kStep * kTilePitch], B[kStep * kTilePitch];
     const int tid = threadIdx.x;
     const int lane = tid & 63, wave = tid >> 6;
-    const int nct = (a.n_in + kTile - 1) / kTile;
-    const int o0 = (int)(blockIdx.x / nct) * kTile, c0 = (int)(blockIdx.x % nct) * kTile;
-    const int e = blockIdx.y;
+    const int o0 = (int)blockIdx.y * kTile, c0 = (int)blockIdx.x * kTile;
+    const int slice = a.S == 1 ? 0 : (int)blockIdx.z / a.N;
+    const int e = (int)blockIdx.z - slice * a.N;
     int first, last;
     expert_rows(a, e, &first, &last);
-    slice_rows(a, blockIdx.z, &first, &last);
+    slice_rows(a, slice, &first, &last);
     const int sr = tid / 8, sc = (tid % 8) * 8;         // row and columns this thread stages
     f32x16 acc;
 #pragma unroll
@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
     const int c = c0 + bo;
     if (c >= a.n_in) return;
     const int o = o0 + 32 * (wave >> 1) + 4 * k2;
-    float* to = (a.S > 1 ? a.part : a.dW) + (((int64_t)blockIdx.z * a.N + e) * a.n_out + o) * a.n_in + c;
+    float* to = (a.S > 1 ? a.part : a.dW) + ((int64_t)blockIdx.z * a.n_out + o) * a.n_in + c;
 #pragma unroll
     for (int v = 0; v < 16; ++v)
         if (o + 8 * (v / 4) + v % 4 < a.n_out) to[(int64_t)(8 * (v / 4) + v % 4) * a.n_in] = acc[v];
@@ -677,7 +677,9 @@ hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, 
         LaunchScope scope("wgrad_mfma", st);
         hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
     } else {
-        const dim3 grid((unsigned)(wgrad_tile_count(d, kTile) / d.N), d.N, a.S);
+        // (column and row tiles apart, at most 2^14 each: together they can be more than a
+        // dimension holds; N S <= 1024)
+        const dim3 grid((unsigned)ceil_div(d.n_in, kTile), (unsigned)ceil_div(d.n_out, kTile), d.N * a.S);
         LaunchScope scope("wgrad_tile", st);
         if (d.act_dtype == PR2_BF16)
             hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, grid, dim3(256), 0, st, a);
