@@ -466,9 +466,10 @@ pr2_status pr2_token_logprob(const pr2_policy_desc* desc, const void* logits, co
  *              pr2_policy_loss_backward reads)
  *   dlogits    [T, V] act_dtype at row stride ldd, or NULL; may be logits itself (same
  *              stride), otherwise the two must not overlap
- * Statistics are held in fp32 (differences to the row's maximum), the sums over tokens in fp64;
- * the same call gives the same bits.  (Calls of other batch sizes may split a row differently
- * and differ in its last bits.)  T = 0 writes zeros to sums_out.
+ * Statistics are held in fp32 (differences to the row's maximum), and the gradient is formed from
+ * them, so that neither depends on how far from zero the logits lie; the sums over tokens are
+ * held in fp64.  The same call gives the same bits.  (Calls of other batch sizes may split a row
+ * differently and differ in its last bits.)  T = 0 writes zeros to sums_out.
  */
 pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, const void* token,
                            const float* logp_old, const float* logp_ref, const float* adv,

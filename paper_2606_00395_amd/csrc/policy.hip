@@ -111,6 +111,7 @@ struct PolicyArgs {
     float* coef;
     float4* rowsum;         // [T] the row's terms of the four sums (null without a loss)
     float4* part;           // [T, S] statistics of the parts of split rows
+    float4* kept;           // [T] maximum, sum, coef and logp for the gradient's launch (may be null)
     void* dz;               // may be null, may be z
     const float* grad;      // backward: one number or null
     int64_t T, ldl, ldd;
@@ -178,6 +179,7 @@ __device__ __forceinline__ Result close_row(const PolicyArgs& a, int64_t t, cons
         if (a.ent) a.ent[t] = ent;
         if (a.coef) a.coef[t] = coef;
         if (a.rowsum) a.rowsum[t] = sums;
+        if (a.kept) a.kept[t] = make_float4(st.m, st.s, coef, logp);
     }
     return Result{coef, logp};
 }
@@ -287,9 +289,11 @@ __global__ void __launch_bounds__(SUMS ? kSumThreads : 256) policy_finish_kernel
     }
 }
 
-// dlogits of row b / S, part b % S for workgroup b, from lse and coef.
-// NT: the gradient passes the caches by.
-template <typename T, bool NT>
+// dlogits of row b / S, part b % S for workgroup b.  KEPT: from what the statistics of the same
+// call left, p = 2^(k (z - M)) / S as the fused form has it; otherwise from the caller's lse
+// and coef, where log p has the rounding of lse (half a last place of a number that grows with
+// the level of the logits).  NT: the gradient passes the caches by.
+template <typename T, bool KEPT, bool NT>
 __global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
     constexpr int E = Chunk<T>::E;
     const uint32_t b = block_number();
@@ -303,13 +307,16 @@ __global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
     const int per = (n + a.S - 1) / a.S;
     const int c0 = part * per, c1 = min(n, c0 + per);
     const int64_t y = a.y64 ? ((const int64_t*)a.y)[t] : (int64_t)((const int32_t*)a.y)[t];
-    const float coef = a.coef[t];
+    float4 kept = make_float4(0.0f, 1.0f, 0.0f, 0.0f);
+    if (KEPT) kept = a.kept[t];
+    const float coef = KEPT ? kept.z : a.coef[t];
     if (coef == 0.0f || y < 0 || y >= a.V) {
         zero_chunks(dz, c0 + (int)threadIdx.x, c1, 256, full, rem);
         return;
     }
-    const float lse = a.lse[t];
+    const float lse = KEPT ? 0.0f : a.lse[t];
     const float g = coef * a.it * (a.grad ? *a.grad : 1.0f);
+    const float gs = KEPT ? -g / kept.y : -g;
     const int yc = (int)(y / E), ye = (int)(y % E);
     constexpr int D = 4;
     for (int c = c0 + (int)threadIdx.x; c < c1; c += D * 256) {
@@ -322,15 +329,18 @@ __global__ void __launch_bounds__(256) policy_grad_kernel(PolicyArgs a) {
         for (int i = 0; i < D; ++i) {
             const int ci = c + i * 256;
             if (ci >= c1) continue;
-            // log p first, in one rounding, then its power
             float v[E];
             Chunk<T>::open(w[i], v);
-            float ly = 0.0f;
+            float ly = kept.w;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                v[j] = fmaf(v[j], a.it, -lse);
-                if (j == ye) ly = v[j];
-                v[j] = -g * exp2_native(v[j] * kLog2e);
+                if (KEPT) {
+                    v[j] = gs * exp2_native((v[j] - kept.x) * a.k);
+                } else {        // log p first, in one rounding, then its power
+                    v[j] = fmaf(v[j], a.it, -lse);
+                    if (j == ye) ly = v[j];
+                    v[j] = gs * exp2_native(v[j] * kLog2e);
+                }
             }
             if (ci == yc) {
                 const float gy = -g * expm1f(ly);       // c s (1 - p_y)
@@ -502,6 +512,7 @@ struct PolicyWs {
     int* counter;
     float4* rowsum;
     float4* part;
+    float4* kept;
     size_t bytes;
 };
 
@@ -512,7 +523,8 @@ PolicyWs policy_ws(const pr2_policy_desc& d, void* base) {
     w.counter = (int*)p;
     const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
     w.rowsum = (float4*)(p ? p + kPartBytes : nullptr);
-    w.bytes = kPartBytes + 3 * stats + 256;
+    w.kept = (float4*)(p ? p + kPartBytes + stats : nullptr);
+    w.bytes = kPartBytes + 2 * stats + 256;
     return w;
 }
 
@@ -624,10 +636,15 @@ hipError_t launch_grad(const pr2_policy_desc& d, PolicyArgs a, hipStream_t s) {
     a.S = row_parts(d);
     LaunchScope scope("policy_grad", s);
     const dim3 grid = wide_grid(d.T * a.S, 256);
-    if (d.T * d.V * (int64_t)sizeof(T) > kStreamBytes)
-        hipLaunchKernelGGL((policy_grad_kernel<T, true>), grid, dim3(256), 0, s, a);
+    const bool stream = d.T * d.V * (int64_t)sizeof(T) > kStreamBytes;
+    if (a.kept && stream)
+        hipLaunchKernelGGL((policy_grad_kernel<T, true, true>), grid, dim3(256), 0, s, a);
+    else if (a.kept)
+        hipLaunchKernelGGL((policy_grad_kernel<T, true, false>), grid, dim3(256), 0, s, a);
+    else if (stream)
+        hipLaunchKernelGGL((policy_grad_kernel<T, false, true>), grid, dim3(256), 0, s, a);
     else
-        hipLaunchKernelGGL((policy_grad_kernel<T, false>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((policy_grad_kernel<T, false, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -756,9 +773,7 @@ pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, cons
             e = bf ? launch_fused<bf16_t>(d, a, w.counter, st) : launch_fused<float>(d, a, w.counter, st);
             if (e == hipSuccess) e = launch_sums(w.rowsum, d.T, sums_out, st);
         } else {
-            const size_t stats = (sizeof(float4) * (size_t)d.T + 255) & ~(size_t)255;
-            if (grad && !a.lse) a.lse = (float*)((char*)w.rowsum + stats);
-            if (grad && !a.coef) a.coef = (float*)((char*)w.rowsum + 2 * stats);
+            if (grad) a.kept = w.kept;
             e = bf ? launch_stats<bf16_t>(d, a, sums_out, st) : launch_stats<float>(d, a, sums_out, st);
             if (e == hipSuccess && grad)
                 e = bf ? launch_grad<bf16_t>(d, a, st) : launch_grad<float>(d, a, st);

@@ -447,3 +447,61 @@ def test_more_rows_than_a_grid_of_one_dimension_holds():
     want = torch.log_softmax(z.double(), 1).gather(1, y.long()[:, None])[:, 0]
     assert torch.all((lp.double() - want).abs() <= 1e-5 + 4e-7 * want.abs())
     assert torch.isfinite(sums).all()
+
+
+# Levels of the logits: p and 1 - p_y depend on differences alone, however far from zero the row
+# lies (None: every logit the lowest finite number).
+LEVELS = (0.0, 1e3, -1e3, 1e4, -1e4, 1e6, -1e6, None)
+
+
+def far_rows(T, V, act):
+    """Rows at every level; every third row's token takes nearly all of the probability."""
+    import torch
+    g = np.random.default_rng([12, T, V])
+    z = 2.5 * g.standard_normal((T, V))
+    y = g.integers(0, V, T)
+    z[np.arange(0, T, 3), y[::3]] = 28.0
+    for t in range(T):
+        level = LEVELS[t % len(LEVELS)]
+        z[t] = np.finfo(np.float32).min if level is None else z[t] + level
+    logits = torch.from_numpy(z).to(torch.float32)
+    if act == BF:
+        low = logits == torch.finfo(torch.float32).min
+        logits = logits.to(torch.bfloat16)
+        logits[low] = torch.finfo(torch.bfloat16).min
+    host_z = logits.float().numpy()
+    logp = O.token_stats(host_z, y)[0]
+    f = lambda a: np.asarray(a, dtype=np.float32)
+    host = dict(logits=host_z, token=y, logp_old=f(logp - 0.05), adv=f(g.choice([-1.5, 0.7], T)),
+                logp_ref=f(logp + g.normal(0, 0.3, T)), weight=f(g.uniform(0.1, 1, T) / T), kl_coef=0.05,
+                inv_temp=1.0)
+    return logits.cuda(), host
+
+
+def check_far_gradient(got, host, bf16, log_p_error=0.0):
+    """Every entry to its own size: an error e of a log-probability moves p by e p and 1 - p_y by
+    e p_y.  logp is within 1e-5 (see above), the other terms' exponents within 3e-5."""
+    ref = O.policy_loss(**host, clip_low=np.float32(0.2), clip_high=np.float32(0.28))
+    rows = np.arange(len(host["token"]))
+    r, d = np.exp(ref["logp"] - host["logp_old"]), host["logp_ref"] - ref["logp"]
+    tc = host["weight"] * (np.abs(host["adv"]) * r + host["kl_coef"] * np.exp(d)) * 2e-5
+    c, p = np.abs(ref["coef"]), ref["p"]
+    py = p[rows, host["token"]]
+    e = np.broadcast_to(np.asarray(log_p_error, dtype=np.float64), py.shape)
+    e = np.expm1(np.minimum(e, 50.0))
+    tol = (tc + (3e-5 + e) * c)[:, None] * p
+    tol[rows, host["token"]] = (tc + 3e-5 * c) * (1 - py) + (1.02e-5 + e) * c * py
+    want = ref["dlogits"]
+    if bf16:
+        tol = tol + 2.0 ** -8 * np.abs(want)
+    assert np.all(np.abs(got["dlogits"] - want) <= host["inv_temp"] * tol + 1e-37)
+
+
+# (T rows of V: both sides of the number of long rows from which on a row is one workgroup's)
+@pytest.mark.parametrize("act,V", [(BF, 80000), ("f32", 40000)])
+@pytest.mark.parametrize("T", [1, 9, 48, 195])
+def test_gradient_of_logits_far_from_zero(T, act, V):
+    logits, host = far_rows(T, V, act)
+    got = call(logits, host)
+    compare(dict(got, dlogits=None), host, act == BF)
+    check_far_gradient(got, host, act == BF)
