@@ -482,6 +482,9 @@ pr2_status pr2_policy_loss(const pr2_policy_desc* desc, const void* logits, cons
  * with p_v = exp(s z_v - lse_t).  grad_loss: one fp32 on the device (the gradient of the first
  * of the sums) or NULL for 1.  Rows with coef_t = 0 get zeros and are not read.  dlogits as
  * above (it may be logits itself).  clip_low, clip_high and kl_coef are not read.  No workspace.
+ * lse_t is one fp32 number, and log p_v = s z_v - lse_t has its rounding, up to |lse_t| 2^-23: p_v is
+ * off by that relatively and 1 - p_y by that times p_y.  (At a level of the logits of 30 that is
+ * 4e-6, at 1e4 1e-3.)  pr2_policy_loss with dlogits has no such error at any level.
  */
 pr2_status pr2_policy_loss_backward(const pr2_policy_desc* desc, const void* logits,
                                     const void* token, const float* lse, const float* coef,

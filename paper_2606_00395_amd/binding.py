@@ -778,7 +778,9 @@ def policy_loss(logits, token, logp_old, adv, sums_out, logp_ref=None, weight=No
 def policy_loss_backward(logits, token, lse, coef, dlogits, grad_loss=None, inv_temp=1.0,
                          stream=None):
     """pr2_policy_loss_backward on torch tensors: dlogits from the ``lse`` and ``coef`` that
-    policy_loss wrote, times ``grad_loss`` (an fp32 tensor of one element) if given."""
+    policy_loss wrote, times ``grad_loss`` (an fp32 tensor of one element) if given.  Log-
+    probabilities have the rounding of ``lse``, up to |lse| 2^-23; policy_loss with ``dlogits``
+    does not."""
     torch = _torch()
     desc, T, dev = _policy_desc(logits, token, inv_temp, dlogits=dlogits)
     if dlogits is None:

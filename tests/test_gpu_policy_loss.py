@@ -505,3 +505,13 @@ def test_gradient_of_logits_far_from_zero(T, act, V):
     got = call(logits, host)
     compare(dict(got, dlogits=None), host, act == BF)
     check_far_gradient(got, host, act == BF)
+
+
+@pytest.mark.parametrize("act,V", [(BF, 80000), ("f32", 40000)])
+@pytest.mark.parametrize("T", [9, 48, 195])
+def test_gradient_from_lse_far_from_zero(T, act, V):
+    """Two calls: log p within the rounding of lse, |lse| 2^-23, as the header states."""
+    logits, host = far_rows(T, V, act)
+    got = call(logits, host, split=True)
+    compare(dict(got, dlogits=None), host, act == BF)
+    check_far_gradient(got, host, act == BF, log_p_error=np.abs(got["lse"]) * 2.0 ** -23)
