@@ -941,6 +941,15 @@ def swiglu_backward_packed(q, scale, dh, d_au, h_out=None, stream=None):
                                            h_out, _stream(stream)))
 
 
+def weight_grad_workspace(dy, q, N=1, stream=None):
+    """A workspace for weight_grad_packed of N weights from up to dy.shape[0] rows."""
+    R, n_out, adt, _ = _need_act(dy, "dy")
+    if q.dim() != 2:
+        raise ValueError("q must be 2-D [Rx, n_in]")
+    desc = WgradDesc(R, q.shape[0], n_out, q.shape[1], N, 1, _ACT_CODES[adt])
+    return _new_ws(int(lib().pr2_weight_grad_workspace_bytes(byref(desc))), dy.device, stream)
+
+
 def weight_grad_packed(dy, q, scale, dW, offsets=None, route_of_row=None, k=1, ws=None,
                        stream=None):
     """pr2_weight_grad_packed on torch tensors: dW [N, n_out, n_in] from dy [R, n_out] and a

@@ -607,17 +607,31 @@ int64_t wgrad_tile_count(const pr2_wgrad_desc& d, int tile) {
 // 48.6 -> 26.1, 8192 of 512 x 512 35.7 -> 31.0, 20 fp32 experts of 33 x 50 25.9 -> 13.6.
 constexpr int kCus = 256;
 constexpr int kMaxSlices = 64;
-int wgrad_slices(const pr2_wgrad_desc& d) {
+struct SliceCost {
+    int64_t steps;          // steps of 32 rows of a tile that is not sliced
+    float step, join, part; // us: a step, the join's launch, a slice's traffic
+    int most;               // slices that can pay; does not decrease with the rows
+};
+SliceCost slice_cost(const pr2_wgrad_desc& d) {
     const bool big = mfma_ok(d);
     const int64_t tiles = wgrad_tile_count(d, big ? BM : kTile);
-    const int64_t rows = d.R / d.N;
-    const int64_t most = std::min<int64_t>({(big ? kCus : 4 * kCus) / tiles, ceil_div(rows, kBK), kMaxSlices});
-    const float step = big ? 0.9f : 1.2f;
-    const float part = 2.0f * sizeof(float) * (float)((int64_t)d.N * d.n_out * d.n_in) / 6.5e6f;
+    SliceCost c{};
+    c.steps = ceil_div(d.R / d.N, kBK);
+    c.step = big ? 0.9f : 1.2f;
+    c.join = 6.0f;
+    c.part = 2.0f * sizeof(float) * (float)((int64_t)d.N * d.n_out * d.n_in) / 6.5e6f;
+    const int64_t fill = std::min<int64_t>({(big ? kCus : 4 * kCus) / tiles, c.steps, kMaxSlices});
+    const float whole = c.step * (float)c.steps;
+    c.most = 1;
+    while (c.most < fill && c.join + (float)(c.most + 1) * c.part < whole) ++c.most;
+    return c;
+}
+int wgrad_slices(const pr2_wgrad_desc& d) {
+    const SliceCost c = slice_cost(d);
     int best = 1;
-    float least = step * (float)ceil_div(rows, kBK);
-    for (int s = 2; s <= most; ++s) {
-        const float t = step * (float)ceil_div(rows, (int64_t)s * kBK) + 6.0f + (float)s * part;
+    float least = c.step * (float)c.steps;
+    for (int s = 2; s <= c.most; ++s) {
+        const float t = c.step * (float)ceil_div(d.R / d.N, (int64_t)s * kBK) + c.join + (float)s * c.part;
         if (t < least) {
             least = t;
             best = s;
@@ -653,7 +667,7 @@ WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
     WgradWs w{};
     char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
     const size_t order = (sizeof(int) * (size_t)d.N + 255) & ~(size_t)255;
-    const int S = wgrad_slices(d);
+    const int S = slice_cost(d).most;       // not the slices of these rows alone: fewer rows can have more
     w.order = (int*)p;
     w.part = (float*)(p ? p + order : nullptr);
     w.bytes = order + (S > 1 ? sizeof(float) * (size_t)S * d.N * d.n_out * d.n_in : 0) + 256;

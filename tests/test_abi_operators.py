@@ -254,3 +254,14 @@ def test_host_checks_under_the_sanitizers():
                         "-p", "no:cacheprovider"], env=env, stdout=subprocess.PIPE,
                        stderr=subprocess.STDOUT, text=True, timeout=600)
     assert r.returncode == 0 and "runtime error" not in r.stdout, r.stdout[-2000:]
+
+
+@pytest.mark.parametrize("n_out,n_in,N,dt", [(512, 512, 1, B.PR2_BF16), (2048, 2048, 1, B.PR2_BF16), (64, 128, 1, B.PR2_BF16),
+                                             (64, 128, 9, B.PR2_F32), (33, 50, 20, B.PR2_F32), (135, 203, 7, B.PR2_BF16)])
+def test_weight_grad_workspace_does_not_decrease_with_the_rows(n_out, n_in, N, dt):
+    def need(R):
+        d = B.WgradDesc(R=R, Rx=R, n_out=n_out, n_in=n_in, N=N, k=1, act_dtype=dt)
+        return B.lib().pr2_weight_grad_workspace_bytes(byref(d))
+
+    sizes = [need(R) for R in [*range(6000), *range(6000, 70000, 371), 2 ** 24, 2 ** 30]]
+    assert sizes[0] > 0 and sizes == sorted(sizes)

@@ -437,3 +437,18 @@ def test_as_many_rows_as_are_allowed():
         assert torch.equal(x[sl], back)
     for r in range(n, R - n, 2 ** 28):
         assert not x[r:min(r + 2 ** 28, R - n)].any()
+
+
+def test_one_workspace_for_batches_up_to_the_largest():
+    """A workspace made for 5000 rows serves every smaller batch, also those in more slices."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    g = np.random.default_rng(9)
+    dy, x = act(g.standard_normal((5000, 512)), True), act(g.standard_normal((5000, 512)), True)
+    q, e = do_pack(x)
+    ws = B.weight_grad_workspace(dy, q)
+    for R in (5000, 2000, 480, 479, 448, 30, 1):
+        a, b = (torch.full((1, 512, 512), float("nan"), device="cuda") for _ in range(2))
+        B.weight_grad_packed(dy[:R], q[:R], e[:R], a, ws=ws)
+        B.weight_grad_packed(dy[:R], q[:R], e[:R], b)
+        assert torch.equal(a, b) and torch.isfinite(a).all(), R
