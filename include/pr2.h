@@ -465,7 +465,9 @@ pr2_status pr2_token_logprob(const pr2_policy_desc* desc, const void* logits, co
  *   logp_out, lse_out, entropy_out, coef_out [T], each may be NULL (lse and coef are what
  *              pr2_policy_loss_backward reads)
  *   dlogits    [T, V] act_dtype at row stride ldd, or NULL; may be logits itself (same
- *              stride), otherwise the two must not overlap
+ *              stride), otherwise the two must not overlap (rows of the same stride may lie
+ *              between each other, as halves of one buffer's columns do)
+ *   No other output may overlap an input or another output.
  * Statistics are held in fp32 (differences to the row's maximum), and the gradient is formed from
  * them, so that neither depends on how far from zero the logits lie; the sums over tokens are
  * held in fp64.  The same call gives the same bits.  (Calls of other batch sizes may split a row

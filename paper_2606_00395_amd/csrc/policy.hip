@@ -571,7 +571,12 @@ pr2_status check_logits(const pr2_policy_desc& d, const void* logits, const void
     if (grad) {
         const uintptr_t z0 = (uintptr_t)logits, z1 = z0 + e * ((size_t)(d.T - 1) * d.ldl + d.V);
         const uintptr_t g0 = (uintptr_t)dlogits, g1 = g0 + e * ((size_t)(d.T - 1) * d.ldd + d.V);
-        if (z0 < g1 && g0 < z1 && !(z0 == g0 && d.ldl == d.ldd))
+        // rows of the same stride can lie between each other: the gradient's start is then `off`
+        // bytes into a row's period, past its logits and with room before the next one's
+        const size_t period = e * (size_t)d.ldl, row = e * (size_t)d.V;
+        const size_t off = g0 >= z0 ? (g0 - z0) % period : (period - (z0 - g0) % period) % period;
+        const bool between = d.ldl == d.ldd && off >= row && off + row <= period;
+        if (z0 < g1 && g0 < z1 && !between && !(z0 == g0 && d.ldl == d.ldd))
             return fail(PR2_ERR_SHAPE, "dlogits overlaps logits without being the same rows");
     }
     return PR2_OK;

@@ -265,3 +265,15 @@ def test_weight_grad_workspace_does_not_decrease_with_the_rows(n_out, n_in, N, d
 
     sizes = [need(R) for R in [*range(6000), *range(6000, 70000, 371), 2 ** 24, 2 ** 30]]
     assert sizes[0] > 0 and sizes == sorted(sizes)
+
+
+def test_rows_of_logits_and_gradient_between_each_other():
+    """Column parts of one buffer do not overlap; parts that share columns do."""
+    d = policy_desc(ldl=250, ldd=250)
+    for start, status in ((200, None), (300, None), (302, "PR2_ERR_SHAPE"), (198, "PR2_ERR_SHAPE"), (700, None),
+                          (-300, None), (-200, None), (-198, "PR2_ERR_SHAPE"), (500, "PR2_ERR_SHAPE"), (2000, None)):
+        for fn in (loss, loss_backward):
+            got = fn(d, dlogits=P1 + start)
+            assert got in READY if status is None else got == status, start
+    assert loss(policy_desc(ldl=250, ldd=251), dlogits=P1 + 200) == "PR2_ERR_SHAPE"
+    assert loss(policy_desc(ldl=250, ldd=250, T=1), dlogits=P1 + 200) in READY

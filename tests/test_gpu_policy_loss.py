@@ -515,3 +515,23 @@ def test_gradient_from_lse_far_from_zero(T, act, V):
     got = call(logits, host, split=True)
     compare(dict(got, dlogits=None), host, act == BF)
     check_far_gradient(got, host, act == BF, log_p_error=np.abs(got["lse"]) * 2.0 ** -23)
+
+
+@pytest.mark.parametrize("act", [BF, "f32"])
+@pytest.mark.parametrize("T", [7, 210])
+def test_logits_and_gradient_as_column_halves_of_one_buffer(T, act):
+    """Each in its half, at odd starts; the gradient is that of a buffer of its own."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    logits, host = make(13, T, 1001, act)
+    both = torch.full((T, 2051), 7.0, dtype=logits.dtype, device="cuda")
+    z, g = both[:, 1:1002], both[:, 1003:2004]
+    z.copy_(logits)
+    args = [up(host[n]) for n in ("token", "logp_old", "adv")]
+    want = torch.full_like(logits, float("nan"))
+    sums = [torch.empty(4, device="cuda") for _ in range(2)]
+    B.policy_loss(logits, *args, sums[0], dlogits=want)
+    B.policy_loss(z, *args, sums[1], dlogits=g)
+    assert torch.equal(g, want) and torch.equal(z, logits) and torch.equal(*sums)
+    for c in (0, 1002, 2004, 2050):
+        assert torch.all(both[:, c] == 7)
