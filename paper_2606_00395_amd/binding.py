@@ -185,7 +185,7 @@ def _torch():
         except ImportError:
             pass
         else:
-            _args.refuse_with(_need, _need_act)
+            _args.refuse_with(*_PLAIN)
             _need, _need_act = _args.need, _args.need_act
         _ACT_CODES.update({torch.bfloat16: PR2_BF16, torch.float32: PR2_F32})
         _torch_module = torch
@@ -280,6 +280,11 @@ def _need_act(x, name="x"):
     if device.type != "cuda":
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     return shape[0], shape[1], x.dtype, device
+
+
+# The two checks themselves: the names above may stand for the compiled ones already when
+# another thread comes to _torch() at the same time, and those must not come back to themselves.
+_PLAIN = (_need, _need_act)
 
 
 def _need_ws(ws, device):

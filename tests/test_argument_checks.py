@@ -106,3 +106,45 @@ def test_tensors_without_storage_or_strides(plain):
         got, want = outcome(B._need, t, "x", shape, torch.float32, CPU), outcome(plain._need, t, "x", shape, torch.float32, CPU)
         assert got == want and issubclass(got[0], Exception)
         assert outcome(B._need_act, t, "x") == outcome(plain._need_act, t, "x")
+
+
+FIRST_CALLS = """
+import builtins, threading
+import torch
+from paper_2606_00395_amd import binding as B
+
+both = threading.Barrier(2)
+plain_import = builtins.__import__
+
+def slow_import(name, *args, **kw):
+    if name == "torch":         # both threads are inside before either goes on
+        try:
+            both.wait(timeout=5)
+        except threading.BrokenBarrierError:
+            pass
+    return plain_import(name, *args, **kw)
+
+builtins.__import__ = slow_import
+threads = [threading.Thread(target=B._torch) for _ in range(2)]
+for t in threads:
+    t.start()
+for t in threads:
+    t.join()
+builtins.__import__ = plain_import
+for call in (lambda: B._need(torch.zeros(3), "x", (4,)), lambda: B._need_act(torch.zeros(3), "x")):
+    try:
+        call()
+    except ValueError as e:
+        print("refused:", e)
+"""
+
+
+def test_first_calls_from_two_threads():
+    """Threads that come to the binding first at the same time; in a process of its own, since a
+    check that comes back to itself ends it."""
+    import subprocess
+    import sys
+    root = os.path.dirname(B.HERE)
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, stdout=subprocess.PIPE,
+                       stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.count("refused:") == 2, (r.returncode, r.stdout[-500:])
