@@ -3,6 +3,8 @@
 Each translation unit compiles to an object under ``_build/`` in parallel,
 then one shared library is linked next to this file, and beside it the binding's
 compiled argument checks (``_args``, against the installed torch).  Always recompiles.
+The library needs hipcc alone; where the checks do not compile (no g++, no headers of
+the interpreter or of torch), none are left and the binding takes its own in Python.
 """
 from __future__ import annotations
 
@@ -49,6 +51,25 @@ def _args_command(out: str):
             "-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", out]
 
 
+def build_args() -> bool:
+    """Builds ``_args``, or takes an older one away and says why there is none."""
+    tmp = ARGS + ".tmp"
+    try:
+        cmd = _args_command(tmp)
+        rc, out = _run(cmd)
+    except (OSError, ImportError, AttributeError) as e:
+        rc, out = 1, str(e)
+    if rc == 0:
+        os.replace(tmp, ARGS)
+        return True
+    for path in (tmp, ARGS):
+        if os.path.exists(path):
+            os.remove(path)
+    print(out, file=sys.stderr)
+    print("compiled argument checks not built; the binding's Python ones are used", file=sys.stderr)
+    return False
+
+
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     objs = []
@@ -57,16 +78,16 @@ def build(verbose: bool = False) -> str:
         obj = os.path.join(BUILD, src.replace(".hip", ".o"))
         objs.append(obj)
         cmds.append([HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj])
-    cmds.append(_args_command(ARGS + ".tmp"))
-    with ThreadPoolExecutor(len(cmds)) as ex:
+    with ThreadPoolExecutor(len(cmds) + 1) as ex:
+        args = ex.submit(build_args)
         results = list(ex.map(_run, cmds))
+        args.result()
     for cmd, (rc, out) in zip(cmds, results):
         if verbose or rc != 0:
             if out.strip():
                 print(out, file=sys.stderr)
         if rc != 0:
-            raise RuntimeError("compilation failed: " + " ".join(cmd))
-    os.replace(ARGS + ".tmp", ARGS)
+            raise RuntimeError("hipcc failed: " + " ".join(cmd))
     tmp = LIB + ".tmp"
     rc, out = _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs])
     if rc != 0:
