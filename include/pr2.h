@@ -423,8 +423,9 @@ pr2_status pr2_predictor_loss(const pr2_moe_desc* desc, const void* h, const flo
  * A row counts only if w_t != 0, 0 <= y_t < V and some logit of it is above -infinity.  Any
  * other row has loss, logp, entropy and coef 0 and a gradient of zeros, whatever stands in its
  * other inputs (NaN included); its lse is -infinity.  A logit of -infinity (an id that may not
- * be sampled) has probability 0.  NaN or +infinity in a row that counts make that row's
- * results NaN.
+ * be sampled) has probability 0.  NaN or +infinity in the logits of a row that counts make its
+ * logp, lse and entropy NaN and with them whatever is formed from them: with A_t = 0 and no KL
+ * term (logp_ref NULL or kl_coef 0) loss, coef and gradient are not, and stay 0.
  *
  * T rows (>= 0, below 2^25), V vocabulary size (>= 1), ldl and ldd (>= V, at most 2^35) the row
  * strides in elements of logits and dlogits (ldd is read only by calls that write dlogits),
@@ -548,9 +549,10 @@ pr2_status pr2_combine_backward(const pr2_moe_desc* desc, const void* dy, const 
  * exponent field (fp32) of the group's largest magnitude, scale = max(E - 6, 1) and
  *   q = clamp(round_to_even(x 2^(127 - scale)), -127, 127),   value = q 2^(scale - 127):
  * a power of two, so that value is exact in bf16 and fp32 and packing gives the same bits on
- * any machine.  A bf16 group's largest magnitude is held exactly, the others to half a step
- * of 1/64 to 1/128 of it.  A group that holds an infinity or a NaN has scale 255 and q = 0, and
- * all its values are NaN.
+ * any machine.  A step, 2^(scale - 127), is 1/128 to 1/64 of the group's largest magnitude (2^-126
+ * where that is below 2^-120).  x is held to half a step, its largest magnitude too: q has 7 bits, a
+ * bf16 magnitude 8.  An fp32 magnitude above 127.5 steps is cut to 127, up to a whole step.  A group
+ * that holds an infinity or a NaN has scale 255 and q = 0, and all its values are NaN.
  * R >= 0 rows of C >= 1 columns, contiguous; q and scale 16-byte aligned.
  */
 pr2_status pr2_act_pack(int64_t R, int32_t C, int act_dtype, const void* x, int8_t* q,

@@ -452,3 +452,27 @@ def test_one_workspace_for_batches_up_to_the_largest():
         B.weight_grad_packed(dy[:R], q[:R], e[:R], a, ws=ws)
         B.weight_grad_packed(dy[:R], q[:R], e[:R], b)
         assert torch.equal(a, b) and torch.isfinite(a).all(), R
+
+
+@pytest.mark.parametrize("bf16", [True, False], ids=["bf16", "f32"])
+def test_distance_of_the_packed_values(bf16):
+    """Half a step of 1/128 to 1/64 of the group's largest magnitude, which is not exact itself;
+    a whole one for fp32 magnitudes that are cut."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    g = np.random.default_rng(10)
+    x = g.uniform(-1, 1, (200, 96)) * np.exp(g.normal(0, 20, (200, 1)))
+    for r, v in enumerate((1.0078125, 1.9921875, 1.9999, 1.0)):       # every 8-bit and a 24-bit mantissa's ends
+        x[r] = np.where(np.arange(96) % 32 == r, v, v / 3)
+    x[4] = 2.0 ** -127
+    x = act(x, bf16)
+    q, e = do_pack(x)
+    back = torch.empty_like(x)
+    B.act_unpack(q, e, back)
+    v, step = host(x), np.repeat(np.exp2(e.double().cpu().numpy() - 127), 32, axis=1)
+    top = np.repeat(np.abs(v).reshape(200, 3, 32).max(2), 32, axis=1)
+    assert np.all((step >= top / 128) & ((step <= top / 64) | (step == 2.0 ** -126)))
+    off = np.abs(host(back) - v) / step
+    cut = np.abs(v) > 127.5 * step
+    assert np.all(off[~cut] <= 0.5) and np.all(off[cut] < 1) and (not bf16 or not cut.any())
+    assert host(back)[0, 0] == 1.0 and host(back)[1, 1] == 1.984375

@@ -535,3 +535,23 @@ def test_logits_and_gradient_as_column_halves_of_one_buffer(T, act):
     assert torch.equal(g, want) and torch.equal(z, logits) and torch.equal(*sums)
     for c in (0, 1002, 2004, 2050):
         assert torch.all(both[:, c] == 7)
+
+
+@pytest.mark.parametrize("split", [False, True], ids=["one_call", "two_calls"])
+@pytest.mark.parametrize("T,V", [(4, 1500), (220, 1500), (4, 80003)])
+def test_nan_logits_under_an_advantage_of_zero(T, V, split):
+    """Neither loss nor gradient depends on the row then, and neither is NaN; what does is."""
+    logits, host = make(14, T, V, BF)
+    logits[1, 700], logits[2, 3] = float("nan"), float("inf")
+    host["adv"][1:3] = 0.0
+    for ref, beta in ((None, 0.0), (host["logp_ref"], 0.0)):
+        host.update(logp_ref=ref, kl_coef=beta)
+        got = call(logits, host, split=split)
+        assert np.isnan(got["logp"][1:3]).all() and np.isnan(got["lse"][1:3]).all()
+        assert np.isnan(got["entropy"][1:3]).all() and np.isnan(got["sums"][3])
+        assert np.all(got["coef"][1:3] == 0) and np.all(got["dlogits"][1:3] == 0)
+        assert np.isfinite(got["sums"][0]) and np.isnan(got["sums"][1]) == (ref is not None)
+        assert np.isfinite(got["dlogits"]).all()
+    host["kl_coef"] = 0.1
+    got = call(logits, host, split=split)
+    assert np.isnan(got["coef"][1:3]).all() and np.isnan(got["dlogits"][1:3]).all() and np.isnan(got["sums"][0])
