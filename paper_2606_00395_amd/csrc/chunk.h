@@ -1,4 +1,5 @@
-// Rows of bf16 or fp32 elements in pieces of 16 bytes, at any element's address.
+// Rows of bf16 or fp32 elements in pieces of 16 bytes, at any element's address, and grids for
+// any number of rows.
 #pragma once
 
 #include "common.h"
@@ -103,5 +104,15 @@ __device__ __forceinline__ void store_chunk(T* row, int c, int full, int rem, co
             if (i < rem) row[(int64_t)c * E + i] = Act<T>::from_f32(v[i]);
     }
 }
+
+// Grids of n workgroups (below 2^31) of `threads`, over two dimensions where one does not hold
+// them: HIP cuts a dimension of more than 2^32 work-items off without an error.  A kernel asks
+// block_number() which workgroup it is and has nothing to do from the n-th on.
+inline dim3 wide_grid(int64_t n, int threads) {
+    const int64_t most = ((int64_t)1 << 31) / threads;
+    const int64_t x = n < most ? n : most;
+    return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+__device__ __forceinline__ uint32_t block_number() { return blockIdx.x + blockIdx.y * gridDim.x; }
 
 }  // namespace pr2

@@ -170,16 +170,6 @@ pr2_status check_route_args(const pr2_moe_desc* desc, const void* x, const float
                             int64_t ldi, float* gate_out, float* logits_out, bool* empty);
 
 // ------------------------------------------------------------ launches ----
-// Grids of n workgroups (below 2^31) of `threads`, over two dimensions where one does not hold
-// them: HIP cuts a dimension of more than 2^32 work-items off without an error.  A kernel asks
-// block_number() which workgroup it is and has nothing to do from the n-th on.
-inline dim3 wide_grid(int64_t n, int threads) {
-    const int64_t most = ((int64_t)1 << 31) / threads;
-    const int64_t x = n < most ? n : most;
-    return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
-}
-__device__ __forceinline__ uint32_t block_number() { return blockIdx.x + blockIdx.y * gridDim.x; }
-
 // Every launch goes through this so that measurement events can bracket it.
 struct LaunchScope {
     LaunchScope(const char* name, hipStream_t s);
