@@ -590,7 +590,8 @@ typedef struct {
     int32_t n_out, n_in, N, k;
     int32_t act_dtype;
 } pr2_wgrad_desc;
-/* 0 for an invalid descriptor.  Does not decrease with R. */
+/* Bytes of workspace that pr2_weight_grad_packed needs (0 where R, N, n_out or n_in is out of its
+ * range, which the call then reports).  Does not decrease with R. */
 size_t pr2_weight_grad_workspace_bytes(const pr2_wgrad_desc* desc);
 pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, const int8_t* q,
                                   const uint8_t* scale, const int32_t* offsets,

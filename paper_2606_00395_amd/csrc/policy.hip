@@ -28,6 +28,8 @@ struct Stat {
     float m, s, e;
 };
 
+// One instruction, a relative error of 2^-22 or so; powers below 2^-126 are 0: a probability that is
+// subnormal in fp32 has a gradient of 0.
 __device__ __forceinline__ float exp2_native(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // moves the terms to the maximum m (>= a.m); exponents are cut off where their power is 0
@@ -501,10 +503,16 @@ int row_parts(const pr2_policy_desc& d) {
 constexpr int64_t kStreamBytes = 32 << 20;
 
 // Long rows, a whole CU each in the fused form, are better read twice by many workgroups while
-// they are few: loss and gradient of 151936 bf16 logits take 16, 23 and 38.5 us in 1, 64 and
-// 191 rows that way, 25, 32 and 40 fused; 256 rows 46 and 46, 2048 rows 343 and 266.  Shorter
-// rows are faster fused at any count (32000 logits: 13 against 16 us for one row, 63 against
-// 77 for 2048).
+// they are few.  Read twice and fused, us, loss and gradient of
+//              32 rows      64          128         192         256         512
+//   151936 bf16  18.8 28.3    23.2 29.6   29.6 31.6   38.5 32.9   44.8 35.0   75.7 74.7
+//    80000 bf16  16.2 26.1    18.3 26.9   22.6 28.5   28.1 29.7   29.5 30.8   47.1 54.8
+//   151936 fp32  20.8 31.1    26.4 37.4   42.9 40.1   57.7 47.8   70.6 65.5   157 160
+//    76000 fp32  17.4 18.5    22.0 20.0   26.6 22.1   35.9 26.0   43.0 30.6   69.9 68.5
+//    50257 fp32  16.0 17.7    18.4 18.7   23.5 20.5   27.2 22.8   33.3 25.2   52.0 43.6
+// so they are even near 140, above 512, 115, 45 and 75 rows.  One limit stands for all, which gives
+// away up to 10 us just below it in fp32 and 8 us at 512 rows of 80000.  Shorter rows are faster
+// fused at any count (32000 logits: 13 against 16 us for one row, 63 against 77 for 2048).
 constexpr int64_t kFewRows = 192;
 bool fuse_rows(const pr2_policy_desc& d) { return d.T >= kFewRows || row_chunks(d) <= kShortRow; }
 

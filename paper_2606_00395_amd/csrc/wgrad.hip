@@ -173,9 +173,9 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
 // is zeros in both operands, since a zero of one would turn an infinity of the other into NaN.
 // A workgroup goes through several tiles of the same rows of dy: the row indexes stay, and
 // the next tile's first steps are fetched before this one's outputs are stored.
-// 128 experts of 1536 x 2048 over 131072 rows take 975-1020 us with the packing (810-845 TFLOP/s; the library's
-// product of that size and layout, with one shared output, reaches 822): 770 in the steps, the
-// MFMA units 42-48 % busy at the clock that the power limit leaves, and 7 us per tile for its
+// 128 experts of 1536 x 2048 over 131072 rows take 955-990 us (833-863 TFLOP/s; the library's
+// product of that size and layout, with one shared output, reaches 822): 775 in the steps, the
+// MFMA units 42-48 % busy at the clock that the power limit leaves, and 8 us per tile for its
 // 256 KB of outputs.  Two workgroups a CU with tiles of 256 x 128, so that one stores while
 // the other multiplies, took 1120.
 constexpr int BM = 256, BN = 256;
@@ -204,7 +204,8 @@ __device__ __forceinline__ void wait_vmcnt() {
 
 // Byte j of q as a signed number, in one instruction.  (A cast is left as shifts, bit-field
 // extracts and conversions, and the kernel below spills 320 registers; with the sign carried as
-// 128 and taken off again it takes 1006 us where this takes 960: 128 experts of 1536 x 2048.)
+// 128 and taken off again it takes 1006 us where this, run in turn, takes 960: 128 experts of 1536 x
+// 2048.)
 template <int j>
 __device__ __forceinline__ float signed_byte(uint32_t q) {
     float f;
