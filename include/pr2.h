@@ -598,6 +598,103 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
                                   const int32_t* route_of_row, float* dW, void* ws,
                                   size_t ws_bytes, pr2_stream_t stream);
 
+/*
+ * The same from x itself: x [Rx, n_in] of dy's type, 16-byte aligned, in the place of (q, scale).
+ * bf16: MFMA with fp32 accumulation; fp32: fp32 products and sums.  Same workspace.
+ */
+pr2_status pr2_weight_grad(const pr2_wgrad_desc* desc, const void* dy, const void* x,
+                           const int32_t* offsets, const int32_t* route_of_row, float* dW, void* ws,
+                           size_t ws_bytes, pr2_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Products of rows sorted by expert with their experts' weights (desc as for the weight gradients;
+ * act_dtype of x, W and out), for experts of the caller's own behind the recorded routes.
+ *   out[r, :] = x[src(r), :] W[e]^T        for the rows r of expert e, offsets[e] .. offsets[e + 1)
+ *   x [Rx, n_in], W [N, n_out, n_in], out [R, n_out], 16-byte aligned, out apart from x and W
+ * with src(r) as above: the token of row r's route (x is then read through the plan and need not be
+ * dispatched), or r itself where route_of_row is NULL (then R <= Rx).  offsets NULL (then N = 1): one
+ * weight for all rows.  A row whose route_of_row is outside [0, k Rx) and the rows from offsets[N] on
+ * are written as zeros.  offsets[0] is 0 and offsets rise to at most R (others give unspecified rows,
+ * no access out of bounds).  R = 0 is a no-op.  NaN and infinities reach the rows and columns that
+ * they are terms of, no others.
+ * Sums in fp32, one rounding to act_dtype at the end; bf16 products are exact.  N <= 1024, R and Rx
+ * below 2^31 - 1024, n_out and n_in at most 2^20, N n_out n_in at most 2^36.  No workspace.  The same
+ * call gives the same bits.
+ */
+pr2_status pr2_grouped_mm(const pr2_wgrad_desc* desc, const void* x, const void* W,
+                          const int32_t* offsets, const int32_t* route_of_row, void* out,
+                          pr2_stream_t stream);
+/* The gradient of the rows: dx[r, :] = dy[r, :] W[e], dy [R, n_out], dx [R, n_in]; zeros from
+ * offsets[N] on.  (Where the product read x through the plan, pr2_dispatch_backward sums a token's
+ * rows of dx.  The weights' gradient is pr2_weight_grad.)  desc.Rx and k are not read. */
+pr2_status pr2_grouped_mm_backward(const pr2_wgrad_desc* desc, const void* dy, const void* W,
+                                   const int32_t* offsets, void* dx, pr2_stream_t stream);
+
+/*
+ * The product in 8 bits, for a rollout whose weights stay fixed:
+ *   out[r, o] = ((float)(sum_c q[src(r), c] Wq[e, o, c]) row_scale[src(r)]) w_scale[e, o]
+ *   q [Rx, n_in] int8, row_scale [Rx] fp32;  Wq [N, n_out, n_in] int8, w_scale [N, n_out] fp32
+ *   out [R, n_out] of act_dtype
+ * The sum is exact (int32; n_in below 2^17), then rounded to fp32, as is each product with a scale.
+ * Otherwise as pr2_grouped_mm.
+ */
+pr2_status pr2_grouped_mm_quant(const pr2_wgrad_desc* desc, const int8_t* q, const float* row_scale,
+                                const int8_t* Wq, const float* w_scale, const int32_t* offsets,
+                                const int32_t* route_of_row, void* out, pr2_stream_t stream);
+
+/*
+ * Rows in 8 bits with one scale each (the row form), of x [R, C] act_dtype: with m the row's largest
+ * magnitude
+ *   row_scale = fp32(max(m, 2^-100) / 127),  q = rint(x / row_scale)  in [-127, 127],
+ * the quotient as in exact arithmetic, ties to even, so that q row_scale is x to half of row_scale.  A row that
+ * holds an infinity or a NaN has row_scale NaN and q = 0.  Weights [N, n_out, n_in] brought to
+ * this form as N n_out rows are what pr2_grouped_mm_quant reads as Wq and w_scale.
+ *   q [R, C] int8, x 16-byte aligned;  row_scale [R] fp32
+ */
+pr2_status pr2_act_quant(int64_t R, int32_t C, int act_dtype, const void* x, int8_t* q,
+                         float* row_scale, pr2_stream_t stream);
+/* The row form of silu(a) u (fp32, not rounded in between), au [R, 2m] as for pr2_swiglu_pack;
+ * q [R, m]. */
+pr2_status pr2_swiglu_quant(int64_t R, int32_t m, int act_dtype, const void* au, int8_t* q,
+                            float* row_scale, pr2_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Root-mean-square norm in front of the layer, the residual's addition in the same pass.
+ *   h = round(x + residual)  (the sum in fp32; x itself without residual),  r = (mean_i h_i^2 + eps)^(-1/2),
+ *   y_i = round(h_i r w_i)                                  round: to act_dtype
+ *   x, residual [T, d] act_dtype; weight [d] fp32; residual may be NULL
+ *   h_out [T, d], y [T, d] act_dtype; rstd_out [T] fp32 (what the backward call reads)
+ *   q [T, d] int8 with scale [T, ceil(d / 32)] uint8: the packed form of y, the bits of pr2_act_pack
+ *   q [T, d] int8 with row_scale [T] fp32: the row form of h r w (not rounded to act_dtype), q that of
+ *     fp32(h w) under pr2_act_quant and row_scale = r times its scale
+ * Each output may be NULL, q goes with one of scale and row_scale.  h_out and y may lie on x or
+ * residual (not both on the same); other overlaps are not allowed.  d <= 32768, T < 2^31, 16-byte
+ * alignment of all but the fp32 tensors.  Sums in fp32: rows whose mean h^2 passes fp32's range
+ * (magnitudes near 2^64) get r = 0.  A NaN or an infinity in a row reaches that row alone.  T = 0 is
+ * a no-op.
+ */
+pr2_status pr2_rms_norm(int64_t T, int32_t d, int act_dtype, float eps, const void* x,
+                        const void* residual, const float* weight, void* h_out, void* y,
+                        float* rstd_out, int8_t* q, uint8_t* scale, float* row_scale,
+                        pr2_stream_t stream);
+
+/* Bytes of workspace for the gradient of the weight (0 where T or d is out of its range).  Does not
+ * decrease with T. */
+size_t pr2_rms_norm_workspace_bytes(int64_t T, int32_t d);
+/*
+ * Its gradients, from h (x where there was no residual) and rstd:
+ *   g = dy w,  dx = round(dh + r (g - h r^2 mean_i(g_i h_i))),  dweight = sum_t dy_t h_t r_t
+ *   dy, h, dx [T, d] act_dtype; dh [T, d] or NULL: the gradient that reaches h beside the norm (its
+ *   use as the residual stream).  dx is the gradient of x and of residual alike; it may be dy, dh or h.
+ *   dweight [d] fp32, overwritten, or NULL when not wanted (then no workspace is needed)
+ *   ws >= pr2_rms_norm_workspace_bytes(T, d)
+ * A row's gradient depends on that row alone.  Sums over rows in fp32 in a fixed order.  T = 0 writes
+ * zeros to dweight.
+ */
+pr2_status pr2_rms_norm_backward(int64_t T, int32_t d, int act_dtype, const void* dy, const void* dh,
+                                 const void* h, const float* rstd, const float* weight, void* dx,
+                                 float* dweight, void* ws, size_t ws_bytes, pr2_stream_t stream);
+
 /* Status name ("PR2_OK", ...); never NULL. */
 const char* pr2_status_string(pr2_status s);
 /* Detail of the last error on this thread ("" if none); valid until the next call. */

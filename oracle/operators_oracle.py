@@ -180,3 +180,46 @@ def weight_grad(dy, x, offsets=None, route_of_row=None, k=1):
         out[e] = dy[rows].T @ x[src[rows]]
         mag[e] = np.abs(dy[rows]).T @ np.abs(x[src[rows]])
     return out, mag
+
+
+def grouped_mm(x, W, offsets=None, route_of_row=None, k=1, rows=None):
+    """out [R, n_out] and the sums of the terms' magnitudes (zeros for a row of no expert or without
+    a source)."""
+    x, W = np.asarray(x, dtype=np.float64), np.asarray(W, dtype=np.float64)
+    R = len(route_of_row) if route_of_row is not None else (x.shape[0] if rows is None else rows)
+    offsets = [0, R] if offsets is None else list(offsets)
+    out = np.zeros((R, W.shape[1]))
+    mag = np.zeros_like(out)
+    for e in range(len(offsets) - 1):
+        for r in range(offsets[e], offsets[e + 1]):
+            src = r if route_of_row is None else (route_of_row[r] // k if route_of_row[r] >= 0 else -1)
+            if 0 <= src < x.shape[0]:
+                out[r] = W[e] @ x[src]
+                mag[r] = np.abs(W[e]) @ np.abs(x[src])
+    return out, mag
+
+
+def grouped_mm_backward(dy, W, offsets=None):
+    """dx [R, n_in] and the sums of the terms' magnitudes."""
+    return grouped_mm(dy, np.swapaxes(np.asarray(W, dtype=np.float64), 1, 2), offsets)
+
+
+def rms_norm(h, weight, eps):
+    """y and rstd."""
+    h = np.asarray(h, dtype=np.float64)
+    rstd = 1 / np.sqrt(np.mean(h * h, axis=1) + eps)
+    return h * rstd[:, None] * weight, rstd
+
+
+def rms_norm_backward(dy, h, rstd, weight, dh=None):
+    """dx, dweight."""
+    n = h * rstd[:, None]
+    g = dy * weight
+    dx = rstd[:, None] * (g - n * np.mean(g * n, axis=1, keepdims=True))
+    return dx if dh is None else dx + dh, np.sum(dy * n, axis=0)
+
+
+def row_scale(v):
+    """The step of each row's form in 8 bits."""
+    m = np.max(np.abs(np.asarray(v, dtype=np.float64)), axis=1)
+    return np.where(np.isfinite(m), np.maximum(m, 2.0 ** -100) / 127, np.nan)

@@ -38,7 +38,9 @@ EXPORTS = ["pr2_workspace_bytes", "pr2_route_predict", "pr2_route_predict_reuse"
            "pr2_policy_loss_backward", "pr2_dispatch_plan", "pr2_dispatch",
            "pr2_dispatch_backward", "pr2_combine", "pr2_combine_backward", "pr2_act_pack",
            "pr2_act_unpack", "pr2_swiglu_pack", "pr2_swiglu_backward_packed",
-           "pr2_weight_grad_workspace_bytes", "pr2_weight_grad_packed",
+           "pr2_weight_grad_workspace_bytes", "pr2_weight_grad_packed", "pr2_weight_grad",
+           "pr2_grouped_mm", "pr2_grouped_mm_backward", "pr2_grouped_mm_quant", "pr2_act_quant",
+           "pr2_swiglu_quant", "pr2_rms_norm", "pr2_rms_norm_workspace_bytes", "pr2_rms_norm_backward",
            "pr2_status_string",
            "pr2_last_error", "pr2_version", "pr2_profile_enable",
            "pr2_profile_reset", "pr2_profile_collect"]
@@ -132,13 +134,23 @@ def lib() -> ctypes.CDLL:
             ("pr2_act_unpack", [c_int64, c_int32, c_int, P, P, P, P]),
             ("pr2_swiglu_pack", [c_int64, c_int32, c_int, P, P, P, P, P]),
             ("pr2_swiglu_backward_packed", [c_int64, c_int32, c_int, P, P, P, P, P, P]),
-            ("pr2_weight_grad_packed", [POINTER(WgradDesc)] + [P] * 7 + [c_size_t, P])):
+            ("pr2_weight_grad_packed", [POINTER(WgradDesc)] + [P] * 7 + [c_size_t, P]),
+            ("pr2_weight_grad", [POINTER(WgradDesc)] + [P] * 6 + [c_size_t, P]),
+            ("pr2_grouped_mm", [POINTER(WgradDesc)] + [P] * 6),
+            ("pr2_grouped_mm_backward", [POINTER(WgradDesc)] + [P] * 5),
+            ("pr2_grouped_mm_quant", [POINTER(WgradDesc)] + [P] * 8),
+            ("pr2_act_quant", [c_int64, c_int32, c_int, P, P, P, P]),
+            ("pr2_swiglu_quant", [c_int64, c_int32, c_int, P, P, P, P]),
+            ("pr2_rms_norm", [c_int64, c_int32, c_int, c_float] + [P] * 10),
+            ("pr2_rms_norm_backward", [c_int64, c_int32, c_int] + [P] * 8 + [c_size_t, P])):
         getattr(L, name).argtypes = args
         getattr(L, name).restype = c_int
     L.pr2_policy_workspace_bytes.argtypes = [POINTER(PolicyDesc)]
     L.pr2_policy_workspace_bytes.restype = c_size_t
     L.pr2_weight_grad_workspace_bytes.argtypes = [POINTER(WgradDesc)]
     L.pr2_weight_grad_workspace_bytes.restype = c_size_t
+    L.pr2_rms_norm_workspace_bytes.argtypes = [c_int64, c_int32]
+    L.pr2_rms_norm_workspace_bytes.restype = c_size_t
     L.pr2_status_string.argtypes = [c_int]
     L.pr2_status_string.restype = c_char_p
     L.pr2_last_error.argtypes = []
@@ -980,6 +992,179 @@ def weight_grad_packed(dy, q, scale, dW, offsets=None, route_of_row=None, k=1, w
         ws = _new_ws(L.pr2_weight_grad_workspace_bytes(desc), dev, stream)
     check(L.pr2_weight_grad_packed(desc, dy.data_ptr(), q, scale, offsets, route_of_row, dW,
                                    ws.data_ptr(), ws.numel(), _stream(stream)))
+
+
+def weight_grad(dy, x, dW, offsets=None, route_of_row=None, k=1, ws=None, stream=None):
+    """pr2_weight_grad on torch tensors: dW [N, n_out, n_in] from dy [R, n_out] and x [Rx, n_in] as
+    they are; ``offsets`` and ``route_of_row`` as in weight_grad_packed, whose workspace serves here
+    too."""
+    R, n_out, adt, dev = _need_act(dy, "dy")
+    Rx, n_in, _, _ = _need_act(x)
+    x = _need(x, "x", (Rx, n_in), adt, dev)
+    N, offsets, route_of_row = _row_plan(offsets, route_of_row, R, dev)
+    dW = _need(dW, "dW", (N, n_out, n_in), _torch().float32, dev)
+    L, desc = lib(), byref(WgradDesc(R, Rx, n_out, n_in, N, k, _ACT_CODES[adt]))
+    ws = _need_ws(ws, dev)
+    if ws is None:
+        ws = _new_ws(L.pr2_weight_grad_workspace_bytes(desc), dev, stream)
+    check(L.pr2_weight_grad(desc, dy.data_ptr(), x, offsets, route_of_row, dW, ws.data_ptr(),
+                            ws.numel(), _stream(stream)))
+
+
+# ------------------------------------------- products of rows sorted by expert --
+
+def _here(device):
+    """The call runs on the current device: tensors of another one are refused."""
+    if device.index is not None and device.index != _raw_device_index():
+        raise ValueError(f"tensors are on {device}, the current device is cuda:{_raw_device_index()}")
+
+
+def _raw_device_index():
+    return _raw_device() if _raw_device is not None else _torch().cuda.current_device()
+
+
+def _row_plan(offsets, route_of_row, R, device):
+    """N and the addresses of offsets and route_of_row as dispatch_plan writes them (each may be
+    missing; without offsets there is one weight)."""
+    torch = _torch()
+    _here(device)
+    N = 1
+    if offsets is not None:
+        shape = offsets.shape
+        if len(shape) != 1 or shape[0] < 2:
+            raise ValueError("offsets must be 1-D [N + 1]")
+        N = shape[0] - 1
+        offsets = _need(offsets, "offsets", shape, torch.int32, device)
+    return N, offsets, _need(route_of_row, "route_of_row", (R,), torch.int32, device, True)
+
+
+def _weights(W, N, columns, axis, dtype, device, name="W"):
+    """n_out, n_in and the address of W [N, n_out, n_in], whose dimension ``axis`` is ``columns``."""
+    shape = W.shape
+    if len(shape) != 3 or shape[0] != N or shape[axis] != columns:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [{N}, "
+                         + (f"{columns}, n_in]" if axis == 1 else f"n_out, {columns}]"))
+    return shape[1], shape[2], _need(W, name, shape, dtype, device)
+
+
+def grouped_mm(x, W, out, offsets=None, route_of_row=None, k=1, stream=None):
+    """pr2_grouped_mm on torch tensors: out [R, n_out] = the rows of x [Rx, n_in] times their experts'
+    W [N, n_out, n_in]^T; ``offsets`` [N + 1] and ``route_of_row`` [R] (with the layer's ``k``) as
+    dispatch_plan writes them.  With ``route_of_row``, x holds tokens and is read through the plan;
+    without, sorted rows.  Without ``offsets``, W is one weight [1, n_out, n_in] for all rows."""
+    Rx, n_in, adt, dev = _need_act(x)
+    R = out.shape[0] if out.dim() == 2 else -1
+    N, offsets, route_of_row = _row_plan(offsets, route_of_row, R, dev)
+    n_out, n_in, W = _weights(W, N, n_in, 2, adt, dev)
+    out = _need(out, "out", (R, n_out), adt, dev)
+    check(lib().pr2_grouped_mm(byref(WgradDesc(R, Rx, n_out, n_in, N, k, _ACT_CODES[adt])), x.data_ptr(), W,
+                               offsets, route_of_row, out, _stream(stream)))
+
+
+def grouped_mm_backward(dy, W, dx, offsets=None, stream=None):
+    """pr2_grouped_mm_backward on torch tensors: dx [R, n_in] = the rows of dy [R, n_out] times their
+    experts' W [N, n_out, n_in] (the gradient of the rows that grouped_mm read; weight_grad forms
+    that of W)."""
+    R, n_out, adt, dev = _need_act(dy, "dy")
+    N, offsets, _ = _row_plan(offsets, None, R, dev)
+    n_out, n_in, W = _weights(W, N, n_out, 1, adt, dev)
+    dx = _need(dx, "dx", (R, n_in), adt, dev)
+    check(lib().pr2_grouped_mm_backward(byref(WgradDesc(R, R, n_out, n_in, N, 1, _ACT_CODES[adt])), dy.data_ptr(),
+                                        W, offsets, dx, _stream(stream)))
+
+
+def _quantised(q, row_scale, R, C, device):
+    torch = _torch()
+    return (_need(q, "q", (R, C), torch.int8, device),
+            _need(row_scale, "row_scale", (R,), torch.float32, device))
+
+
+def grouped_mm_quant(q, row_scale, Wq, w_scale, out, offsets=None, route_of_row=None, k=1, stream=None):
+    """pr2_grouped_mm_quant on torch tensors: grouped_mm of rows q int8 [Rx, n_in] with row_scale fp32
+    [Rx] (as act_quant, swiglu_quant and rms_norm write them) and weights Wq int8 [N, n_out, n_in]
+    with w_scale fp32 [N, n_out]; out is bf16 or fp32."""
+    torch = _torch()
+    R, columns, adt, dev = _need_act(out, "out")
+    if q.dim() != 2:
+        raise ValueError("q must be 2-D [Rx, n_in]")
+    Rx, n_in = q.shape
+    q, row_scale = _quantised(q, row_scale, Rx, n_in, dev)
+    N, offsets, route_of_row = _row_plan(offsets, route_of_row, R, dev)
+    n_out, n_in, Wq = _weights(Wq, N, n_in, 2, torch.int8, dev, "Wq")
+    w_scale = _need(w_scale, "w_scale", (N, n_out), torch.float32, dev)
+    out = _need(out, "out", (R, n_out), adt, dev)
+    check(lib().pr2_grouped_mm_quant(byref(WgradDesc(R, Rx, n_out, n_in, N, k, _ACT_CODES[adt])), q, row_scale, Wq,
+                                     w_scale, offsets, route_of_row, out, _stream(stream)))
+
+
+def act_quant(x, q, row_scale, stream=None):
+    """pr2_act_quant on torch tensors: x [R, C] to q int8 [R, C] and row_scale fp32 [R]."""
+    R, C, adt, dev = _need_act(x)
+    _here(dev)
+    q, row_scale = _quantised(q, row_scale, R, C, dev)
+    check(lib().pr2_act_quant(R, C, _ACT_CODES[adt], x.data_ptr(), q, row_scale, _stream(stream)))
+
+
+def swiglu_quant(au, q, row_scale, stream=None):
+    """pr2_swiglu_quant on torch tensors: silu(a) u of au [R, 2m] to q int8 [R, m] and row_scale
+    fp32 [R]."""
+    R, C, adt, dev = _need_act(au, "au")
+    if C % 2:
+        raise ValueError("au must hold a and u, [R, 2m]")
+    _here(dev)
+    q, row_scale = _quantised(q, row_scale, R, C // 2, dev)
+    check(lib().pr2_swiglu_quant(R, C // 2, _ACT_CODES[adt], au.data_ptr(), q, row_scale, _stream(stream)))
+
+
+# ------------------------------------------------------ norm before the layer --
+
+def rms_norm(x, weight, y=None, residual=None, h_out=None, rstd_out=None, q=None, scale=None,
+             row_scale=None, eps=1e-6, stream=None):
+    """pr2_rms_norm on torch tensors: y [T, d] = the norm of h = x + ``residual`` times ``weight`` fp32
+    [d]; ``h_out`` [T, d] receives h, ``rstd_out`` fp32 [T] what rms_norm_backward reads, ``q`` int8
+    [T, d] the 8-bit form of the output: with ``scale`` (uint8 [T, ceil(d / 32)]) that of act_pack,
+    with ``row_scale`` (fp32 [T]) that of act_quant.  Outputs not given are not formed."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(x)
+    _here(dev)
+    f, rows, full = torch.float32, (T,), (T, d)
+    weight = _need(weight, "weight", (d,), f, dev)
+    residual = _need(residual, "residual", full, adt, dev, True)
+    h_out = _need(h_out, "h_out", full, adt, dev, True)
+    y = _need(y, "y", full, adt, dev, True)
+    rstd_out = _need(rstd_out, "rstd_out", rows, f, dev, True)
+    q = _need(q, "q", full, torch.int8, dev, True)
+    scale = _need(scale, "scale", (T, -(-d // PACK_GROUP)), torch.uint8, dev, True)
+    row_scale = _need(row_scale, "row_scale", rows, f, dev, True)
+    check(lib().pr2_rms_norm(T, d, _ACT_CODES[adt], eps, x.data_ptr(), residual, weight, h_out, y, rstd_out, q,
+                             scale, row_scale, _stream(stream)))
+
+
+def rms_norm_workspace(dy, stream=None):
+    """A workspace for rms_norm_backward over up to dy.shape[0] rows."""
+    T, d, _, dev = _need_act(dy, "dy")
+    return _new_ws(int(lib().pr2_rms_norm_workspace_bytes(T, d)), dev, stream)
+
+
+def rms_norm_backward(dy, h, rstd, weight, dx, dh=None, dweight=None, ws=None, stream=None):
+    """pr2_rms_norm_backward on torch tensors: dx [T, d] (the gradient of x and of the residual; may
+    be ``dy``, ``dh`` or ``h``) and ``dweight`` fp32 [d] from dy, h and rstd; ``dh`` is the gradient that reaches h
+    beside the norm."""
+    torch = _torch()
+    T, d, adt, dev = _need_act(dy, "dy")
+    _here(dev)
+    f, full = torch.float32, (T, d)
+    h = _need(h, "h", full, adt, dev)
+    rstd = _need(rstd, "rstd", (T,), f, dev)
+    weight = _need(weight, "weight", (d,), f, dev)
+    dx = _need(dx, "dx", full, adt, dev)
+    dh = _need(dh, "dh", full, adt, dev, True)
+    dweight = _need(dweight, "dweight", (d,), f, dev, True)
+    ws = _need_ws(ws, dev)
+    if ws is None and dweight is not None:
+        ws = _new_ws(lib().pr2_rms_norm_workspace_bytes(T, d), dev, stream)
+    check(lib().pr2_rms_norm_backward(T, d, _ACT_CODES[adt], dy.data_ptr(), dh, h, rstd, weight, dx, dweight,
+                                      _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 # ------------------------------------------------------ measurement hooks --

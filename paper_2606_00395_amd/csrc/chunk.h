@@ -115,4 +115,10 @@ inline dim3 wide_grid(int64_t n, int threads) {
 }
 __device__ __forceinline__ uint32_t block_number() { return blockIdx.x + blockIdx.y * gridDim.x; }
 
+// whether two tensors share memory (null: no tensor); same_allowed: other than by being the same one
+inline bool share_memory(const void* p, size_t n, const void* q, size_t m, bool same_allowed = false) {
+    const uintptr_t a = (uintptr_t)p, b = (uintptr_t)q;
+    return p && q && a < b + m && b < a + n && !(same_allowed && a == b);
+}
+
 }  // namespace pr2

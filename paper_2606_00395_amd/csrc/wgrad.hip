@@ -1,5 +1,5 @@
-// Weight gradients whose input operand is an 8-bit checkpoint:
-//   dW[e] [n_out, n_in] = sum over expert e's rows r of dy[r]^T value(x)[src(r)],
+// Weight gradients of linear layers, their input rows as they are or as an 8-bit checkpoint:
+//   dW[e] [n_out, n_in] = sum over expert e's rows r of dy[r]^T x[src(r)],
 // src(r) the token of row r's route, or r itself.
 //
 // A packed value is an int8 times a power of two, exact in bf16 and fp32, so nothing is
@@ -14,8 +14,9 @@ namespace {
 
 struct WgradArgs {
     const void* dy;             // [R, n_out]
-    const int8_t* q;            // [Rx, n_in]
+    const int8_t* q;            // [Rx, n_in]; null: x is not packed
     const uint8_t* scale;       // [Rx, groups]
+    const void* x;              // [Rx, n_in] as dy, where it is not packed
     const int* offsets;         // [N + 1] or null (one weight over all rows)
     const int* route;           // [R] or null
     float* dW;                  // [N, n_out, n_in]
@@ -91,7 +92,7 @@ __device__ __forceinline__ uint64_t load8_packed(const int8_t* row, int c, int n
     return w;
 }
 
-template <typename T>
+template <typename T, bool PACKED>
 __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
     __shared__ __attribute__((aligned(16))) float A[kStep * kTilePitch], B[kStep * kTilePitch];
     const int tid = threadIdx.x;
@@ -110,10 +111,10 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
     // step before.  Columns past the matrix hold anything, they reach only outputs that are
     // not stored.
     constexpr int E = Chunk<T>::E;
-    const bool whole = o0 + kTile <= a.n_out;
-    u32x4 wa[8 / E];
-    uint64_t wb;
-    uint32_t byte;
+    const bool whole = o0 + kTile <= a.n_out, whole_x = c0 + kTile <= a.n_in;
+    u32x4 wa[8 / E], wx[8 / E];
+    uint64_t wb = 0;
+    uint32_t byte = 0;
     bool on;
     auto fetch = [&](int r0) __attribute__((always_inline)) {
         const int r = min(r0 + sr, last - 1);
@@ -123,8 +124,14 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         const T* row = (const T*)a.dy + (int64_t)r * a.n_out;
         if (whole) load8<T, true>(row, o0 + sc, a.n_out, wa);
         else load8<T, false>(row, o0 + sc, a.n_out, wa);
-        wb = load8_packed(a.q + xr * a.n_in, c0 + sc, a.n_in);
-        byte = a.scale[xr * a.groups + min(c0 + sc, a.n_in - 1) / 32];
+        if (PACKED) {
+            wb = load8_packed(a.q + xr * a.n_in, c0 + sc, a.n_in);
+            byte = a.scale[xr * a.groups + min(c0 + sc, a.n_in - 1) / 32];
+        } else {
+            const T* from = (const T*)a.x + xr * a.n_in;
+            if (whole_x) load8<T, true>(from, c0 + sc, a.n_in, wx);
+            else load8<T, false>(from, c0 + sc, a.n_in, wx);
+        }
     };
     const int ao = 32 * (wave >> 1) + (lane & 31), bo = 32 * (wave & 1) + (lane & 31), k2 = lane >> 5;
     if (a.Rx == 0) last = first;        // no row has a source
@@ -133,12 +140,16 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         // a row without a source is zeros in both operands: nothing of it multiplies
         float va[8], vb[8];
 #pragma unroll
-        for (int i = 0; i < 8 / E; ++i) Chunk<T>::open(wa[i], va + i * E);
+        for (int i = 0; i < 8 / E; ++i) {
+            Chunk<T>::open(wa[i], va + i * E);
+            if (!PACKED) Chunk<T>::open(wx[i], vb + i * E);
+        }
         const float step = on ? __uint_as_float(byte << 23) : 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             va[i] = on ? va[i] : 0.0f;
-            vb[i] = (float)(int8_t)(wb >> (8 * i)) * step;
+            if (PACKED) vb[i] = (float)(int8_t)(wb >> (8 * i)) * step;
+            else vb[i] = on ? vb[i] : 0.0f;
         }
         __syncthreads();
 #pragma unroll
@@ -163,12 +174,14 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         if (o + 8 * (v / 4) + v % 4 < a.n_out) to[(int64_t)(8 * (v / 4) + v % 4) * a.n_in] = acc[v];
 }
 
-// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16): 256 x 256 outputs at a time, eight
+// bf16 dy on MFMA (n_out a multiple of 8, n_in of 16, or of 8 where x is not packed): 256 x 256 outputs
+// at a time, eight
 // wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through a
 // ring of four LDS stages.  Both operands lie along K rows of 512 bytes (the tile's columns
 // as bf16) and are read as fragments by the transposing LDS read.  dy is copied into LDS
 // directly by four of the wavefronts; the other four load the packed rows (half of dy's
-// bytes), turn them into bf16 in registers, among their MFMAs, and write them.
+// bytes), turn them into bf16 in registers, among their MFMAs, and write them, or copy the rows of
+// x as the first four copy dy's.
 // Row indexes go to LDS a few thousand at a time; a row past the last one or without a source
 // is zeros in both operands, since a zero of one would turn an infinity of the other into NaN.
 // A workgroup goes through several tiles of the same rows of dy: the row indexes stay, and
@@ -232,11 +245,13 @@ __device__ __forceinline__ u32x4 open_packed(uint32_t q0, uint32_t q1, float ste
     return r;
 }
 
-// The tiles of one work item, for the wavefronts that load packed rows (PACKS) or dy: two
+// The tiles of one work item, for the wavefronts that load packed rows, dy or the rows of x:
 // instances, so that what the one kind keeps in flight is no merge of both kinds' registers.
-template <bool PACKS>
+enum { LOAD_DY = 0, LOAD_PACKED = 1, LOAD_X = 2 };
+template <int LOADS>
 __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* lds, uint32_t* src,
                                             int* s_bad) {
+    constexpr bool PACKS = LOADS == LOAD_PACKED;
     // Work items (expert, slice, row tile, group of column tiles).  Many experts are dealt to the
     // XCDs round-robin and an expert's items run on one XCD, whose L2 then holds its rows; of
     // few experts (split) each XCD takes an eighth of each one's items, a contiguous range,
@@ -334,6 +349,14 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         whole = __builtin_amdgcn_readfirstlane(any) ? 0 : clen / kBK;
     };
     auto stage_of = [&](int h) __attribute__((always_inline)) { return lds + (h % kStages) * kStageB; };
+    // rows of x: the same places of the other operand, each half wavefront's row by its index
+    auto copy_x = [&](int ct, int h, int i) __attribute__((always_inline)) {
+        unsigned char* dst = stage_of(h) + kOpB + krow * kPitch + i * 1024;
+        const uint32_t row = src[h * kBK + krow + 2 * i + hi];
+        const int c = ct * BN + 8 * ((lane & 31) ^ (4 * (hi + 2 * (i & 1))));
+        const bf16_t* p = (const bf16_t*)a.x + (uint64_t)row * (uint32_t)a.n_in + (c < a.n_in ? c : 0);
+        dma16(row != kNoRow ? p : kZeros, dst);
+    };
     auto copy_dy = [&](int h, int i) __attribute__((always_inline)) {
         unsigned char* dst = stage_of(h) + krow * kPitch + i * 1024;
         const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
@@ -390,7 +413,10 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         } else {
             for (int h = 0; h < min(nh, kStages); ++h) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) copy_dy(h, i);
+                for (int i = 0; i < kCopies; ++i) {
+                    if (LOADS == LOAD_X) copy_x(ct, h, i);
+                    else copy_dy(h, i);
+                }
             }
         }
     };
@@ -474,7 +500,8 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
                         write_packed(S_, h + 2, j);     // (past the end into a stage nobody reads)
                         if (j == 3) load_packed(S_, ct, h + 4);
                     } else if (h + kStages < nh) {
-                        copy_dy(h + kStages, j);
+                        if (LOADS == LOAD_X) copy_x(ct, h + kStages, j);
+                        else copy_dy(h + kStages, j);
                     }
                 };
                 if (active) {
@@ -538,13 +565,16 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
     }
 }
 
+template <bool PACKED>
 __global__ void __launch_bounds__(kMfmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 wgrad_mfma_kernel(WgradArgs a) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStageB];
     __shared__ __attribute__((aligned(16))) uint32_t src[kRowsHeld];
     __shared__ int s_bad[kMfmaThreads / 64];
-    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= 4) wgrad_tiles<true>(a, lds, src, s_bad);
-    else wgrad_tiles<false>(a, lds, src, s_bad);
+    if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) >= 4)
+        wgrad_tiles<PACKED ? LOAD_PACKED : LOAD_X>(a, lds, src, s_bad);
+    else
+        wgrad_tiles<LOAD_DY>(a, lds, src, s_bad);
 }
 
 // dW = the slices' partial sums in slice order, four elements per thread
@@ -588,8 +618,8 @@ pr2_status check_wgrad(const pr2_wgrad_desc* desc) {
     return PR2_OK;
 }
 
-bool mfma_ok(const pr2_wgrad_desc& d) {
-    return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % 16 == 0;
+bool mfma_ok(const pr2_wgrad_desc& d, bool packed) {
+    return d.act_dtype == PR2_BF16 && d.n_out % 8 == 0 && d.n_in % (packed ? 16 : 8) == 0;
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -613,8 +643,8 @@ struct SliceCost {
     float step, join, part; // us: a step, the join's launch, a slice's traffic
     int most;               // slices that can pay; does not decrease with the rows
 };
-SliceCost slice_cost(const pr2_wgrad_desc& d) {
-    const bool big = mfma_ok(d);
+SliceCost slice_cost(const pr2_wgrad_desc& d, bool packed) {
+    const bool big = mfma_ok(d, packed);
     const int64_t tiles = wgrad_tile_count(d, big ? BM : kTile);
     SliceCost c{};
     c.steps = ceil_div(d.R / d.N, kBK);
@@ -627,8 +657,8 @@ SliceCost slice_cost(const pr2_wgrad_desc& d) {
     while (c.most < fill && c.join + (float)(c.most + 1) * c.part < whole) ++c.most;
     return c;
 }
-int wgrad_slices(const pr2_wgrad_desc& d) {
-    const SliceCost c = slice_cost(d);
+int wgrad_slices(const pr2_wgrad_desc& d, bool packed) {
+    const SliceCost c = slice_cost(d, packed);
     int best = 1;
     float least = c.step * (float)c.steps;
     for (int s = 2; s <= c.most; ++s) {
@@ -668,7 +698,9 @@ WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
     WgradWs w{};
     char* p = base ? (char*)(((uintptr_t)base + 255) & ~(uintptr_t)255) : nullptr;
     const size_t order = (sizeof(int) * (size_t)d.N + 255) & ~(size_t)255;
-    const int S = slice_cost(d).most;       // not the slices of these rows alone: fewer rows can have more
+    // not the slices of these rows alone: fewer rows can have more (nor of one form of x: they share
+    // the size)
+    const int S = std::max(slice_cost(d, true).most, slice_cost(d, false).most);
     w.order = (int*)p;
     w.part = (float*)(p ? p + order : nullptr);
     w.bytes = order + (S > 1 ? sizeof(float) * (size_t)S * d.N * d.n_out * d.n_in : 0) + 256;
@@ -676,10 +708,11 @@ WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
 }
 
 hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
-    a.S = d.R > 0 ? wgrad_slices(d) : 1;
+    const bool packed = a.q != nullptr;
+    a.S = d.R > 0 ? wgrad_slices(d, packed) : 1;
     a.part = w.part;
     hipError_t e;
-    if (d.R > 0 && d.Rx > 0 && mfma_ok(d)) {
+    if (d.R > 0 && d.Rx > 0 && mfma_ok(d, packed)) {
         a.G = wgrad_group(d);
         const int64_t items = ceil_div(d.n_out, BM) * ceil_div(ceil_div(d.n_in, BN), a.G) * a.S;
         a.split = d.N < kManyExperts;
@@ -690,16 +723,18 @@ hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, 
             a.order = w.order;
         }
         LaunchScope scope("wgrad_mfma", st);
-        hipLaunchKernelGGL(wgrad_mfma_kernel, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
+        if (packed) hipLaunchKernelGGL(wgrad_mfma_kernel<true>, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
+        else hipLaunchKernelGGL(wgrad_mfma_kernel<false>, dim3((unsigned)grid), dim3(kMfmaThreads), 0, st, a);
     } else {
         // (column and row tiles apart, at most 2^14 each: together they can be more than a
         // dimension holds; N S <= 1024)
         const dim3 grid((unsigned)ceil_div(d.n_in, kTile), (unsigned)ceil_div(d.n_out, kTile), d.N * a.S);
         LaunchScope scope("wgrad_tile", st);
-        if (d.act_dtype == PR2_BF16)
-            hipLaunchKernelGGL(wgrad_tile_kernel<bf16_t>, grid, dim3(256), 0, st, a);
-        else
-            hipLaunchKernelGGL(wgrad_tile_kernel<float>, grid, dim3(256), 0, st, a);
+        const bool bf16 = d.act_dtype == PR2_BF16;
+        if (bf16 && packed) hipLaunchKernelGGL((wgrad_tile_kernel<bf16_t, true>), grid, dim3(256), 0, st, a);
+        else if (bf16) hipLaunchKernelGGL((wgrad_tile_kernel<bf16_t, false>), grid, dim3(256), 0, st, a);
+        else if (packed) hipLaunchKernelGGL((wgrad_tile_kernel<float, true>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((wgrad_tile_kernel<float, false>), grid, dim3(256), 0, st, a);
     }
     e = hipGetLastError();
     if (e != hipSuccess || a.S == 1) return e;
@@ -708,6 +743,42 @@ hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, 
     hipLaunchKernelGGL(wgrad_join_kernel, dim3((unsigned)ceil_div(n, 1024)), dim3(256), 0, st, a.part,
                        n, a.S, a.dW);
     return hipGetLastError();
+}
+
+// x, or (packed) its packed form (q, scale)
+pr2_status weight_grad(const pr2_wgrad_desc* desc, bool packed, const void* dy, const int8_t* q,
+                       const uint8_t* scale, const void* x, const int32_t* offsets, const int32_t* route_of_row, float* dW, void* ws,
+                       size_t ws_bytes, pr2_stream_t stream) {
+    pr2_status s = check_wgrad(desc);
+    if (s != PR2_OK) return s;
+    const pr2_wgrad_desc& d = *desc;
+    if (!dW) return fail(PR2_ERR_NULL, "dW is NULL");
+    if ((uintptr_t)dW % 16) return fail(PR2_ERR_ALIGN, "dW is not 16-byte aligned");
+    if (d.R > 0) {
+        if (packed && (!dy || !q || !scale)) return fail(PR2_ERR_NULL, "dy, q and scale are required");
+        if (!packed && (!dy || (!x && d.Rx > 0))) return fail(PR2_ERR_NULL, "dy and x are required");
+        if ((uintptr_t)dy % 16 || (uintptr_t)q % 16 || (uintptr_t)scale % 16)
+            return fail(PR2_ERR_ALIGN, "dy, q and scale must be 16-byte aligned");
+        if (!offsets && d.N != 1) return fail(PR2_ERR_NULL, "offsets is NULL with N = %d > 1", d.N);
+        if (!route_of_row && d.R > d.Rx)
+            return fail(PR2_ERR_SHAPE, "R = %lld > Rx = %lld without route_of_row", (long long)d.R,
+                        (long long)d.Rx);
+        if ((uintptr_t)offsets % 4 || (uintptr_t)route_of_row % 4)
+            return fail(PR2_ERR_ALIGN, "offsets or route_of_row is not 4-byte aligned");
+        const size_t need = wgrad_ws(d, nullptr).bytes;
+        if (need && !ws) return fail(PR2_ERR_NULL, "ws is NULL (need %zu bytes)", need);
+        if (ws_bytes < need)
+            return fail(PR2_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
+    }
+    s = device_ready();
+    if (s != PR2_OK) return s;
+    drop_split_records(ws, ws_bytes);
+    const hipStream_t st = (hipStream_t)stream;
+    WgradArgs a{dy, q, scale, x, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
+                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1, false};
+    const hipError_t e = launch_wgrad(d, a, wgrad_ws(d, ws), st);
+    if (e != hipSuccess) return hip_fail(e, packed ? "weight_grad_packed launch" : "weight_grad launch");
+    return ok();
 }
 
 }  // namespace
@@ -724,39 +795,18 @@ size_t pr2_weight_grad_workspace_bytes(const pr2_wgrad_desc* desc) {
     return wgrad_ws(*desc, nullptr).bytes;
 }
 
+pr2_status pr2_weight_grad(const pr2_wgrad_desc* desc, const void* dy, const void* x, const int32_t* offsets,
+                           const int32_t* route_of_row, float* dW, void* ws, size_t ws_bytes,
+                           pr2_stream_t stream) {
+    if ((uintptr_t)x % 16) return fail(PR2_ERR_ALIGN, "x is not 16-byte aligned");
+    return weight_grad(desc, false, dy, nullptr, nullptr, x, offsets, route_of_row, dW, ws, ws_bytes, stream);
+}
+
 pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, const int8_t* q,
                                   const uint8_t* scale, const int32_t* offsets,
                                   const int32_t* route_of_row, float* dW, void* ws,
                                   size_t ws_bytes, pr2_stream_t stream) {
-    pr2_status s = check_wgrad(desc);
-    if (s != PR2_OK) return s;
-    const pr2_wgrad_desc& d = *desc;
-    if (!dW) return fail(PR2_ERR_NULL, "dW is NULL");
-    if ((uintptr_t)dW % 16) return fail(PR2_ERR_ALIGN, "dW is not 16-byte aligned");
-    if (d.R > 0) {
-        if (!dy || !q || !scale) return fail(PR2_ERR_NULL, "dy, q and scale are required");
-        if ((uintptr_t)dy % 16 || (uintptr_t)q % 16 || (uintptr_t)scale % 16)
-            return fail(PR2_ERR_ALIGN, "dy, q and scale must be 16-byte aligned");
-        if (!offsets && d.N != 1) return fail(PR2_ERR_NULL, "offsets is NULL with N = %d > 1", d.N);
-        if (!route_of_row && d.R > d.Rx)
-            return fail(PR2_ERR_SHAPE, "R = %lld > Rx = %lld without route_of_row", (long long)d.R,
-                        (long long)d.Rx);
-        if ((uintptr_t)offsets % 4 || (uintptr_t)route_of_row % 4)
-            return fail(PR2_ERR_ALIGN, "offsets or route_of_row is not 4-byte aligned");
-        const size_t need = pr2_weight_grad_workspace_bytes(desc);
-        if (need && !ws) return fail(PR2_ERR_NULL, "ws is NULL (need %zu bytes)", need);
-        if (ws_bytes < need)
-            return fail(PR2_ERR_WORKSPACE, "workspace %zu bytes < %zu needed", ws_bytes, need);
-    }
-    s = device_ready();
-    if (s != PR2_OK) return s;
-    drop_split_records(ws, ws_bytes);
-    const hipStream_t st = (hipStream_t)stream;
-    WgradArgs a{dy, q, scale, d.R ? offsets : nullptr, route_of_row, dW, d.R, d.Rx, d.n_out, d.n_in,
-                d.N, d.k, (d.n_in + 31) / 32, nullptr, nullptr, 1, 1, false};
-    const hipError_t e = launch_wgrad(d, a, wgrad_ws(d, ws), st);
-    if (e != hipSuccess) return hip_fail(e, "weight_grad_packed launch");
-    return ok();
+    return weight_grad(desc, true, dy, q, scale, nullptr, offsets, route_of_row, dW, ws, ws_bytes, stream);
 }
 
 }  // extern "C"
