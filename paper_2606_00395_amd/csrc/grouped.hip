@@ -235,6 +235,649 @@ __global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
     }
 }
 
+// --------------------------------------------------------- matrix instructions --
+// bf16 rows of a multiple of 16 bytes on v_mfma_f32_16x16x32_bf16, 8-bit ones on
+// v_mfma_i32_16x16x64_i8: a lane's fragment is 16 consecutive bytes of a row in both, so one kernel
+// in bytes serves both.
+template <typename E> struct Mma;
+template <> struct Mma<bf16_t> {
+    using Frag = bf16x8;
+    using Acc = f32x4;
+    __device__ __forceinline__ static Acc mul(Frag a, Frag b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+template <> struct Mma<int8_t> {
+    using Frag = i32x4;
+    using Acc = i32x4;
+    __device__ __forceinline__ static Acc mul(Frag a, Frag b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+    }
+};
+
+constexpr int kRowB = 128;                  // bytes of a row per K slice
+constexpr int MT = 16;
+__device__ __attribute__((aligned(16))) const unsigned char kZeros[16] = {};
+
+// 16-byte chunk c of LDS row r lies at c ^ swz(r): 8 or 16 consecutive rows read at the same chunk
+// hit disjoint banks
+__device__ __forceinline__ int swz(int r) { return (r & 7) ^ ((r >> 3) & 1); }
+
+// wait until at most n of this wavefront's copies are outstanding
+template <int n>
+__device__ __forceinline__ void wait_vmcnt() {
+    static_assert(n >= 0 && n < 16, "vmcnt field");
+    __builtin_amdgcn_s_waitcnt(0x0f70 | n);
+}
+// a barrier that leaves the copies in flight
+__device__ __forceinline__ void plain_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+}
+
+// Four consecutive columns of a row's sums as outputs; `on` false: a row without a source.
+template <typename E>
+__device__ __forceinline__ f32x4 finish(const typename Mma<E>::Acc& acc, bool on, float sr, const f32x4& sw) {
+    f32x4 y;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        if (sizeof(E) == 1) y[v] = (float)acc[v] * sr * sw[v];
+        else y[v] = (float)acc[v];
+        y[v] = on ? y[v] : 0.0f;
+    }
+    return y;
+}
+// the channels' scales of columns c .. c + 3 of C (zeros past them)
+__device__ __forceinline__ f32x4 four_scales(const float* w, int c, int C) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    if (c + 4 <= C) return *(const f32x4_any*)(w + c);
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (c + v < C) s[v] = w[c + v];
+    return s;
+}
+// four columns from c on of a row of C, wherever the row starts
+template <typename O>
+__device__ __forceinline__ void store_four(O* row, int c, int C, const f32x4& y) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    typedef uint64_t u64_any __attribute__((aligned(2)));
+    if (c + 4 <= C) {
+        if (sizeof(O) == 4) {
+            *(f32x4_any*)(row + c) = y;
+        } else {
+            const uint32_t lo = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16;
+            const uint32_t hi = (uint32_t)f32_to_bf16(y[2]) | (uint32_t)f32_to_bf16(y[3]) << 16;
+            *(u64_any*)(row + c) = (uint64_t)hi << 32 | lo;
+        }
+        return;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (c + v < C) row[c + v] = Act<O>::from_f32(y[v]);
+}
+// zeros in the columns of a panel of the rows that belong to no expert
+template <typename O>
+__device__ __forceinline__ void zero_tile(const MmArgs& a, const RowTile& t, int width, int threads) {
+    const int c0 = t.panel * width, n = min(width, a.C - c0);
+    for (int i = threadIdx.x; i < t.rows * width; i += threads) {
+        const int r = i / width, c = i % width;
+        if (c < n) ((O*)a.out)[(int64_t)(t.row0 + r) * a.C + c0 + c] = Act<O>::from_f32(0.0f);
+    }
+}
+
+// 256 rows x 256 columns per workgroup, eight wavefronts of 64 x 128 (two per SIMD).  K advances in
+// slices of 128 bytes a row, copied into LDS directly, two stages; the slice's only barrier sits
+// between its two sub-steps, so that the fragments of the next sub-step are always read among the
+// MFMAs of the one before.  Chunks past a row's end are copied from zeros, in both operands.  The
+// MFMAs take (weights, rows), so that a lane holds four consecutive columns of one row.
+constexpr int BM = 256, BP = 256;
+constexpr int WM = 64, WN = 128;
+constexpr int MI = WM / MT, NJ = WN / MT;
+constexpr int kThreads = 512;
+constexpr int kGroups = 8;                  // copies of 8 rows per wavefront and slice
+constexpr int kStageB = (BM + BP) * kRowB;
+
+template <typename E, typename O>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+mm_mfma_kernel(MmArgs a) {
+    using M = Mma<E>;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStageB];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, BM, (a.C + BP - 1) / BP, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<O>(a, t, BP, kThreads);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1;
+    const int c0 = t.panel * BP;
+    // blocks past the tile's rows or the matrix only help copy
+    const bool active = wr * WM < t.rows && c0 + wc * WN < a.C;
+    const int kb = a.K * (int)sizeof(E);
+
+    // wavefronts 0-3 copy the rows, 4-7 the weights: copy i rows wrow0 + 8 i + lane / 8
+    const int wrow0 = (wave & 3) * 64;
+    const unsigned char* base;
+    uint32_t off[kGroups];
+    const int chunk0 = (lane & 7) ^ swz(lane >> 3);         // of copies 0, 2, ..; the others ^ 1
+    if (wave < 4) {
+        base = (const unsigned char*)a.x + (a.route ? 0 : (int64_t)t.row0 * kb);
+        int src[kGroups];
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            const int r = min(wrow0 + 8 * i + lane / 8, t.rows - 1);
+            src[i] = a.route ? a.route[t.row0 + r] : r;
+        }
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            const int row = a.route ? min(max(src[i], 0) / a.k, a.Rx - 1) : src[i];
+            off[i] = (uint32_t)row * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
+        }
+    } else {
+        base = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + c0) * kb;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) {
+            const int r = min(wrow0 + 8 * i + lane / 8, a.C - 1 - c0);
+            off[i] = (uint32_t)r * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
+        }
+    }
+    // copies of this wavefront per slice, in twos: fewer where the rows end
+    const int rows_here = wave < 4 ? t.rows : a.C - c0;
+    const int ncopy = min(kGroups, max(0, (rows_here - wrow0 + 15) / 16) * 2);
+    const int whole = kb / kRowB;                           // slices inside every row
+    const int nk = max(2, (kb + kRowB - 1) / kRowB);
+    auto issue = [&](int kt, int q) __attribute__((always_inline)) {
+        if (ncopy <= 2 * q) return;
+        const unsigned char* from = base + kt * kRowB;
+        unsigned char* to = lds + (kt & 1) * kStageB + (wave * kGroups + 2 * q) * 1024;
+        if (kt < whole) {
+            dma16_at(from, off[2 * q], to);
+            dma16_at(from, off[2 * q + 1], to + 1024);
+        } else {
+            const int left = kb - kt * kRowB;
+            dma16(chunk0 * 16 < left ? from + off[2 * q] : kZeros, to);
+            dma16((chunk0 ^ 1) * 16 < left ? from + off[2 * q + 1] : kZeros, to + 1024);
+        }
+    };
+    auto issue_all = [&](int kt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < kGroups / 2; ++q) issue(kt, q);
+    };
+
+    typename M::Acc acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
+    // fragments: lane l reads row l % 16 of a block, chunk 4 ks + (0, 2, 1, 3)[l / 16] (both operands
+    // alike, and so that the two halves of a read cycle hit disjoint banks)
+    const int lrow = lane & 15, grp = lane >> 4;
+    const int cperm = ((grp & 1) << 1) | (grp >> 1);
+    int kpos[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
+    const int a0 = wr * WM * kRowB, b0 = (BM + wc * WN) * kRowB;
+    typename M::Frag fa[2][MI], fb[2][NJ];
+    auto frag = [&](int at) __attribute__((always_inline)) {
+        return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(lds + at));
+    };
+    auto sync = [&]() __attribute__((always_inline)) {
+        wait_vmcnt<0>();
+        __syncthreads();
+    };
+    // MFMAs of a sub-step on fragment set S, among them the reads of the next one's and the copies
+    // of slice kt
+    auto phase = [&](auto S_, auto READ, auto ISSUE, int stage, int ks, int kt) __attribute__((always_inline)) {
+        constexpr int S = decltype(S_)::value;
+        const int at = stage * kStageB + kpos[ks];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (decltype(ISSUE)::value) issue(kt, q);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 2 * q; j < 2 * q + 2; ++j)
+#pragma unroll
+                for (int i = 0; i < MI; ++i) acc[i][j] = M::mul(fb[S][j], fa[S][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (decltype(READ)::value && q < 3) {
+                if (q < 2) {
+#pragma unroll
+                    for (int h = 2 * q; h < 2 * q + 2; ++h) {
+                        fa[S ^ 1][h] = frag(at + a0 + h * MT * kRowB);
+                        fb[S ^ 1][h] = frag(at + b0 + h * MT * kRowB);
+                    }
+                } else {
+#pragma unroll
+                    for (int h = 4; h < NJ; ++h) fb[S ^ 1][h] = frag(at + b0 + h * MT * kRowB);
+                }
+            }
+        }
+    };
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
+    issue_all(0);
+    issue_all(1);
+    if (ncopy == kGroups) wait_vmcnt<kGroups>();
+    else wait_vmcnt<0>();
+    plain_barrier();
+    int kt = 0;
+    if (active) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[0][i] = frag(kpos[0] + a0 + i * MT * kRowB);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fb[0][j] = frag(kpos[0] + b0 + j * MT * kRowB);
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        for (; kt + 2 < nk; ++kt) {
+            phase(C0{}, C1{}, C0{}, kt & 1, 1, 0);
+            sync();
+            phase(C1{}, C1{}, C1{}, (kt + 1) & 1, 0, kt + 2);
+        }
+        phase(C0{}, C1{}, C0{}, kt & 1, 1, 0);
+        sync();
+        phase(C1{}, C1{}, C0{}, (kt + 1) & 1, 0, 0);
+        phase(C0{}, C1{}, C0{}, (kt + 1) & 1, 1, 0);
+        phase(C1{}, C0{}, C0{}, 0, 0, 0);
+    } else {
+        for (; kt + 2 < nk; ++kt) {
+            sync();
+            issue_all(kt + 2);
+        }
+        sync();
+    }
+
+    // a lane's rows: 16 i + lane % 16 of the wavefront's block
+    const int col0 = c0 + wc * WN + 4 * grp;
+    bool on[MI];
+    float sr[MI];
+    if (active) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int src = source(a, t.row0 + min(wr * WM + i * MT + lrow, t.rows - 1));
+            on[i] = src >= 0;
+            sr[i] = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+        }
+    }
+    const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
+    const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (sizeof(O) == 4) {
+        // 64 bytes of a row per store and 16 lanes, straight from the registers
+        if (!active) return;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int r = wr * WM + i * MT + lrow;
+                if (r < t.rows)
+                    store_four((O*)a.out + (int64_t)(t.row0 + r) * a.C, col0 + j * MT, a.C,
+                               finish<E>(acc[i][j], on[i], sr[i], s4));
+            }
+        }
+        return;
+    }
+    // bf16: through this wavefront's share of the freed stages (16-byte chunks XOR-swizzled by row, the
+    // halves of a chunk swapped in rows with bit 3 set: every write cycle's rows in other banks), so
+    // that a store covers whole 256-byte row segments
+    __syncthreads();
+    if (!active) return;
+    constexpr int RB = WN * 2, NCH = RB / 16;
+    unsigned char* stage_w = lds + wave * (WM * RB);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int row = i * MT + lrow, col = j * MT + 4 * grp;
+            const f32x4 y = finish<E>(acc[i][j], on[i], sr[i], s4);
+            const uint32_t lo = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16;
+            const uint32_t hi = (uint32_t)f32_to_bf16(y[2]) | (uint32_t)f32_to_bf16(y[3]) << 16;
+            *(uint2*)(stage_w + row * RB + (((col >> 3) ^ (row & (NCH - 1))) << 4) + (((col & 4) << 1) ^ (row & 8))) =
+                make_uint2(lo, hi);
+        }
+    }
+    // (one wavefront's own region: its LDS operations complete in order)
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    __builtin_amdgcn_wave_barrier();
+    const int ch = lane % NCH;
+    const int col = c0 + wc * WN + ch * 8, left = a.C - col;
+#pragma unroll
+    for (int p = 0; p < WM / (64 / NCH); ++p) {
+        const int row = p * (64 / NCH) + lane / NCH;
+        const int r = wr * WM + row;
+        u32x4 v = *(const u32x4*)(stage_w + row * RB + ((ch ^ (row & (NCH - 1))) << 4));
+        if (row & 8) v = u32x4{v[2], v[3], v[0], v[1]};
+        if (r >= t.rows) continue;
+        bf16_t* to = (bf16_t*)a.out + (int64_t)(t.row0 + r) * a.C + col;
+        if (left >= 8) {
+            store16<false>(to, v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < left) to[e] = (bf16_t)(v[e / 2] >> (16 * (e & 1)));
+        }
+    }
+}
+
+// Few rows per expert: the weights' bytes in flight are what matters.  64 rows x 128 columns per
+// workgroup of four wavefronts, slices of 128 bytes a row through a ring of three stages, two
+// workgroups on a CU.
+constexpr int kFewM = 64, kFewP = 128;
+constexpr int kFewStageB = (kFewM + kFewP) * kRowB;
+constexpr int kFewStages = 3;
+constexpr int kFewRows = 32;                // rows per expert up to which it is taken
+
+template <typename E, typename O>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+mm_few_kernel(MmArgs a) {
+    using M = Mma<E>;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewStages * kFewStageB];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, kFewM, (a.C + kFewP - 1) / kFewP, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<O>(a, t, kFewP, 256);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c0 = t.panel * kFewP;
+    const int kb = a.K * (int)sizeof(E);
+    // copies: weight rows 32 wave .. + 31 (four of 8), rows 16 wave .. + 15 (two, fewer past the end)
+    const int chunk0 = (lane & 7) ^ swz(lane >> 3);
+    const unsigned char* wb = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + c0) * kb;
+    const unsigned char* xb = (const unsigned char*)a.x + (a.route ? 0 : (int64_t)t.row0 * kb);
+    uint32_t woff[4], xoff[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        woff[i] = (uint32_t)min(32 * wave + 8 * i + lane / 8, a.C - 1 - c0) * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
+    const int nx = max(0, min(2, (t.rows - 16 * wave + 7) / 8));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = min(16 * wave + 8 * i + lane / 8, t.rows - 1);
+        const int row = a.route ? min(max(a.route[t.row0 + r], 0) / a.k, a.Rx - 1) : r;
+        xoff[i] = (uint32_t)row * (uint32_t)kb + ((chunk0 ^ i) << 4);
+    }
+    const int whole = kb / kRowB;
+    const int nk = max(2, (kb + kRowB - 1) / kRowB);
+    auto copy = [&](const unsigned char* from, uint32_t off, int chunk, int left, unsigned char* to)
+        __attribute__((always_inline)) {
+        if (left >= kRowB) dma16_at(from, off, to);
+        else dma16(chunk * 16 < left ? from + off : kZeros, to);
+    };
+    auto issue = [&](int kt) __attribute__((always_inline)) {
+        unsigned char* st = lds + (kt % kFewStages) * kFewStageB;
+        const int left = kt < whole ? kRowB : kb - kt * kRowB;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            copy(wb + kt * kRowB, woff[i], chunk0 ^ (i & 1), left, st + (kFewM + 32 * wave + 8 * i) * kRowB);
+        if (nx > 0) copy(xb + kt * kRowB, xoff[0], chunk0, left, st + 16 * wave * kRowB);
+        if (nx > 1) copy(xb + kt * kRowB, xoff[1], chunk0 ^ 1, left, st + (16 * wave + 8) * kRowB);
+    };
+    // a slice has landed, the one after it may still be in flight
+    auto wait_one = [&]() __attribute__((always_inline)) {
+        if (nx == 2) wait_vmcnt<6>();
+        else if (nx == 1) wait_vmcnt<5>();
+        else wait_vmcnt<4>();
+    };
+    const int lrow = lane & 15, grp = lane >> 4;
+    const int cperm = ((grp & 1) << 1) | (grp >> 1);
+    int kpos[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
+    const int b0 = (kFewM + 32 * wave) * kRowB, b1 = b0 + 16 * kRowB;
+    typename M::Acc acc[4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
+    const int mi = (t.rows + 15) / 16;
+    issue(0);
+    issue(1);
+    for (int kt = 0; kt < nk; ++kt) {
+        if (kt + 1 < nk) wait_one();
+        else wait_vmcnt<0>();
+        __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
+        plain_barrier();
+        if (kt + 2 < nk) issue(kt + 2);
+        const unsigned char* st = lds + (kt % kFewStages) * kFewStageB;
+        auto frag = [&](int at) __attribute__((always_inline)) {
+            return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(st + at));
+        };
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const typename M::Frag w0 = frag(b0 + kpos[ks]), w1 = frag(b1 + kpos[ks]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= mi) continue;
+                const typename M::Frag x = frag(16 * i * kRowB + kpos[ks]);
+                acc[i][0] = M::mul(w0, x, acc[i][0]);
+                acc[i][1] = M::mul(w1, x, acc[i][1]);
+            }
+        }
+    }
+    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16
+    const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
+    f32x4 s4[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+    const int col = c0 + 32 * wave + 4 * grp;
+    if (sizeof(E) == 1) {
+        s4[0] = four_scales(sw, col, a.C);
+        s4[1] = four_scales(sw, col + 16, a.C);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 16 * i + lrow;
+        if (r >= t.rows) continue;
+        const int src = source(a, t.row0 + r);
+        const float sr = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+        O* row = (O*)a.out + (int64_t)(t.row0 + r) * a.C;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) store_four(row, col + 16 * j, a.C, finish<E>(acc[i][j], src >= 0, sr, s4[j]));
+    }
+}
+
+// dx = dy W on v_mfma_f32_32x32x16_bf16 (n_out and n_in multiples of 8): 256 x 256 outputs, K = n_out in
+// steps of 32 through a ring of four stages.  The rows of dy run along K (64 bytes of each a
+// step); the weights lie along their columns, 32 K rows of 512 bytes, and are read as fragments by the
+// transposing LDS read.
+constexpr int kBK = 32;
+constexpr int kBStages = 4, kCopies = 4;
+constexpr int kOpB = kBK * 512;
+constexpr int kBStageB = 2 * kOpB;
+constexpr int BI = WM / 32, BJ = WN / 32;
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+
+// chunk c of a 64-byte LDS row r lies at c ^ rswz(r)
+__device__ __forceinline__ int rswz(int r) { return (r >> 2) & 3; }
+
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+mm_back_mfma_kernel(MmArgs a) {
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kBStages * kBStageB];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, BM, (a.C + BP - 1) / BP, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<bf16_t>(a, t, BP, kThreads);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wr = wave >> 1, wc = wave & 1;
+    const int half = wave >> 2, wq = wave & 3;      // copies: 0 the rows of dy, 1 the weights
+    const int c0 = t.panel * BP;
+    const bool active = wr * WM < t.rows && c0 + wc * WN < a.C;
+    const int hi = lane >> 5;
+    const bf16_t* const xb = (const bf16_t*)a.x + (int64_t)t.row0 * a.K;
+    const bf16_t* const wb = (const bf16_t*)a.W + (int64_t)t.expert * a.K * a.C + c0;
+    uint32_t off[kCopies];
+    int xk = 0;                                     // first K of this lane's chunk of a step, copies 0 and 2
+    if (half == 0) {
+        // copy i: rows 64 wq + 16 i + lane / 4
+        xk = 8 * ((lane & 3) ^ rswz(lane / 4));
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int r = 64 * wq + 16 * i + lane / 4;
+            off[i] = 2u * ((uint32_t)min(r, t.rows - 1) * (uint32_t)a.K + xk);
+        }
+    } else {
+        // copy i: K rows 8 wq + 2 i (lanes 0-31) and + 1, chunk c of K row kr at c ^ 4 (kr & 3).  (Columns
+        // past the matrix read the panel's first: they reach only outputs that are not stored.)
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int c = 8 * ((lane & 31) ^ (4 * (hi + 2 * (i & 1))));
+            off[i] = 2u * ((uint32_t)hi * (uint32_t)a.C + (c0 + c < a.C ? c : 0));
+        }
+    }
+    const int whole = a.K / kBK;
+    const int nh = max(kBStages, (a.K + kBK - 1) / kBK);
+    auto issue = [&](int h) __attribute__((always_inline)) {
+        unsigned char* dst = lds + (h % kBStages) * kBStageB + half * kOpB + wq * 4096;
+        if (half == 0) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                if (h < whole) dma16_at(xb + h * kBK, off[i], dst + i * 1024);
+                else dma16(h * kBK + xk < a.K ? (const unsigned char*)(xb + h * kBK) + off[i] : kZeros, dst + i * 1024);
+            }
+        } else {
+            const bf16_t* p = wb + (int64_t)(h * kBK + 8 * wq) * a.C;
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const bf16_t* q = p + (int64_t)(2 * i) * a.C;
+                if (h < whole) dma16_at(q, off[i], dst + i * 1024);
+                else dma16(h * kBK + 8 * wq + 2 * i + hi < a.K ? (const unsigned char*)q + off[i] : kZeros, dst + i * 1024);
+            }
+        }
+    };
+
+    f32x16 acc[BI][BJ];
+#pragma unroll
+    for (int i = 0; i < BI; ++i)
+#pragma unroll
+        for (int j = 0; j < BJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.0f;
+    const int lrow = lane & 31;
+    int kpos[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * 64 + (((2 * ks + hi) ^ rswz(lrow)) << 4);
+    // weights: two transposing reads a fragment, each of four K values of a column
+    const int s16 = lane & 15, g4 = lane >> 4;
+    const int nl = 16 * (g4 & 1) + 4 * (s16 & 3);
+    const int kl = 8 * (g4 >> 1) + (s16 >> 2);
+    const int tsw = (nl >> 3) ^ (4 * (kl & 3));
+    int a_pos[BI], b_pos[BJ];
+#pragma unroll
+    for (int i = 0; i < BI; ++i) a_pos[i] = (wr * WM + i * 32) * 64;
+#pragma unroll
+    for (int j = 0; j < BJ; ++j)
+        b_pos[j] = kOpB + kl * 512 + (((wc * WN + j * 32) >> 3 ^ tsw) << 4) + ((nl & 4) << 1);
+    auto wait_steps = [&](int n) __attribute__((always_inline)) {
+        if (n >= 2) wait_vmcnt<2 * kCopies>();
+        else if (n == 1) wait_vmcnt<kCopies>();
+        else wait_vmcnt<0>();
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
+        plain_barrier();
+    };
+    bf16x8 fa[2][BI], fb[2][BJ];
+    auto tr_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
+        const v4s hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * 512));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto row_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, *(const u32x4*)p);
+    };
+    // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the other set
+    auto phase = [&](auto S_, int stage, int ks) __attribute__((always_inline)) {
+        constexpr int S = decltype(S_)::value;
+        const unsigned char* st = lds + stage * kBStageB;
+#pragma unroll
+        for (int j = 0; j < BJ; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < BI; ++i)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[S][j], fa[S][i], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (j == 0) {
+                fa[S ^ 1][0] = row_frag(st + a_pos[0] + kpos[ks]);
+                fa[S ^ 1][1] = row_frag(st + a_pos[1] + kpos[ks]);
+                fb[S ^ 1][0] = tr_frag(st + b_pos[0] + ks * 8192);
+            } else if (j == 1) {
+                fb[S ^ 1][1] = tr_frag(st + b_pos[1] + ks * 8192);
+                fb[S ^ 1][2] = tr_frag(st + b_pos[2] + ks * 8192);
+                fb[S ^ 1][3] = tr_frag(st + b_pos[3] + ks * 8192);
+            }
+        }
+    };
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
+#pragma unroll
+    for (int h = 0; h < kBStages; ++h) issue(h);
+    wait_vmcnt<3 * kCopies>();
+    barrier();
+    if (active) {
+#pragma unroll
+        for (int i = 0; i < BI; ++i) fa[0][i] = row_frag(lds + a_pos[i] + kpos[0]);
+#pragma unroll
+        for (int j = 0; j < BJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
+        for (int h = 0; h < nh; ++h) {
+            phase(C0{}, h % kBStages, 1);
+            wait_steps(min(nh - 1, h + kBStages - 1) - (h + 1));
+            barrier();
+            if (h + kBStages < nh) issue(h + kBStages);
+            // (past the last step the reads fetch an old stage; unused)
+            phase(C1{}, (h + 1) % kBStages, 0);
+        }
+    } else {
+        for (int h = 0; h < nh; ++h) {
+            wait_steps(min(nh - 1, h + kBStages - 1) - (h + 1));
+            barrier();
+            if (h + kBStages < nh) issue(h + kBStages);
+        }
+    }
+    // Lane l holds row l % 32 of each 32-row block, columns 8 (v / 4) + 4 (l / 32) + v % 4 of each
+    // 32-column block; staged as the product's outputs are.
+    __syncthreads();
+    if (!active) return;
+    constexpr int RB = WN * 2, NCH = RB / 16;
+    unsigned char* sw = lds + wave * (WM * RB);
+#pragma unroll
+    for (int i = 0; i < BI; ++i) {
+        const int row = i * 32 + lrow;
+#pragma unroll
+        for (int j = 0; j < BJ; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; v += 4) {
+                const int col = j * 32 + 2 * v + 4 * hi;
+                const uint32_t w0 = (uint32_t)f32_to_bf16(acc[i][j][v]) | (uint32_t)f32_to_bf16(acc[i][j][v + 1]) << 16;
+                const uint32_t w1 = (uint32_t)f32_to_bf16(acc[i][j][v + 2]) | (uint32_t)f32_to_bf16(acc[i][j][v + 3]) << 16;
+                *(uint2*)(sw + row * RB + (((col >> 3) ^ (row & (NCH - 1))) << 4) + (((col & 4) << 1) ^ (row & 8))) =
+                    make_uint2(w0, w1);
+            }
+    }
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    __builtin_amdgcn_wave_barrier();
+    const int ch = lane % NCH;
+    const int col = c0 + wc * WN + ch * 8;
+#pragma unroll
+    for (int p = 0; p < WM / (64 / NCH); ++p) {
+        const int row = p * (64 / NCH) + lane / NCH;
+        const int r = wr * WM + row;
+        u32x4 v = *(const u32x4*)(sw + row * RB + ((ch ^ (row & (NCH - 1))) << 4));
+        if (row & 8) v = u32x4{v[2], v[3], v[0], v[1]};
+        if (r < t.rows && col < a.C) *(u32x4*)((bf16_t*)a.out + (int64_t)(t.row0 + r) * a.C + col) = v;
+    }
+}
+
 // out = 0 (no row has a source)
 __global__ void __launch_bounds__(256) mm_zero_kernel(uint32_t* p, int64_t words, uint16_t* last) {
     const int64_t i = (int64_t)block_number() * 256 + threadIdx.x;
@@ -306,20 +949,33 @@ hipError_t launch_tiles(const char* name, K kernel, const MmArgs& a, int rows, i
     return hipGetLastError();
 }
 
+// Whether the copies reach every row: whole 16-byte chunks, and 32-bit offsets into gathered rows (into
+// sorted ones they start at the tile).
+bool mfma_ok(const MmArgs& a, int64_t element) {
+    return a.K * element % 16 == 0 && (!a.route || (int64_t)a.Rx * a.K * element < (int64_t)1 << 32);
+}
+bool few_rows(const MmArgs& a) { return a.R <= (int64_t)kFewRows * a.N; }
+
 hipError_t launch_mm(const pr2_wgrad_desc& d, const MmArgs& a, hipStream_t st) {
-    if (d.act_dtype == PR2_BF16) return launch_tiles("mm_tile", mm_tile_kernel<bf16_t, false>, a, kTile, kTile, 256, st);
-    return launch_tiles("mm_tile", mm_tile_kernel<float, false>, a, kTile, kTile, 256, st);
+    if (d.act_dtype == PR2_F32)
+        return launch_tiles("mm_tile", mm_tile_kernel<float, false>, a, kTile, kTile, 256, st);
+    if (!mfma_ok(a, 2)) return launch_tiles("mm_tile", mm_tile_kernel<bf16_t, false>, a, kTile, kTile, 256, st);
+    if (few_rows(a)) return launch_tiles("mm_few", mm_few_kernel<bf16_t, bf16_t>, a, kFewM, kFewP, 256, st);
+    return launch_tiles("mm_mfma", mm_mfma_kernel<bf16_t, bf16_t>, a, BM, BP, kThreads, st);
 }
 
 hipError_t launch_mm_back(const pr2_wgrad_desc& d, const MmArgs& a, hipStream_t st) {
-    if (d.act_dtype == PR2_BF16)
-        return launch_tiles("mm_back_tile", mm_tile_kernel<bf16_t, true>, a, kTile, kTile, 256, st);
-    return launch_tiles("mm_back_tile", mm_tile_kernel<float, true>, a, kTile, kTile, 256, st);
+    if (d.act_dtype == PR2_F32)
+        return launch_tiles("mm_back_tile", mm_tile_kernel<float, true>, a, kTile, kTile, 256, st);
+    if (a.K % 8 || a.C % 8) return launch_tiles("mm_back_tile", mm_tile_kernel<bf16_t, true>, a, kTile, kTile, 256, st);
+    return launch_tiles("mm_back_mfma", mm_back_mfma_kernel, a, BM, BP, kThreads, st);
 }
 
-hipError_t launch_mm8(const pr2_wgrad_desc& d, const MmArgs& a, hipStream_t st) {
-    if (d.act_dtype == PR2_BF16) return launch_tiles("mm8_tile", mm8_tile_kernel<bf16_t>, a, kTile, kTile, 256, st);
-    return launch_tiles("mm8_tile", mm8_tile_kernel<float>, a, kTile, kTile, 256, st);
+template <typename O>
+hipError_t launch_mm8(const MmArgs& a, hipStream_t st) {
+    if (!mfma_ok(a, 1)) return launch_tiles("mm8_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
+    if (few_rows(a)) return launch_tiles("mm8_few", mm_few_kernel<int8_t, O>, a, kFewM, kFewP, 256, st);
+    return launch_tiles("mm8_mfma", mm_mfma_kernel<int8_t, O>, a, BM, BP, kThreads, st);
 }
 
 }  // namespace
@@ -384,7 +1040,7 @@ pr2_status pr2_grouped_mm_quant(const pr2_wgrad_desc* desc, const int8_t* q, con
     const MmArgs a{q, Wq, offsets, route_of_row, out, row_scale, w_scale, (int)d.R, (int)d.Rx, d.n_in, d.n_out,
                    d.N, d.k};
     const hipError_t e = d.Rx == 0 ? launch_zero(out, d.R * d.n_out * act_bytes(d), st)
-                                   : launch_mm8(d, a, st);
+                                   : d.act_dtype == PR2_BF16 ? launch_mm8<bf16_t>(a, st) : launch_mm8<float>(a, st);
     if (e != hipSuccess) return hip_fail(e, "grouped_mm_quant launch");
     return ok();
 }
