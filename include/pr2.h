@@ -670,8 +670,8 @@ pr2_status pr2_swiglu_quant(int64_t R, int32_t m, int act_dtype, const void* au,
  * Each output may be NULL, q goes with one of scale and row_scale.  h_out and y may lie on x or
  * residual (not both on the same); other overlaps are not allowed.  d <= 32768, T < 2^31, 16-byte
  * alignment of all but the fp32 tensors.  Sums in fp32: rows whose mean h^2 passes fp32's range
- * (magnitudes near 2^64) get r = 0.  A NaN or an infinity in a row reaches that row alone.  T = 0 is
- * a no-op.
+ * (magnitudes near 2^64) get r = 0.  A row's results have the same bits in any batch, and a NaN or an
+ * infinity in a row reaches that row alone.  T = 0 is a no-op.
  */
 pr2_status pr2_rms_norm(int64_t T, int32_t d, int act_dtype, float eps, const void* x,
                         const void* residual, const float* weight, void* h_out, void* y,
@@ -688,7 +688,7 @@ size_t pr2_rms_norm_workspace_bytes(int64_t T, int32_t d);
  *   use as the residual stream).  dx is the gradient of x and of residual alike; it may be dy, dh or h.
  *   dweight [d] fp32, overwritten, or NULL when not wanted (then no workspace is needed)
  *   ws >= pr2_rms_norm_workspace_bytes(T, d)
- * A row's gradient depends on that row alone.  Sums over rows in fp32 in a fixed order.  T = 0 writes
+ * A row of dx has the same bits in any batch.  Sums over rows in fp32 in a fixed order.  T = 0 writes
  * zeros to dweight.
  */
 pr2_status pr2_rms_norm_backward(int64_t T, int32_t d, int act_dtype, const void* dy, const void* dh,

@@ -6,6 +6,7 @@
 //
 // A row without a source and the rows behind the last expert's are zeros.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "chunk.h"
@@ -30,6 +31,11 @@ struct MmArgs {
     int K, C;                   // length of the sums, columns of out
     int N, k;
 };
+
+// Outputs of at least this much are written past the caches, half the size of the last-level cache: the
+// tiles that run meanwhile find more of their weights and rows there (16384 tokens, 8 of 64 or 128 experts, bf16
+// 1 to 4 % of the product, 8 bits 3 to 9 %).
+constexpr int64_t kStreamBytes = 128 << 20;
 
 // the row of x behind row r of the product, -1 if it has none
 __device__ __forceinline__ int source(const MmArgs& a, int r) {
@@ -149,8 +155,29 @@ __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
 constexpr int kStep8 = 128;
 constexpr int kPitch8 = kStep8 + 16;
 
+// 16 bytes from any address, by loads of whole words, put together where they are used: a load that is
+// not 4-byte aligned takes several times as long (517 x 1001 outputs of 999 int8 in 32 x 32 tiles: 13.5 us,
+// of 1000 6.5).  No word is read that holds none of the bytes.  ANY false: the address is 4-byte aligned.
+template <bool ANY> struct Piece {
+    u32x4 w;
+    uint32_t next;
+    __device__ __forceinline__ void load(const unsigned char* p) {
+        typedef u32x4 u32x4_word __attribute__((aligned(4)));
+        const uint32_t drop = ANY ? (uint32_t)(uintptr_t)p & 3 : 0;
+        const uint32_t* words = (const uint32_t*)(p - drop);
+        w = *(const u32x4_word*)words;
+        if (ANY) next = words[drop ? 4 : 3];
+    }
+    // drop: how far behind a word's start p was
+    __device__ __forceinline__ u32x4 bytes(uint32_t drop) const {
+        if (!ANY) return w;
+        return u32x4{__builtin_amdgcn_alignbyte(w[1], w[0], drop), __builtin_amdgcn_alignbyte(w[2], w[1], drop),
+                     __builtin_amdgcn_alignbyte(w[3], w[2], drop), drop ? __builtin_amdgcn_alignbyte(next, w[3], drop) : w[3]};
+    }
+};
+
 // 16 bytes of a row from byte c on, those past the row's n as 0
-__device__ __forceinline__ u32x4 load16_bytes(const int8_t* row, int c, int n) {
+__device__ __forceinline__ u32x4 load16_bytes(const unsigned char* row, int c, int n) {
     if (c + 16 <= n) return *(const u32x4_byte*)(row + c);
     u32x4 w = {0, 0, 0, 0};
     if (c >= n) return w;
@@ -190,13 +217,30 @@ __global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
     const int len = real ? a.K : 0;
     const int expert = real ? t.expert : 0;
     const int8_t* W = (const int8_t*)a.W + (int64_t)expert * a.K * a.C;
-    u32x4 wa[2], wb[2];
+    // pieces of rows tid / 8 and + 32
+    const unsigned char *xr[2], *wr[2];
+    uint32_t xd[2], wd[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = tid / 8 + 32 * i;
+        xr[i] = (const unsigned char*)a.x + (int64_t)max(s_src[r], 0) * a.K;
+        wr[i] = (const unsigned char*)W + (int64_t)min(c0 + r, a.C - 1) * a.K;
+        xd[i] = (uint32_t)(uintptr_t)xr[i] & 3;
+        wd[i] = (uint32_t)(uintptr_t)wr[i] & 3;
+    }
+    Piece<true> wa[2], wb[2];
     auto fetch = [&](int k0) __attribute__((always_inline)) {
+        const int c = k0 + (tid % 8) * 16;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int r = tid / 8 + 32 * i, c = k0 + (tid % 8) * 16;
-            wa[i] = load16_bytes((const int8_t*)a.x + (int64_t)max(s_src[r], 0) * a.K, c, a.K);
-            wb[i] = load16_bytes(W + (int64_t)min(c0 + r, a.C - 1) * a.K, c, a.K);
+            if (k0 + kStep8 <= a.K) {
+                wa[i].load(xr[i] + c);
+                wb[i].load(wr[i] + c);
+            } else {
+                wa[i].w = load16_bytes(xr[i], c, a.K);
+                wb[i].w = load16_bytes(wr[i], c, a.K);
+                xd[i] = wd[i] = 0;
+            }
         }
     };
     const int half = lane >> 5, l32 = lane & 31;
@@ -210,8 +254,8 @@ __global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = (tid / 8 + 32 * i) * kPitch8 + (tid % 8) * 16;
-            *(u32x4*)(A + at) = wa[i];
-            *(u32x4*)(B + at) = wb[i];
+            *(u32x4*)(A + at) = wa[i].bytes(xd[i]);
+            *(u32x4*)(B + at) = wb[i].bytes(wd[i]);
         }
         __syncthreads();
         if (k0 + kStep8 < len) fetch(k0 + kStep8);
@@ -243,15 +287,29 @@ template <typename E> struct Mma;
 template <> struct Mma<bf16_t> {
     using Frag = bf16x8;
     using Acc = f32x4;
+    static constexpr int kSteps = 1;
     __device__ __forceinline__ static Acc mul(Frag a, Frag b, Acc c) {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
+    __device__ __forceinline__ static Acc step(Frag a, Frag b, int, Acc c) { return mul(a, b, c); }
 };
 template <> struct Mma<int8_t> {
     using Frag = i32x4;
     using Acc = i32x4;
+    static constexpr int kSteps = 1;
     __device__ __forceinline__ static Acc mul(Frag a, Frag b, Acc c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+    }
+    __device__ __forceinline__ static Acc step(Frag a, Frag b, int, Acc c) { return mul(a, b, c); }
+};
+
+// fp32: four K values of a row, one a step of v_mfma_f32_16x16x4_f32
+template <> struct Mma<float> {
+    using Frag = f32x4;
+    using Acc = f32x4;
+    static constexpr int kSteps = 4;
+    __device__ __forceinline__ static Acc step(const Frag& a, const Frag& b, int k, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
     }
 };
 
@@ -341,9 +399,9 @@ constexpr int kThreads = 512;
 constexpr int kGroups = 8;                  // copies of 8 rows per wavefront and slice
 constexpr int kStageB = (BM + BP) * kRowB;
 
-template <typename E, typename O>
+template <typename E, typename O, bool STREAM>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-mm_mfma_kernel(MmArgs a) {
+mm_wide_kernel(MmArgs a) {
     using M = Mma<E>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStageB];
     RowTile t;
@@ -556,7 +614,7 @@ mm_mfma_kernel(MmArgs a) {
         if (r >= t.rows) continue;
         bf16_t* to = (bf16_t*)a.out + (int64_t)(t.row0 + r) * a.C + col;
         if (left >= 8) {
-            store16<false>(to, v);
+            store16<STREAM>(to, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -571,7 +629,6 @@ mm_mfma_kernel(MmArgs a) {
 constexpr int kFewM = 64, kFewP = 128;
 constexpr int kFewStageB = (kFewM + kFewP) * kRowB;
 constexpr int kFewStages = 3;
-constexpr int kFewRows = 32;                // rows per expert up to which it is taken
 
 template <typename E, typename O>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
@@ -579,7 +636,7 @@ mm_few_kernel(MmArgs a) {
     using M = Mma<E>;
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kFewStages * kFewStageB];
     RowTile t;
-    if (!find_tile(a.offsets, a.N, a.R, kFewM, (a.C + kFewP - 1) / kFewP, block_number(), &t)) return;
+    if (!find_tile<true>(a.offsets, a.N, a.R, kFewM, (a.C + kFewP - 1) / kFewP, block_number(), &t)) return;
     if (t.expert >= a.N) {
         zero_tile<O>(a, t, kFewP, 256);
         return;
@@ -610,8 +667,10 @@ mm_few_kernel(MmArgs a) {
         if (left >= kRowB) dma16_at(from, off, to);
         else dma16(chunk * 16 < left ? from + off : kZeros, to);
     };
-    auto issue = [&](int kt) __attribute__((always_inline)) {
-        unsigned char* st = lds + (kt % kFewStages) * kFewStageB;
+    const int turn = (5 * t.panel + 3 * t.expert) % nk;
+    auto issue = [&](int step) __attribute__((always_inline)) {
+        const int kt = step + turn < nk ? step + turn : step + turn - nk;
+        unsigned char* st = lds + (step % kFewStages) * kFewStageB;
         const int left = kt < whole ? kRowB : kb - kt * kRowB;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -683,6 +742,341 @@ mm_few_kernel(MmArgs a) {
     }
 }
 
+constexpr int kMidM = 128, kMidP = 128, kMidStages = 2;
+constexpr int kMidStageB = (kMidM + kMidP) * kRowB;
+
+template <typename E, typename O>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+mm_mid_kernel(MmArgs a) {
+    using M = Mma<E>;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kMidStages * kMidStageB];
+    RowTile t;
+    if (!find_tile<true>(a.offsets, a.N, a.R, kMidM, (a.C + kMidP - 1) / kMidP, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<O>(a, t, kMidP, 256);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c0 = t.panel * kMidP;
+    const int kb = a.K * (int)sizeof(E);
+    // copies: weight rows 32 wave .. + 31 (four of 8), rows 32 wave .. + 31 (four, fewer past the end)
+    const int chunk0 = (lane & 7) ^ swz(lane >> 3);
+    const unsigned char* wb = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + c0) * kb;
+    const unsigned char* xb = (const unsigned char*)a.x + (a.route ? 0 : (int64_t)t.row0 * kb);
+    uint32_t woff[4], xoff[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        woff[i] = (uint32_t)min(32 * wave + 8 * i + lane / 8, a.C - 1 - c0) * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
+    const int nx = max(0, min(4, (t.rows - 32 * wave + 7) / 8));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = min(32 * wave + 8 * i + lane / 8, t.rows - 1);
+        const int row = a.route ? min(max(a.route[t.row0 + r], 0) / a.k, a.Rx - 1) : r;
+        xoff[i] = (uint32_t)row * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
+    }
+    const int whole = kb / kRowB;
+    const int nk = max(2, (kb + kRowB - 1) / kRowB);
+    auto copy = [&](const unsigned char* from, uint32_t off, int chunk, int left, unsigned char* to)
+        __attribute__((always_inline)) {
+        if (left >= kRowB) dma16_at(from, off, to);
+        else dma16(chunk * 16 < left ? from + off : kZeros, to);
+    };
+    const int turn = (5 * t.panel + 3 * t.expert) % nk;
+    auto issue = [&](int step) __attribute__((always_inline)) {
+        const int kt = step + turn < nk ? step + turn : step + turn - nk;
+        unsigned char* st = lds + (step % kMidStages) * kMidStageB;
+        const int left = kt < whole ? kRowB : kb - kt * kRowB;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            copy(wb + kt * kRowB, woff[i], chunk0 ^ (i & 1), left, st + (kMidM + 32 * wave + 8 * i) * kRowB);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < nx) copy(xb + kt * kRowB, xoff[i], chunk0 ^ (i & 1), left, st + (32 * wave + 8 * i) * kRowB);
+    };
+    const int lrow = lane & 15, grp = lane >> 4;
+    const int cperm = ((grp & 1) << 1) | (grp >> 1);
+    int kpos[2];
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
+    const int wr = wave >> 1, wc = wave & 1;
+    const int a0 = wr * 64 * kRowB, b0 = (kMidM + 64 * wc) * kRowB;
+    typename M::Acc acc[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
+    const int mi = (t.rows - 64 * wr + 15) / 16;
+    issue(0);
+    for (int kt = 0; kt < nk; ++kt) {
+        wait_vmcnt<0>();
+        __builtin_amdgcn_s_waitcnt(0xc07f);      // lgkmcnt(0)
+        plain_barrier();
+        if (kt + 1 < nk) issue(kt + 1);
+        const unsigned char* st = lds + (kt % kMidStages) * kMidStageB;
+        auto frag = [&](int at) __attribute__((always_inline)) {
+            return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(st + at));
+        };
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            typename M::Frag w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = frag(b0 + 16 * j * kRowB + kpos[ks]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i >= mi) continue;
+                const typename M::Frag x = frag(a0 + 16 * i * kRowB + kpos[ks]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = M::mul(w[j], x, acc[i][j]);
+            }
+        }
+    }
+    // lane l holds columns 4 (l / 16) .. + 3 of row l % 16
+    const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
+    f32x4 s4[4];
+    const int col = c0 + 64 * wc + 4 * grp;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s4[j] = sizeof(E) == 1 ? four_scales(sw, col + 16 * j, a.C) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 64 * wr + 16 * i + lrow;
+        if (r >= t.rows) continue;
+        const int src = source(a, t.row0 + r);
+        const float sr = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+        O* row = (O*)a.out + (int64_t)(t.row0 + r) * a.C;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_four(row, col + 16 * j, a.C, finish<E>(acc[i][j], src >= 0, sr, s4[j]));
+    }
+}
+
+// Few rows or few outputs: what counts is how many workgroups there are and how long each one's chain of
+// loads is.  32 rows x 32 columns, the four wavefronts of a workgroup take every fourth 128 bytes
+// of K, straight from memory into the MFMAs' layout (a fragment is 16 bytes of a row, from any
+// address), two pairs of 64 bytes in flight; their sums meet in LDS, in order.
+template <typename E, typename O, bool ANY>
+__global__ void __launch_bounds__(256) mm_thin_kernel(MmArgs a) {
+    using M = Mma<E>;
+    using Acc = typename M::Acc;
+    constexpr int RB = 2, CB = 2, kRows = 16 * RB, kCols = 16 * CB;
+    __shared__ __attribute__((aligned(16))) Acc sums[4][RB * CB][64];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, kRows, (a.C + kCols - 1) / kCols, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<O>(a, t, kCols, 256);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lrow = lane & 15, grp = lane >> 4;
+    const int c0 = t.panel * kCols;
+    const int kb = a.K * (int)sizeof(E);
+    const unsigned char *x[RB], *w[CB];
+    uint32_t xd[RB], wd[CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        const int src = source(a, t.row0 + min(16 * i + lrow, t.rows - 1));
+        x[i] = (const unsigned char*)a.x + (int64_t)max(src, 0) * kb;
+        xd[i] = (uint32_t)(uintptr_t)x[i] & 3;
+    }
+#pragma unroll
+    for (int j = 0; j < CB; ++j) {
+        w[j] = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + min(c0 + 16 * j + lrow, a.C - 1)) * kb;
+        wd[j] = (uint32_t)(uintptr_t)w[j] & 3;
+    }
+    Acc acc[RB][CB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
+    struct Set {
+        Piece<ANY> x[2][RB], w[2][CB];
+    };
+    auto mul = [&](const Set& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            typename M::Frag fx[RB], fw[CB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) fx[i] = __builtin_bit_cast(typename M::Frag, s.x[h][i].bytes(xd[i]));
+#pragma unroll
+            for (int j = 0; j < CB; ++j) fw[j] = __builtin_bit_cast(typename M::Frag, s.w[h][j].bytes(wd[j]));
+#pragma unroll
+            for (int k = 0; k < M::kSteps; ++k)     // (a step of every block before the next: none waits for its own sum)
+#pragma unroll
+                for (int i = 0; i < RB; ++i)
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) acc[i][j] = M::step(fw[j], fx[i], k, acc[i][j]);
+        }
+    };
+    auto load = [&](Set& s, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) s.w[h][j].load(w[j] + at + 64 * h + 16 * grp);
+#pragma unroll
+            for (int i = 0; i < RB; ++i) s.x[h][i].load(x[i] + at + 64 * h + 16 * grp);
+        }
+    };
+    int at = 128 * wave;
+    Set s0, s1;
+    const int whole = kb - 128;             // last place with 128 bytes behind it
+    if (at <= whole) load(s0, at);
+    for (; at <= whole; at += 1024) {
+        const bool two = at + 512 <= whole;
+        if (two) load(s1, at + 512);
+        mul(s0);
+        if (at + 1024 <= whole) load(s0, at + 1024);
+        if (two) mul(s1);
+    }
+    // the row's last bytes, fewer than 128: of one wavefront, zeros behind them
+    const int rest = kb / 128 * 128;
+    if (rest < kb && (kb / 128) % 4 == wave) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < CB; ++j) {
+                s0.w[h][j].w = load16_bytes(w[j], rest + 64 * h + 16 * grp, kb);
+                wd[j] = 0;
+            }
+#pragma unroll
+            for (int i = 0; i < RB; ++i) {
+                s0.x[h][i].w = load16_bytes(x[i], rest + 64 * h + 16 * grp, kb);
+                xd[i] = 0;
+            }
+        }
+        mul(s0);
+    }
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) sums[wave][i * CB + j][lane] = acc[i][j];
+    __syncthreads();
+    // block b: wavefront b % 4; lane l holds columns 4 (l / 16) .. + 3 of row l % 16
+    const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
+#pragma unroll
+    for (int b0 = 0; b0 < RB * CB; b0 += 4) {
+        const int b = b0 + wave;
+        if (b >= RB * CB) continue;
+        Acc v = sums[0][b][lane];
+#pragma unroll
+        for (int q = 1; q < 4; ++q) v += sums[q][b][lane];
+        const int r = 16 * (b / CB) + lrow, c = c0 + 16 * (b % CB) + 4 * grp;
+        if (r >= t.rows || c >= a.C) continue;
+        const int src = source(a, t.row0 + r);
+        f32x4 s4 = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (sizeof(E) == 1) s4 = four_scales(sw, c, a.C);
+        const float sr = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+        store_four((O*)a.out + (int64_t)(t.row0 + r) * a.C, c, a.C, finish<E>(v, src >= 0, sr, s4));
+    }
+}
+
+// The same of dx = dy W: a wavefront takes every fourth K (n_out) step of 32 (fp32: 16), a lane E columns of
+// E K rows (16 bytes each, 256 bytes of a row by 16 lanes).  MFMA j has the j-th of every lane's columns, so
+// that the lane's own pieces hold its fragments, transposed in registers for bf16 (for fp32 an
+// element is a fragment).
+template <typename T> struct BackMma;
+template <> struct BackMma<bf16_t> {
+    // column j of 8 K rows of 8 columns
+    __device__ __forceinline__ static bf16x8 column(const u32x4 (&w)[8], int j) {
+        u32x4 f;
+        const uint32_t pick = j & 1 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_perm(w[2 * i + 1][j / 2], w[2 * i][j / 2], pick);
+        return __builtin_bit_cast(bf16x8, f);
+    }
+    __device__ __forceinline__ static f32x4 mul(const u32x4 (&w)[8], int j, const u32x4& x, f32x4 c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(column(w, j), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+    }
+};
+template <> struct BackMma<float> {
+    __device__ __forceinline__ static f32x4 mul(const u32x4 (&w)[4], int j, const u32x4& x, f32x4 c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i][j]), __uint_as_float(x[i]), c, 0, 0, 0);
+        return c;
+    }
+};
+
+template <typename T, int RB>
+__global__ void __launch_bounds__(256) mm_back_thin_kernel(MmArgs a) {
+    constexpr int E = Chunk<T>::E;              // columns and K rows of a lane
+    constexpr int kRows = 16 * RB, kCols = 16 * E, kK = 4 * E;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[4][RB * E][64];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, kRows, (a.C + kCols - 1) / kCols, block_number(), &t)) return;
+    if (t.expert >= a.N) {
+        zero_tile<T>(a, t, kCols, 256);
+        return;
+    }
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lrow = lane & 15, grp = lane >> 4;
+    const int c = t.panel * kCols + E * lrow;
+    const T* x[RB];
+#pragma unroll
+    for (int i = 0; i < RB; ++i) x[i] = (const T*)a.x + (int64_t)(t.row0 + min(16 * i + lrow, t.rows - 1)) * a.K;
+    const T* w = (const T*)a.W + (int64_t)t.expert * a.K * a.C;
+    f32x4 acc[RB][E];
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int full = a.C / E, rem = a.C % E;
+    struct Set {
+        u32x4 x[RB], w[E];
+    };
+    auto load = [&](Set& s, int k0) __attribute__((always_inline)) {
+        const int k = k0 + E * grp;
+#pragma unroll
+        for (int i = 0; i < RB; ++i) s.x[i] = load_chunk(x[i], k / E, a.K / E, a.K % E);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            s.w[i] = load_chunk(w + (int64_t)min(k + i, a.K - 1) * a.C, c / E, full, rem);
+            if (k + i >= a.K) s.w[i] = u32x4{0, 0, 0, 0};
+        }
+    };
+    auto mul = [&](const Set& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+#pragma unroll
+            for (int i = 0; i < RB; ++i) acc[i][j] = BackMma<T>::mul(s.w, j, s.x[i], acc[i][j]);
+    };
+    Set s0, s1;
+    int k0 = kK * wave;
+    if (k0 < a.K) load(s0, k0);
+    for (; k0 < a.K; k0 += 8 * kK) {
+        const bool two = k0 + 4 * kK < a.K;
+        if (two) load(s1, k0 + 4 * kK);
+        mul(s0);
+        if (k0 + 8 * kK < a.K) load(s0, k0 + 8 * kK);
+        if (two) mul(s1);
+    }
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < E; ++j) sums[wave][i * E + j][lane] = acc[i][j];
+    __syncthreads();
+    // Lane l of MFMA j holds row l % 16 and of columns E m + j those with m = 4 (l / 16) + v: wavefront q
+    // takes v = q, whose E columns are consecutive.
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        const int r = 16 * i + lrow;
+        if (r >= t.rows) continue;
+        float y[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v += ((const float*)&sums[q][i * E + j][lane])[wave];
+            y[j] = v;
+        }
+        store_chunk((T*)a.out + (int64_t)(t.row0 + r) * a.C, t.panel * 16 + 4 * grp + wave, full, rem, y);
+    }
+}
+
 // dx = dy W on v_mfma_f32_32x32x16_bf16 (n_out and n_in multiples of 8): 256 x 256 outputs, K = n_out in
 // steps of 32 through a ring of four stages.  The rows of dy run along K (64 bytes of each a
 // step); the weights lie along their columns, 32 K rows of 512 bytes, and are read as fragments by the
@@ -699,7 +1093,7 @@ typedef __attribute__((address_space(3))) v4s lds_v4s;
 __device__ __forceinline__ int rswz(int r) { return (r >> 2) & 3; }
 
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-mm_back_mfma_kernel(MmArgs a) {
+mm_back_wide_kernel(MmArgs a) {
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kBStages * kBStageB];
     RowTile t;
     if (!find_tile(a.offsets, a.N, a.R, BM, (a.C + BP - 1) / BP, block_number(), &t)) return;
@@ -907,7 +1301,7 @@ pr2_status check_mm(const pr2_wgrad_desc* desc, bool source_rows) {
         return fail(PR2_ERR_UNSUPPORTED, "n_out = %d or n_in = %d > 2^20", d.n_out, d.n_in);
     if ((int64_t)d.N * d.n_out * d.n_in > (int64_t)1 << 36)
         return fail(PR2_ERR_UNSUPPORTED, "N n_out n_in > 2^36");
-    const int64_t groups = tile_groups(d.R, d.N, kTile, ceil_div(std::max(d.n_out, d.n_in), kTile));
+    const int64_t groups = tile_groups(d.R, d.N, 16, ceil_div(std::max(d.n_out, d.n_in), 32));     // no kernel has more
     if (groups > 0x7fffffff) return fail(PR2_ERR_UNSUPPORTED, "R rows of these widths are more than 2^31 tiles");
     return PR2_OK;
 }
@@ -954,28 +1348,100 @@ hipError_t launch_tiles(const char* name, K kernel, const MmArgs& a, int rows, i
 bool mfma_ok(const MmArgs& a, int64_t element) {
     return a.K * element % 16 == 0 && (!a.route || (int64_t)a.Rx * a.K * element < (int64_t)1 << 32);
 }
-bool few_rows(const MmArgs& a) { return a.R <= (int64_t)kFewRows * a.N; }
 
-hipError_t launch_mm(const pr2_wgrad_desc& d, const MmArgs& a, hipStream_t st) {
-    if (d.act_dtype == PR2_F32)
-        return launch_tiles("mm_tile", mm_tile_kernel<float, false>, a, kTile, kTile, 256, st);
-    if (!mfma_ok(a, 2)) return launch_tiles("mm_tile", mm_tile_kernel<bf16_t, false>, a, kTile, kTile, 256, st);
-    if (few_rows(a)) return launch_tiles("mm_few", mm_few_kernel<bf16_t, bf16_t>, a, kFewM, kFewP, 256, st);
-    return launch_tiles("mm_mfma", mm_mfma_kernel<bf16_t, bf16_t>, a, BM, BP, kThreads, st);
+// Which tile: the one that is expected to take the least time.  In us, fitted to products of 1, 8 and 64
+// experts of 1 to 1024 rows, 256 to 2048 columns, 512 to 4096 bytes of K, bf16 and int8, every kernel
+// at each of the 190 sizes (378 for both types): alone on its CU a tile takes start + chain a slice of 128
+// bytes of K, and where all CUs are busy a CU takes 1 + busy a slice for each of its tiles (wide
+// tiles, one on a CU, in whole rounds).
+// By this rule the products take 1.5 % more than by the best kernel at each size, 20 % at most; with the
+// 256-row tile alone 2.4 times as long at the sizes of one expert.
+struct TileCost {
+    int rows, columns;
+    float start, chain, busy;
+    bool rounds;            // one tile fills a CU
+};
+constexpr TileCost kThinCost{32, 32, 1.8f, 0.11f, 0.16f, false};
+constexpr TileCost kThinAnyCost{32, 32, 1.8f, 0.2f, 0.33f, false};     // rows off 4 bytes
+constexpr TileCost kThinF32Cost{32, 32, 1.8f, 0.11f, 0.2f, false};
+constexpr TileCost kFewCost{kFewM, kFewP, 0.95f, 0.645f, 0.535f, false};
+constexpr TileCost kMidCost{kMidM, kMidP, 1.4f, 0.68f, 0.74f, false};
+constexpr TileCost kWideCost{BM, BP, 3.5f, 0.75f, 2.0f, true};
+constexpr TileCost kTileF32Cost{kTile, kTile, 1.5f, 0.72f, 0.55f, false};
+constexpr TileCost kTileBf16Cost{kTile, kTile, 1.5f, 1.4f, 1.1f, false};
+constexpr TileCost kTile8Cost{kTile, kTile, 1.5f, 0.7f, 0.45f, false};
+constexpr TileCost kBackThin1Cost{16, 128, 1.4f, 0.5f, 0.286f, false};
+constexpr TileCost kBackThin2Cost{32, 128, 1.0f, 0.62f, 0.477f, false};
+constexpr TileCost kBackThin1F32Cost{16, 64, 1.4f, 0.25f, 0.2f, false};
+constexpr TileCost kBackWideCost{BM, BP, 2.6f, 1.16f, 1.6f, true};
+
+float tile_time(const MmArgs& a, int element, const TileCost& t) {
+    constexpr float kCus = 256.0f;
+    // experts with rows, of routes that fall evenly, and their tiles, the last one of each half full
+    const float N = (float)a.N, R = (float)a.R;
+    const float experts = N * (1.0f - expf(-R / N));
+    const float tiles = std::max(experts, R / (float)t.rows + 0.5f * experts);
+    const float items = std::ceil(tiles) * (float)ceil_div(a.C, t.columns);
+    const float slices = (float)a.K * (float)element / 128.0f;
+    const float one = t.start + t.chain * slices, loaded = 1.0f + t.busy * slices;
+    float time = std::max(one, items / kCus * loaded);
+    if (t.rounds) {
+        const float full = std::floor(items / kCus);
+        const float last = items / kCus - full;
+        time = full * std::max(loaded, one) + (last > 0.0f ? one + last * std::max(loaded - one, 0.0f) : 0.0f);
+    }
+    return time;
 }
 
-hipError_t launch_mm_back(const pr2_wgrad_desc& d, const MmArgs& a, hipStream_t st) {
-    if (d.act_dtype == PR2_F32)
-        return launch_tiles("mm_back_tile", mm_tile_kernel<float, true>, a, kTile, kTile, 256, st);
-    if (a.K % 8 || a.C % 8) return launch_tiles("mm_back_tile", mm_tile_kernel<bf16_t, true>, a, kTile, kTile, 256, st);
-    return launch_tiles("mm_back_mfma", mm_back_mfma_kernel, a, BM, BP, kThreads, st);
+template <typename E, typename O>
+hipError_t launch_product(const MmArgs& a, hipStream_t st) {
+    constexpr bool f32 = sizeof(E) == 4, i8 = sizeof(E) == 1;
+    const bool words = a.K * (int)sizeof(E) % 4 == 0;
+    const float thin = tile_time(a, sizeof(E), f32 ? kThinF32Cost : words ? kThinCost : kThinAnyCost);
+    float few = 3e38f, mid = 3e38f, wide = 3e38f, tile = 3e38f;
+    if constexpr (!f32) {
+        if (mfma_ok(a, sizeof(E))) {
+            few = tile_time(a, sizeof(E), kFewCost);
+            mid = tile_time(a, sizeof(E), kMidCost);
+            wide = tile_time(a, sizeof(E), kWideCost);
+        }
+    }
+    if (few == 3e38f) tile = tile_time(a, sizeof(E), f32 ? kTileF32Cost : i8 ? kTile8Cost : kTileBf16Cost);
+    const float least = std::min({thin, few, mid, wide, tile});
+    if (thin == least) {
+        if (words) return launch_tiles("mm_thin", mm_thin_kernel<E, O, false>, a, 32, 32, 256, st);
+        if constexpr (!f32) return launch_tiles("mm_thin", mm_thin_kernel<E, O, true>, a, 32, 32, 256, st);
+    }
+    if (tile == least) {
+        if constexpr (i8) return launch_tiles("mm_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
+        else return launch_tiles("mm_tile", mm_tile_kernel<E, false>, a, kTile, kTile, 256, st);
+    }
+    if constexpr (!f32) {
+        if (few == least) return launch_tiles("mm_few", mm_few_kernel<E, O>, a, kFewM, kFewP, 256, st);
+        if (mid == least) return launch_tiles("mm_mid", mm_mid_kernel<E, O>, a, kMidM, kMidP, 256, st);
+        if constexpr (sizeof(O) == 2)
+            if ((int64_t)a.R * a.C * 2 >= kStreamBytes)
+                return launch_tiles("mm_wide", mm_wide_kernel<E, O, true>, a, BM, BP, kThreads, st);
+        return launch_tiles("mm_wide", mm_wide_kernel<E, O, false>, a, BM, BP, kThreads, st);
+    }
+    return hipErrorUnknown;         // (fp32 has the two above)
 }
 
-template <typename O>
-hipError_t launch_mm8(const MmArgs& a, hipStream_t st) {
-    if (!mfma_ok(a, 1)) return launch_tiles("mm8_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
-    if (few_rows(a)) return launch_tiles("mm8_few", mm_few_kernel<int8_t, O>, a, kFewM, kFewP, 256, st);
-    return launch_tiles("mm8_mfma", mm_mfma_kernel<int8_t, O>, a, BM, BP, kThreads, st);
+template <typename T>
+hipError_t launch_back(const MmArgs& a, hipStream_t st) {
+    constexpr bool f32 = sizeof(T) == 4;
+    const bool mfma = !f32 && a.K % 8 == 0 && a.C % 8 == 0;
+    const float one = tile_time(a, sizeof(T), f32 ? kBackThin1F32Cost : kBackThin1Cost);
+    const float two = f32 ? 3e38f : tile_time(a, sizeof(T), kBackThin2Cost);
+    const float wide = tile_time(a, sizeof(T), mfma ? kBackWideCost : f32 ? kTileF32Cost : kTileBf16Cost);
+    const float least = std::min({one, two, wide});
+    if (one == least)
+        return launch_tiles("mm_back_thin", mm_back_thin_kernel<T, 1>, a, 16, 16 * Chunk<T>::E, 256, st);
+    if constexpr (!f32) {
+        if (two == least) return launch_tiles("mm_back_thin", mm_back_thin_kernel<T, 2>, a, 32, 128, 256, st);
+        if (mfma) return launch_tiles("mm_back_wide", mm_back_wide_kernel, a, BM, BP, kThreads, st);
+    }
+    return launch_tiles("mm_back_tile", mm_tile_kernel<T, true>, a, kTile, kTile, 256, st);
 }
 
 }  // namespace
@@ -999,7 +1465,8 @@ pr2_status pr2_grouped_mm(const pr2_wgrad_desc* desc, const void* x, const void*
     const hipStream_t st = (hipStream_t)stream;
     const MmArgs a{x, W, offsets, route_of_row, out, nullptr, nullptr, (int)d.R, (int)d.Rx, d.n_in, d.n_out, d.N, d.k};
     const hipError_t e = d.Rx == 0 ? launch_zero(out, d.R * d.n_out * act_bytes(d), st)
-                                   : launch_mm(d, a, st);
+                        : d.act_dtype == PR2_BF16 ? launch_product<bf16_t, bf16_t>(a, st)
+                                                  : launch_product<float, float>(a, st);
     if (e != hipSuccess) return hip_fail(e, "grouped_mm launch");
     return ok();
 }
@@ -1016,7 +1483,8 @@ pr2_status pr2_grouped_mm_backward(const pr2_wgrad_desc* desc, const void* dy, c
         return s;
     if ((s = device_ready()) != PR2_OK) return s;
     const MmArgs a{dy, W, offsets, nullptr, dx, nullptr, nullptr, (int)d.R, (int)d.R, d.n_out, d.n_in, d.N, 1};
-    const hipError_t e = launch_mm_back(d, a, (hipStream_t)stream);
+    const hipStream_t st = (hipStream_t)stream;
+    const hipError_t e = d.act_dtype == PR2_BF16 ? launch_back<bf16_t>(a, st) : launch_back<float>(a, st);
     if (e != hipSuccess) return hip_fail(e, "grouped_mm_backward launch");
     return ok();
 }
@@ -1040,7 +1508,8 @@ pr2_status pr2_grouped_mm_quant(const pr2_wgrad_desc* desc, const int8_t* q, con
     const MmArgs a{q, Wq, offsets, route_of_row, out, row_scale, w_scale, (int)d.R, (int)d.Rx, d.n_in, d.n_out,
                    d.N, d.k};
     const hipError_t e = d.Rx == 0 ? launch_zero(out, d.R * d.n_out * act_bytes(d), st)
-                                   : d.act_dtype == PR2_BF16 ? launch_mm8<bf16_t>(a, st) : launch_mm8<float>(a, st);
+                                   : d.act_dtype == PR2_BF16 ? launch_product<int8_t, bf16_t>(a, st)
+                                                  : launch_product<int8_t, float>(a, st);
     if (e != hipSuccess) return hip_fail(e, "grouped_mm_quant launch");
     return ok();
 }

@@ -31,18 +31,20 @@ template <> __device__ __forceinline__ float sigmoid<bf16_t>(float a) {
 }
 template <> __device__ __forceinline__ float sigmoid<float>(float a) { return 1.0f / (1.0f + expf(-a)); }
 
-template <typename T, bool SWIGLU, typename G>
-__device__ __forceinline__ void row_piece(const G& g, const T* x, int C, int i, float* v) {
-    Chunk<T>::open(g.load(x, i), v);
+// the values of a piece: x, or silu(a) u
+template <typename T, bool SWIGLU, int E>
+__device__ __forceinline__ void open_piece(const u32x4& x, const u32x4& second, float* v) {
+    Chunk<T>::open(x, v);
     if (!SWIGLU) return;
-    float u[G::E];
-    Chunk<T>::open(g.load(x + C, i), u);
+    float u[E];
+    Chunk<T>::open(second, u);
 #pragma unroll
-    for (int j = 0; j < G::E; ++j) v[j] = v[j] * sigmoid<T>(v[j]) * u[j];
+    for (int j = 0; j < E; ++j) v[j] = v[j] * sigmoid<T>(v[j]) * u[j];
 }
 
 template <typename G>
 __device__ __forceinline__ void store_row_piece(const G& g, int8_t* row, int i, const float* v, const RowStep& s) {
+    if (!g.any(i)) return;
     uint32_t q[G::E / 4];
     quantise_row<G::E>(v, s, q);
     if (!g.on(i)) return;
@@ -71,19 +73,28 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) quant_kernel(QuantArgs 
     using G = RowGroup<T, NW, F>;
     constexpr int E = G::E, P = G::kPieces;
     constexpr int kRows = NW == 1 ? 4 : 1;
-    __shared__ uint32_t red[2 * NW];
+    __shared__ uint32_t red[8 * NW];
     int turn = 0;
     const int sub = NW == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const G g(a.C, NW == 1 ? threadIdx.x & 63 : threadIdx.x);
     for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.R; row += (int64_t)gridDim.x * kRows) {
         const T* x = (const T*)a.x + row * (SWIGLU ? 2 : 1) * a.C;
-        float v[F];
-        uint32_t m = 0;
+        u32x4 raw[P], second[P];
 #pragma unroll
-        for (int i = 0; i < P; ++i) row_piece<T, SWIGLU>(g, x, a.C, i, v + i * E);
-        m = largest<F>(v);
-        m = row_reduce<NW>(m, red, turn, MaxU32());
-        const RowStep s = row_step(m);
+        for (int i = 0; i < P; ++i) {
+            raw[i] = g.load(x, i);
+            if (SWIGLU) second[i] = g.load(x + a.C, i);
+        }
+        float v[F];
+        uint32_t m[P];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            m[i] = 0;
+            if (!g.any(i)) continue;
+            open_piece<T, SWIGLU, E>(raw[i], second[i], v + i * E);
+            m[i] = largest<E>(v + i * E);
+        }
+        const RowStep s = row_step(row_max<NW, P, 1>(m, red, turn));
         if (g.lane == 0) a.scale[row] = s.step;
 #pragma unroll
         for (int i = 0; i < P; ++i) store_row_piece(g, a.q + row * a.C, i, v + i * E, s);
@@ -95,23 +106,22 @@ template <typename T, bool SWIGLU>
 __global__ void __launch_bounds__(1024) quant_wide_kernel(QuantArgs a) {
     using G = RowGroup<T, 16, Chunk<T>::E>;
     constexpr int E = G::E;
-    __shared__ uint32_t red[32];
+    __shared__ uint32_t red[8 * 16];
     int turn = 0;
     const G all(a.C, threadIdx.x);
     const int pieces = (a.C + E * G::kLanes - 1) / (E * G::kLanes);
     for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
         const T* x = (const T*)a.x + row * (SWIGLU ? 2 : 1) * a.C;
-        uint32_t m = 0;
+        uint32_t m[1] = {0};
         float v[E];
         for (int i = 0; i < pieces; ++i) {
-            row_piece<T, SWIGLU>(all, x, a.C, i, v);
-            m = max(m, largest<E>(v));
+            open_piece<T, SWIGLU, E>(all.load(x, i), SWIGLU ? all.load(x + a.C, i) : u32x4{0, 0, 0, 0}, v);
+            m[0] = max(m[0], largest<E>(v));
         }
-        m = row_reduce<16>(m, red, turn, MaxU32());
-        const RowStep s = row_step(m);
+        const RowStep s = row_step(row_max<16, 1, 1>(m, red, turn));
         if (threadIdx.x == 0) a.scale[row] = s.step;
         for (int i = 0; i < pieces; ++i) {
-            row_piece<T, SWIGLU>(all, x, a.C, i, v);
+            open_piece<T, SWIGLU, E>(all.load(x, i), SWIGLU ? all.load(x + a.C, i) : u32x4{0, 0, 0, 0}, v);
             store_row_piece(all, a.q + row * a.C, i, v, s);
         }
     }
@@ -129,10 +139,15 @@ void quant_launch(const QuantArgs& a, hipStream_t st) {
 template <typename T, bool SWIGLU>
 hipError_t launch_quant(const QuantArgs& a, hipStream_t st) {
     LaunchScope scope(SWIGLU ? "swiglu_quant" : "act_quant", st);
+    const bool few = a.R <= 8 * kCus;           // (more lanes a row, as for the norm)
     if (a.C <= 512) quant_launch<T, SWIGLU, 1, 8>(a, st);
+    else if (a.C <= 2048 && few) quant_launch<T, SWIGLU, 4, 8>(a, st);
     else if (a.C <= 1024) quant_launch<T, SWIGLU, 1, 16>(a, st);
     else if (a.C <= 2048) quant_launch<T, SWIGLU, 1, 32>(a, st);
+    else if (a.C <= 4096) quant_launch<T, SWIGLU, 4, 16>(a, st);
+    else if (a.C <= 8192 && few) quant_launch<T, SWIGLU, 16, 8>(a, st);
     else if (a.C <= 8192) quant_launch<T, SWIGLU, 4, 32>(a, st);
+    else if (a.C <= 16384) quant_launch<T, SWIGLU, 16, 16>(a, st);
     else if (a.C <= kHeld) quant_launch<T, SWIGLU, 16, 32>(a, st);
     else
         hipLaunchKernelGGL((quant_wide_kernel<T, SWIGLU>), dim3((unsigned)std::min<int64_t>(a.R, 2 * kCus)),

@@ -19,6 +19,11 @@ template <typename T, int NW, int F> struct RowGroup {
     __device__ __forceinline__ RowGroup(int d_, int lane_) : d(d_), lane(lane_) {}
     __device__ __forceinline__ int column(int i) const { return (lane + i * kLanes) * E; }
     __device__ __forceinline__ bool on(int i) const { return column(i) < d; }
+    // Whether any lane of the wavefront has a piece i (a scalar branch).  Rows on 16 wavefronts leave many
+    // without one (quantising 3600 rows of 9000 36 -> 30 us); on fewer the branch costs more than it saves.
+    __device__ __forceinline__ bool any(int i) const {
+        return NW < 16 || __builtin_amdgcn_readfirstlane(column(i)) < d;
+    }
     __device__ __forceinline__ bool narrow() const { return d < E; }
     __device__ __forceinline__ int start(int i) const { return max(0, min(column(i), d - E)); }
     __device__ __forceinline__ int skip(int i) const { return column(i) - start(i); }
@@ -61,12 +66,12 @@ template <typename T, int NW, int F> struct RowGroup {
     }
 };
 
-// one step of a reduction inside the wavefront: the value of lane ^ n
-template <int n>
-__device__ __forceinline__ uint32_t lane_xor(uint32_t v) {
-    if (n == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, false);
-    if (n == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, false);
-    return (uint32_t)__shfl_xor((int)v, n);
+// the value of another lane by DPP: of lane ^ 1 and lane ^ 2, and of a mirrored lane of 8 and of 16,
+// which stands for lane ^ 4 and lane ^ 8 once the lanes of 4 and of 8 are alike
+enum { XOR1 = 0xb1, XOR2 = 0x4e, MIRROR8 = 0x141, MIRROR16 = 0x140 };
+template <int ctrl>
+__device__ __forceinline__ uint32_t from_lane(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false);
 }
 struct AddF32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
@@ -76,32 +81,63 @@ struct AddF32 {
 struct MaxU32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
 };
+// over 16 lanes, as a tree of neighbours
 template <typename Op>
-__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, Op op) {
-    v = op(v, lane_xor<1>(v));
-    v = op(v, lane_xor<2>(v));
-    v = op(v, lane_xor<4>(v));
-    v = op(v, lane_xor<8>(v));
-    v = op(v, lane_xor<16>(v));
-    return op(v, lane_xor<32>(v));
+__device__ __forceinline__ uint32_t reduce16(uint32_t v, Op op) {
+    v = op(v, from_lane<XOR1>(v));
+    v = op(v, from_lane<XOR2>(v));
+    v = op(v, from_lane<MIRROR8>(v));
+    return op(v, from_lane<MIRROR16>(v));
 }
 
-// A reduction over the NW wavefronts of a row, the same bits in every lane.  `red` holds 2 NW
-// words; `turn` alternates, so that one barrier is enough: the words of a turn are written again
-// only behind the next turn's barrier, which every wavefront reaches after it read them.
-template <int NW, typename Op>
-__device__ __forceinline__ uint32_t row_reduce(uint32_t v, uint32_t* red, int& turn, Op op) {
-    v = wave_reduce(v, op);
-    if (NW == 1) return v;
-    uint32_t* r = red + turn * NW;
-    turn ^= 1;
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) r[wave] = v;
-    __syncthreads();
-    v = r[0];
+// Over a row of NW wavefronts with P pieces in each lane: every piece over its groups of 16 lanes, each
+// group's NW P pieces as a tree of neighbours in the row's order, then the four groups.  Pieces behind the
+// row's end are zeros, so the result does not depend on how many wavefronts and pieces hold the row: a
+// row's norm has the same bits in any batch.  `red` holds 8 NW MOST words (MOST: the most pieces of a
+// reduction in the kernel); `turn` alternates, so that one barrier is enough: the words of a turn are
+// written again only behind the next turn's barrier, which every wavefront reaches after it read them.
+template <int NW, int P, int MOST, typename Op>
+__device__ __forceinline__ uint32_t row_reduce(uint32_t (&v)[P], uint32_t* red, int& turn, Op op) {
 #pragma unroll
-    for (int w = 1; w < NW; ++w) v = op(v, r[w]);
-    return v;
+    for (int i = 0; i < P; ++i) v[i] = reduce16(v[i], op);
+    uint32_t w;
+    if (NW == 1) {
+#pragma unroll
+        for (int n = 1; n < P; n *= 2)
+#pragma unroll
+            for (int i = 0; i < P; i += 2 * n) v[i] = op(v[i], v[i + n]);
+        w = v[0];
+    } else {
+        constexpr int n = NW * P, M = n < 16 ? 1 : n / 16;      // pieces, and those that a lane joins
+        uint32_t* r = red + turn * (4 * NW * MOST);
+        turn ^= 1;
+        const int group = (threadIdx.x & 63) >> 4, at = threadIdx.x & 15;
+        if (at == 0) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) r[4 * (i * NW + (threadIdx.x >> 6)) + group] = v[i];
+        }
+        __syncthreads();
+        uint32_t u[M];
+#pragma unroll
+        for (int m = 0; m < M; ++m) u[m] = at * M + m < n ? r[4 * (at * M + m) + group] : 0u;
+#pragma unroll
+        for (int q = 1; q < M; q *= 2)
+#pragma unroll
+            for (int m = 0; m < M; m += 2 * q) u[m] = op(u[m], u[m + q]);
+        w = reduce16(u[0], op);
+    }
+    const uint32_t a = __builtin_amdgcn_readlane(w, 0), b = __builtin_amdgcn_readlane(w, 16);
+    const uint32_t c = __builtin_amdgcn_readlane(w, 32), d = __builtin_amdgcn_readlane(w, 48);
+    return op(op(a, b), op(c, d));
+}
+
+// the row's largest magnitude (bits), of its pieces'
+template <int NW, int P, int MOST>
+__device__ __forceinline__ uint32_t row_max(const uint32_t (&m)[P], uint32_t* red, int& turn) {
+    uint32_t one[1] = {m[0]};
+#pragma unroll
+    for (int i = 1; i < P; ++i) one[0] = max(one[0], m[i]);
+    return row_reduce<NW, 1, MOST>(one, red, turn, MaxU32());
 }
 
 // The row form of 8 bits: q = rint(v / step), step = fp32(max(m, 2^-100) / 127) with m (its bits) the

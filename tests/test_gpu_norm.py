@@ -1,8 +1,8 @@
 """The norm in front of the layer and the row form in 8 bits, against the float64 definitions.
 
 Tolerances, set before any run.  h is compared bit for bit.  A sum of d squares or products over
-lanes, wavefronts and a tree has at most 32 + 6 + 16 additions in a row and the product's rounding: 55
-roundings of 2^-24.  r takes half of that (a root) and four more roundings: 32 2^-24; y two more;
+a piece, the lanes and the pieces has at most 55 roundings of 2^-24 in a row (8 elements, a tree of 6 over the
+lanes, one of 7 over 128 pieces, and the products').  r takes half of that (a root) and four more roundings: 32 2^-24; y two more;
 so y is within 36 2^-24 relatively, and within 2^-8 more as bf16.  dx = dh + r (g - n mean(g n)),
 n = h r: every factor of its terms adds a rounding, so dx is within 70 2^-24 of r (|g| + |n| mean|g n|)
 and 2 2^-24 of |dh|, and 2^-8 of itself as bf16.  dweight over T rows is within (T + 4) 2^-24 of the
@@ -198,6 +198,31 @@ def test_backward_against_differences():
         e = np.zeros(d)
         e[i] = step
         assert abs((loss(x, w + e) - loss(x, w - e)) / (2 * step) - host(dw)[i]) < 1e-5
+
+
+@TYPES
+@pytest.mark.parametrize("d", [300, 600, 1500, 2048, 3000, 5000, 8192])
+def test_a_row_has_the_same_bits_in_any_batch(d, bf16):
+    import torch
+    from paper_2606_00395_amd import binding as B
+    T = 2600
+    s = forward(T, d, bf16)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    dy = torch.randn((T, d), generator=g, device="cuda").to(s["x"].dtype)
+    dx, a8, b8 = torch.empty_like(dy), torch.empty_like(s["q"]), torch.empty(T, device="cuda")
+    B.rms_norm_backward(dy, s["h"], s["rstd"], s["w"], dx)
+    B.act_quant(s["y"], a8, b8)
+    for n in (1, 7, 300):
+        c = {k: v[-n:].clone() for k, v in s.items() if k not in ("w",)}
+        B.rms_norm(c["x"], s["w"], c["y"].zero_(), residual=c["res"], h_out=c["h"].zero_(), rstd_out=c["rstd"].zero_(),
+                   q=c["q"].zero_(), scale=c["e"].zero_())
+        B.rms_norm(c["x"], s["w"], residual=c["res"], q=c["q8"].zero_(), row_scale=c["rs"].zero_())
+        for k in ("y", "h", "rstd", "q", "e", "q8", "rs"):
+            assert torch.equal(c[k], s[k][-n:]), (n, k)
+        part, q, rs = torch.empty_like(dx[-n:]), torch.empty_like(a8[-n:]), torch.empty(n, device="cuda")
+        B.rms_norm_backward(dy[-n:].clone(), c["h"], c["rstd"], s["w"], part)
+        B.act_quant(c["y"], q, rs)
+        assert torch.equal(part, dx[-n:]) and torch.equal(q, a8[-n:]) and torch.equal(rs, b8[-n:])
 
 
 def test_no_rows():
