@@ -645,7 +645,7 @@ pr2_status pr2_grouped_mm_quant(const pr2_wgrad_desc* desc, const int8_t* q, con
 /*
  * Rows in 8 bits with one scale each (the row form), of x [R, C] act_dtype: with m the row's largest
  * magnitude
- *   row_scale = fp32(max(m, 2^-100) / 127),  q = rint(x / row_scale)  in [-127, 127],
+ *   row_scale = fp32(max(m, 2^-100) fp32(1 / 127)),  q = rint(x / row_scale)  in [-127, 127],
  * the quotient as in exact arithmetic, ties to even, so that q row_scale is x to half of row_scale.  A row that
  * holds an infinity or a NaN has row_scale NaN and q = 0.  Weights [N, n_out, n_in] brought to
  * this form as N n_out rows are what pr2_grouped_mm_quant reads as Wq and w_scale.

@@ -220,6 +220,7 @@ def rms_norm_backward(dy, h, rstd, weight, dh=None):
 
 
 def row_scale(v):
-    """The step of each row's form in 8 bits."""
+    """The step of each row's form in 8 bits: the product of two fp32 numbers, rounded to fp32."""
     m = np.max(np.abs(np.asarray(v, dtype=np.float64)), axis=1)
-    return np.where(np.isfinite(m), np.maximum(m, 2.0 ** -100) / 127, np.nan)
+    step = np.maximum(m, 2.0 ** -100) * np.float64(np.float32(1) / np.float32(127))
+    return np.where(np.isfinite(m), step.astype(np.float32).astype(np.float64), np.nan)

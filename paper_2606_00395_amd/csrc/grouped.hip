@@ -217,29 +217,29 @@ __global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
     const int len = real ? a.K : 0;
     const int expert = real ? t.expert : 0;
     const int8_t* W = (const int8_t*)a.W + (int64_t)expert * a.K * a.C;
-    // pieces of rows tid / 8 and + 32
-    const unsigned char *xr[2], *wr[2];
-    uint32_t xd[2], wd[2];
+    struct Set {
+        u32x4 a[2], b[2];
+    };
+    const unsigned char *xr[2], *wr[2];             // rows tid / 8 and + 32
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int r = tid / 8 + 32 * i;
         xr[i] = (const unsigned char*)a.x + (int64_t)max(s_src[r], 0) * a.K;
         wr[i] = (const unsigned char*)W + (int64_t)min(c0 + r, a.C - 1) * a.K;
-        xd[i] = (uint32_t)(uintptr_t)xr[i] & 3;
-        wd[i] = (uint32_t)(uintptr_t)wr[i] & 3;
     }
-    Piece<true> wa[2], wb[2];
-    auto fetch = [&](int k0) __attribute__((always_inline)) {
+    auto fetch = [&](Set& s, int k0) __attribute__((always_inline)) {
         const int c = k0 + (tid % 8) * 16;
+        if (k0 + kStep8 <= a.K) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (k0 + kStep8 <= a.K) {
-                wa[i].load(xr[i] + c);
-                wb[i].load(wr[i] + c);
-            } else {
-                wa[i].w = load16_bytes(xr[i], c, a.K);
-                wb[i].w = load16_bytes(wr[i], c, a.K);
-                xd[i] = wd[i] = 0;
+            for (int i = 0; i < 2; ++i) {
+                s.a[i] = *(const u32x4_byte*)(xr[i] + c);
+                s.b[i] = *(const u32x4_byte*)(wr[i] + c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s.a[i] = load16_bytes(xr[i], c, a.K);
+                s.b[i] = load16_bytes(wr[i], c, a.K);
             }
         }
     };
@@ -248,23 +248,30 @@ __global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
     i32x16 acc;
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[v] = 0;
-    if (len) fetch(0);
-    for (int k0 = 0; k0 < len; k0 += kStep8) {
+    // two steps in flight behind the one that is multiplied
+    auto step = [&](Set& s, int k0) __attribute__((always_inline)) {
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int at = (tid / 8 + 32 * i) * kPitch8 + (tid % 8) * 16;
-            *(u32x4*)(A + at) = wa[i].bytes(xd[i]);
-            *(u32x4*)(B + at) = wb[i].bytes(wd[i]);
+            *(u32x4*)(A + at) = s.a[i];
+            *(u32x4*)(B + at) = s.b[i];
         }
         __syncthreads();
-        if (k0 + kStep8 < len) fetch(k0 + kStep8);
+        if (k0 + 2 * kStep8 < len) fetch(s, k0 + 2 * kStep8);
 #pragma unroll
         for (int k = 0; k < kStep8; k += 32) {
             const i32x4 fa = *(const i32x4*)(A + ao * kPitch8 + k + 16 * half);
             const i32x4 fb = *(const i32x4*)(B + bo * kPitch8 + k + 16 * half);
             acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, acc, 0, 0, 0);
         }
+    };
+    Set s0, s1;
+    if (len) fetch(s0, 0);
+    if (kStep8 < len) fetch(s1, kStep8);
+    for (int k0 = 0; k0 < len; k0 += 2 * kStep8) {
+        step(s0, k0);
+        if (k0 + kStep8 < len) step(s1, k0 + kStep8);
     }
     const int c = c0 + bo;
     if (c >= a.C) return;

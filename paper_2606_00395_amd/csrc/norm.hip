@@ -44,6 +44,28 @@ __device__ __forceinline__ uint32_t pack_scale(uint32_t m) {
     return e == 255 ? 255u : (uint32_t)max(e - 6, 1);
 }
 
+// (mean + eps)^-1/2 in two parts, so that y has one fp32 rounding before its own: a y that is rounded to the
+// other side is a whole step of act_dtype off, and may move its packed group's values by a step of theirs.
+struct Root {
+    float hi, lo;
+    bool one;               // no second part
+    // h r w
+    __device__ __forceinline__ float times(float h, float w) const {
+        if (one) return h * hi * w;
+        const float p = hi * w;
+        const float rest = __builtin_fmaf(lo, w, __builtin_fmaf(hi, w, -p));
+        return __builtin_fmaf(h, p, h * rest);
+    }
+};
+__device__ __forceinline__ Root root_of(double x) {
+    const float r0 = 1.0f / sqrtf((float)x);
+    // (sums past fp32's range, no number, or r w past the range where h r w is not)
+    if (!(r0 > 1e-18f && r0 < 1e18f)) return Root{r0, 0.0f, true};
+    const double a = (double)r0, r = a + 0.5 * a * __builtin_fma(-x * a, a, 1.0);       // a Newton step
+    const float hi = (float)r;
+    return Root{hi, (float)(r - (double)hi), false};
+}
+
 // STREAM: the rows are read past the caches
 template <typename T, int NW, int F, bool STREAM>
 __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a) {
@@ -57,7 +79,7 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
     float w[F];
 #pragma unroll
     for (int i = 0; i < P; ++i) g.load_f32(a.w, i, w + i * E);
-    const float inv_d = 1.0f / (float)a.d;
+    const double inv_d = 1.0 / (double)a.d;
     for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.T; row += (int64_t)gridDim.x * kRows) {
         const T* x = (const T*)a.x + row * a.d;
         u32x4 raw[P];
@@ -93,7 +115,8 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             part[i] = __float_as_uint(s);
         }
         const float sum = __uint_as_float(row_reduce<NW, P, P>(part, red, turn, AddF32()));
-        const float r = 1.0f / sqrtf(sum * inv_d + a.eps);
+        const Root root = root_of((double)sum * inv_d + (double)a.eps);
+        const float r = root.hi;
         // (behind the reduction: every element has been read, h may lie where x or the residual does)
         if (a.h) {
 #pragma unroll
@@ -135,7 +158,7 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             if (!g.any(i)) continue;
             float v[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = h[i * E + j] * r * w[i * E + j];
+            for (int j = 0; j < E; ++j) v[j] = root.times(h[i * E + j], w[i * E + j]);
             const u32x4 out = Chunk<T>::close(v);
             if (a.y) g.store((T*)a.y + row * a.d, i, out);
             if (!a.scale) continue;

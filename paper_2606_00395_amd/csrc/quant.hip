@@ -1,7 +1,7 @@
 // Rows in 8 bits with one scale each, what the products with 8-bit weights read: of a tensor, or of
 // silu(a) u.
 //
-//   m = the row's largest magnitude,  scale = max(m, 2^-100) / 127,  q = rint(v / scale)
+//   m = the row's largest magnitude,  scale = max(m, 2^-100) (1 / 127),  q = rint(v / scale)
 //
 // Bound by HBM: a row is read once and held in registers while its maximum is formed (rows above
 // 32768 elements are read again).

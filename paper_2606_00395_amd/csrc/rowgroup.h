@@ -140,8 +140,8 @@ __device__ __forceinline__ uint32_t row_max(const uint32_t (&m)[P], uint32_t* re
     return row_reduce<NW, 1, MOST>(one, red, turn, MaxU32());
 }
 
-// The row form of 8 bits: q = rint(v / step), step = fp32(max(m, 2^-100) / 127) with m (its bits) the
-// row's largest magnitude.  (Below 2^-100 the inverse would leave fp32's range.)
+// The row form of 8 bits: q = rint(v / step), step = fp32(max(m, 2^-100) fp32(1 / 127)) with m (its bits)
+// the row's largest magnitude.  (Below 2^-100 the inverse would leave fp32's range.)
 struct RowStep {
     float step, inverse;
     bool finite;
@@ -149,7 +149,7 @@ struct RowStep {
 __device__ __forceinline__ RowStep row_step(uint32_t m_bits) {
     const float m = fmaxf(__uint_as_float(m_bits), 0x1p-100f);
     const bool finite = m_bits < 0x7f800000u;
-    return RowStep{finite ? m / 127.0f : __uint_as_float(0x7fc00000u), finite ? 127.0f / m : 0.0f, finite};
+    return RowStep{finite ? m * (1.0f / 127.0f) : __uint_as_float(0x7fc00000u), finite ? 127.0f / m : 0.0f, finite};
 }
 // v / step rounded to even as exact arithmetic rounds it: the product with the inverse is off by up to
 // 127 3 2^-24, so that next to a half it may take the wrong side.  The remainder v - q step

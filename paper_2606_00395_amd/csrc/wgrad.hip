@@ -174,6 +174,100 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         if (o + 8 * (v / 4) + v % 4 < a.n_out) to[(int64_t)(8 * (v / 4) + v % 4) * a.n_in] = acc[v];
 }
 
+// Few outputs from rows that are not packed: 32 x 32 per workgroup, each of its four wavefronts takes every
+// fourth 16 rows on v_mfma_f32_16x16x4_f32, straight from memory (a lane loads two columns of a row; MFMA
+// (i, j) has the i-th of the lanes' columns of dy and the j-th of x's), the next 16 rows in flight, and their
+// sums meet in LDS, in order.  The chain of a row step is short then and there are four times as many
+// workgroups (the rule that takes it says what it gains).
+constexpr int kThin = 32;
+template <typename T>
+__global__ void __launch_bounds__(256) wgrad_thin_kernel(WgradArgs a) {
+    typedef typename Chunk<T>::Bits Bits;
+    __shared__ f32x4 sums[4][4][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at = lane & 15, grp = lane >> 4;
+    const int o0 = (int)blockIdx.y * kThin, c0 = (int)blockIdx.x * kThin, e = (int)blockIdx.z;
+    int first, last;
+    expert_rows(a, e, &first, &last);
+    if (a.Rx == 0) last = first;
+    // this lane's columns 2 at and 2 at + 1; those past the matrix read its last one and are not stored
+    int oc[2], cc[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        oc[j] = min(o0 + 2 * at + j, a.n_out - 1);
+        cc[j] = min(c0 + 2 * at + j, a.n_in - 1);
+    }
+    struct Set {
+        Bits y[4][2], x[4][2];      // of rows 4 grp + 0 .. 3
+        bool on[4];
+    };
+    auto load = [&](Set& s, int r0) __attribute__((always_inline)) {
+        int src[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = r0 + 4 * grp + i;
+            src[i] = r < last ? source_row(a, r) : -1;
+            s.on[i] = src[i] >= 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Bits* y = (const Bits*)a.dy + (int64_t)min(r0 + 4 * grp + i, last - 1) * a.n_out;
+            const Bits* x = (const Bits*)a.x + (int64_t)max(src[i], 0) * a.n_in;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s.y[i][j] = y[oc[j]];
+                s.x[i][j] = x[cc[j]];
+            }
+        }
+    };
+    f32x4 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    auto mul = [&](const Set& s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float y[2], x[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                // (a row without a source is zeros in both operands: nothing of it multiplies)
+                y[j] = s.on[q] ? Act<T>::to_f32(__builtin_bit_cast(T, s.y[q][j])) : 0.0f;
+                x[j] = s.on[q] ? Act<T>::to_f32(__builtin_bit_cast(T, s.x[q][j])) : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(y[i], x[j], acc[i][j], 0, 0, 0);
+        }
+    };
+    Set s0, s1;
+    int r = first + 16 * wave;
+    if (r < last) load(s0, r);
+    for (; r < last; r += 128) {
+        const bool two = r + 64 < last;
+        if (two) load(s1, r + 64);
+        mul(s0);
+        if (r + 128 < last) load(s0, r + 128);
+        if (two) mul(s1);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) sums[wave][b][lane] = acc[b / 2][b % 2];
+    __syncthreads();
+    // block b = (i, j) of wavefront b: lane l holds outputs 2 (4 (l / 16) + v) + i of column 2 (l % 16) + j
+    f32x4 v = sums[0][wave][lane];
+#pragma unroll
+    for (int q = 1; q < 4; ++q) v += sums[q][wave][lane];
+    const int c = c0 + 2 * at + wave % 2;
+    if (c >= a.n_in) return;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int o = o0 + 2 * (4 * grp + q) + wave / 2;
+        if (o < a.n_out) a.dW[((int64_t)e * a.n_out + o) * a.n_in + c] = v[q];
+    }
+}
+
 // bf16 dy on MFMA (n_out a multiple of 8, n_in of 16, or of 8 where x is not packed): 256 x 256 outputs
 // at a time, eight
 // wavefronts of 64 x 128 on v_mfma_f32_32x32x16_bf16, K (the rows) in steps of 32 through a
@@ -688,6 +782,13 @@ bool order_pays(const pr2_wgrad_desc& d, int64_t items) {
     return d.N > 1 && d.N * items > kCus && d.R > 512;
 }
 
+// Few rows an expert and few outputs: 7 experts of 135 x 203 over 175 rows each 8.7 -> 6.2 us, one of 32 x 32 over
+// 175 9.5 -> 6.2 (over 1226 9.7 -> 15.1), 7 of 400 x 390 over 175 13.3 -> 11.6, of 1001 x 999 41 -> 50.
+bool thin_ok(const pr2_wgrad_desc& d, bool packed) {
+    return !packed && d.R > 0 && !mfma_ok(d, packed) && d.R <= 512 * (int64_t)d.N &&
+           wgrad_tile_count(d, kThin) <= 5 * kCus;
+}
+
 struct WgradWs {
     int* order;
     float* part;
@@ -709,6 +810,13 @@ WgradWs wgrad_ws(const pr2_wgrad_desc& d, void* base) {
 
 hipError_t launch_wgrad(const pr2_wgrad_desc& d, WgradArgs a, const WgradWs& w, hipStream_t st) {
     const bool packed = a.q != nullptr;
+    if (thin_ok(d, packed)) {
+        LaunchScope scope("wgrad_thin", st);
+        const dim3 grid((unsigned)ceil_div(d.n_in, kThin), (unsigned)ceil_div(d.n_out, kThin), d.N);
+        if (d.act_dtype == PR2_BF16) hipLaunchKernelGGL(wgrad_thin_kernel<bf16_t>, grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(wgrad_thin_kernel<float>, grid, dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
     a.S = d.R > 0 ? wgrad_slices(d, packed) : 1;
     a.part = w.part;
     hipError_t e;

@@ -72,4 +72,5 @@ def test_products_and_their_gradients(seed):
 
 def test_step_of_the_row_form():
     s = O.row_scale(np.array([[127.0, -3.0], [0.0, 0.0], [np.inf, 1.0], [np.nan, 1.0]]))
-    assert s[0] == 1 and s[1] == 2.0 ** -100 / 127 and np.isnan(s[2]) and np.isnan(s[3])
+    assert abs(s[0] - 1) <= 2.0 ** -23 and abs(s[1] * 127 * 2.0 ** 100 - 1) <= 2.0 ** -23
+    assert np.isnan(s[2]) and np.isnan(s[3]) and np.all(s[:2] == s[:2].astype(np.float32))
