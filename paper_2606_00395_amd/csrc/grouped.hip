@@ -45,40 +45,34 @@ __device__ __forceinline__ int source(const MmArgs& a, int r) {
     return q >= 0 && t < a.Rx ? t : -1;
 }
 
-// ------------------------------------------------ any type, width and row count --
-// 64 x 64 outputs per workgroup, four wavefronts of 32 x 32 on v_mfma_f32_32x32x2_f32 (fp32
-// products and sums), 32 K at a time staged in LDS as fp32, the next 32 in flight meanwhile.  An
-// operand whose rows run along K lies in LDS as it comes and is read four K at a time; the weights of
-// dy W, whose rows run along the columns, are read one K at a time.  A step's four K of either half
-// wavefront are the same in both operands, so that any order of them gives the sum.
+// ------------------------------------------------------------------- fp32 rows --
+// 64 x 64 outputs per workgroup, four wavefronts of 32 x 32 on v_mfma_f32_32x32x2_f32, 32 K at a time
+// staged in LDS, the next 32 in flight meanwhile.  An operand whose rows run along K is read four K at a time; the
+// weights of dy W, whose rows run along the columns, one K at a time.  A step's four K of either half
+// wavefront are the same in both operands, so that any order of them gives the sum.  (2000 x 2000 x 2000
+// in 144 us, 111 TFLOP/s; the library's product 121.)
 constexpr int kTile = 64;
 constexpr int kStep = 32;
 constexpr int kRowPitch = kStep + 4;        // 16-byte reads of 32 rows: every bank equally often
 constexpr int kColPitch = kTile + 8;        // K rows 4 apart (the two half wavefronts) 32 banks apart
 
 // 8 elements of a row from element c on, the ones past the row's n (or all, if !on) as 0
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int c, int n, bool on, u32x4 (&w)[8 / Chunk<T>::E]) {
-    constexpr int E = Chunk<T>::E;
+__device__ __forceinline__ void load8(const float* row, int c, int n, bool on, f32x4 (&w)[2]) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
     if (on && c + 8 <= n) {
-#pragma unroll
-        for (int i = 0; i < 8 / E; ++i) w[i] = load16<false>(row + c + i * E);
+        w[0] = *(const f32x4_any*)(row + c);
+        w[1] = *(const f32x4_any*)(row + c + 4);
         return;
     }
-#pragma unroll
-    for (int i = 0; i < 8 / E; ++i) w[i] = u32x4{0, 0, 0, 0};
+    w[0] = w[1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     if (!on) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (c + i >= n) continue;
-        const uint32_t b = __builtin_bit_cast(typename Chunk<T>::Bits, row[c + i]);
-        if (E == 4) w[i / 4][i % 4] = b;
-        else w[0][i / 2] |= i & 1 ? b << 16 : b;
-    }
+    for (int i = 0; i < 8; ++i)
+        if (c + i < n) w[i / 4][i % 4] = row[c + i];
 }
 
 // BACK: out = x W (W [K, C] an expert), else out = x W^T (W [C, K])
-template <typename T, bool BACK>
+template <bool BACK>
 __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
     __shared__ __attribute__((aligned(16))) float A[kTile * kRowPitch];
     __shared__ __attribute__((aligned(16))) float B[BACK ? kStep * kColPitch : kTile * kRowPitch];
@@ -90,14 +84,13 @@ __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
     if (tid < kTile) s_src[tid] = tid < t.rows && t.expert < a.N ? source(a, t.row0 + tid) : -1;
     __syncthreads();
     const int len = t.expert < a.N ? a.K : 0;
-    const T* W = (const T*)a.W + (int64_t)(len ? t.expert : 0) * a.K * a.C;
+    const float* W = (const float*)a.W + (int64_t)(len ? t.expert : 0) * a.K * a.C;
 
     const int ar = tid / 4, ak = (tid % 4) * 8;             // what this thread stages of x
     const int br = BACK ? tid / 8 : ar, bk = BACK ? (tid % 8) * 8 : ak;
     const int src = s_src[ar];
-    const T* x = (const T*)a.x + (int64_t)max(src, 0) * a.K;
-    constexpr int E = Chunk<T>::E;
-    u32x4 wa[8 / E], wb[8 / E];
+    const float* x = (const float*)a.x + (int64_t)max(src, 0) * a.K;
+    f32x4 wa[2], wb[2];
     auto fetch = [&](int k0) __attribute__((always_inline)) {
         load8(x, k0 + ak, a.K, src >= 0, wa);
         if (BACK) load8(W + (int64_t)min(k0 + br, a.K - 1) * a.C, c0 + bk, a.C, k0 + br < a.K, wb);
@@ -110,18 +103,13 @@ __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
     for (int v = 0; v < 16; ++v) acc[v] = 0.0f;
     if (len) fetch(0);
     for (int k0 = 0; k0 < len; k0 += kStep) {
-        float va[8], vb[8];
-#pragma unroll
-        for (int i = 0; i < 8 / E; ++i) {
-            Chunk<T>::open(wa[i], va + i * E);
-            Chunk<T>::open(wb[i], vb + i * E);
-        }
         __syncthreads();
-        float* const to = B + (BACK ? br * kColPitch : br * kRowPitch) + bk;
+        float* const to_a = A + ar * kRowPitch + ak;
+        float* const to_b = B + (BACK ? br * kColPitch : br * kRowPitch) + bk;
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            *(f32x4*)(A + ar * kRowPitch + ak + i) = f32x4{va[i], va[i + 1], va[i + 2], va[i + 3]};
-            *(f32x4*)(to + i) = f32x4{vb[i], vb[i + 1], vb[i + 2], vb[i + 3]};
+        for (int i = 0; i < 2; ++i) {
+            *(f32x4*)(to_a + 4 * i) = wa[i];
+            *(f32x4*)(to_b + 4 * i) = wb[i];
         }
         __syncthreads();
         if (k0 + kStep < len) fetch(k0 + kStep);
@@ -146,12 +134,12 @@ __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
     for (int v = 0; v < 16; ++v) {
         const int r = 32 * (wave >> 1) + 8 * (v / 4) + 4 * half + v % 4;
         // (a row without a source is 0 even where the weights are not finite)
-        if (r < t.rows)
-            ((T*)a.out)[(int64_t)(t.row0 + r) * a.C + c] = Act<T>::from_f32(s_src[r] >= 0 ? acc[v] : 0.0f);
+        if (r < t.rows) ((float*)a.out)[(int64_t)(t.row0 + r) * a.C + c] = s_src[r] >= 0 ? acc[v] : 0.0f;
     }
 }
 
-// The same in 8 bits: 128 K at a time as bytes, v_mfma_i32_32x32x32_i8.
+// ------------------------------------------------------- 8-bit rows of any length --
+// 64 x 64 outputs as above, 128 K at a time as bytes, v_mfma_i32_32x32x32_i8.
 constexpr int kStep8 = 128;
 constexpr int kPitch8 = kStep8 + 16;
 
@@ -1375,7 +1363,6 @@ constexpr TileCost kFewCost{kFewM, kFewP, 0.95f, 0.645f, 0.535f, false};
 constexpr TileCost kMidCost{kMidM, kMidP, 1.4f, 0.68f, 0.74f, false};
 constexpr TileCost kWideCost{BM, BP, 3.5f, 0.75f, 2.0f, true};
 constexpr TileCost kTileF32Cost{kTile, kTile, 1.5f, 0.72f, 0.55f, false};
-constexpr TileCost kTileBf16Cost{kTile, kTile, 1.5f, 1.4f, 1.1f, false};
 constexpr TileCost kTile8Cost{kTile, kTile, 1.5f, 0.7f, 0.45f, false};
 constexpr TileCost kBackThin1Cost{16, 128, 1.4f, 0.5f, 0.286f, false};
 constexpr TileCost kBackThin2Cost{32, 128, 1.0f, 0.62f, 0.477f, false};
@@ -1403,52 +1390,48 @@ float tile_time(const MmArgs& a, int element, const TileCost& t) {
 template <typename E, typename O>
 hipError_t launch_product(const MmArgs& a, hipStream_t st) {
     constexpr bool f32 = sizeof(E) == 4, i8 = sizeof(E) == 1;
+    constexpr float kNever = 3e38f;
     const bool words = a.K * (int)sizeof(E) % 4 == 0;
     const float thin = tile_time(a, sizeof(E), f32 ? kThinF32Cost : words ? kThinCost : kThinAnyCost);
-    float few = 3e38f, mid = 3e38f, wide = 3e38f, tile = 3e38f;
-    if constexpr (!f32) {
-        if (mfma_ok(a, sizeof(E))) {
-            few = tile_time(a, sizeof(E), kFewCost);
-            mid = tile_time(a, sizeof(E), kMidCost);
-            wide = tile_time(a, sizeof(E), kWideCost);
-        }
+    float few = kNever, mid = kNever, wide = kNever, tile = kNever;
+    if (!f32 && mfma_ok(a, sizeof(E))) {
+        few = tile_time(a, sizeof(E), kFewCost);
+        mid = tile_time(a, sizeof(E), kMidCost);
+        wide = tile_time(a, sizeof(E), kWideCost);
+    } else if (f32 || i8) {
+        // (bf16 rows off 16 bytes take 32 x 32 tiles: against 64 x 64 of fp32 MFMA 2000 x 2002 x 2002 in
+        // 100 us for 153, 2000 x 2001 x 2001 in 166 for 163, 8 x 4000 x 1001 x 999 in 77 for 80)
+        tile = tile_time(a, sizeof(E), f32 ? kTileF32Cost : kTile8Cost);
     }
-    if (few == 3e38f) tile = tile_time(a, sizeof(E), f32 ? kTileF32Cost : i8 ? kTile8Cost : kTileBf16Cost);
     const float least = std::min({thin, few, mid, wide, tile});
-    if (thin == least) {
-        if (words) return launch_tiles("mm_thin", mm_thin_kernel<E, O, false>, a, 32, 32, 256, st);
-        if constexpr (!f32) return launch_tiles("mm_thin", mm_thin_kernel<E, O, true>, a, 32, 32, 256, st);
-    }
-    if (tile == least) {
-        if constexpr (i8) return launch_tiles("mm_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
-        else return launch_tiles("mm_tile", mm_tile_kernel<E, false>, a, kTile, kTile, 256, st);
-    }
     if constexpr (!f32) {
         if (few == least) return launch_tiles("mm_few", mm_few_kernel<E, O>, a, kFewM, kFewP, 256, st);
         if (mid == least) return launch_tiles("mm_mid", mm_mid_kernel<E, O>, a, kMidM, kMidP, 256, st);
         if constexpr (sizeof(O) == 2)
-            if ((int64_t)a.R * a.C * 2 >= kStreamBytes)
+            if (wide == least && (int64_t)a.R * a.C * 2 >= kStreamBytes)
                 return launch_tiles("mm_wide", mm_wide_kernel<E, O, true>, a, BM, BP, kThreads, st);
-        return launch_tiles("mm_wide", mm_wide_kernel<E, O, false>, a, BM, BP, kThreads, st);
+        if (wide == least) return launch_tiles("mm_wide", mm_wide_kernel<E, O, false>, a, BM, BP, kThreads, st);
+        if (thin == least && !words) return launch_tiles("mm_thin", mm_thin_kernel<E, O, true>, a, 32, 32, 256, st);
     }
-    return hipErrorUnknown;         // (fp32 has the two above)
+    if (thin == least) return launch_tiles("mm_thin", mm_thin_kernel<E, O, false>, a, 32, 32, 256, st);
+    if constexpr (i8) return launch_tiles("mm_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
+    return launch_tiles("mm_tile", mm_tile_kernel<false>, a, kTile, kTile, 256, st);
 }
 
-template <typename T>
-hipError_t launch_back(const MmArgs& a, hipStream_t st) {
-    constexpr bool f32 = sizeof(T) == 4;
-    const bool mfma = !f32 && a.K % 8 == 0 && a.C % 8 == 0;
-    const float one = tile_time(a, sizeof(T), f32 ? kBackThin1F32Cost : kBackThin1Cost);
-    const float two = f32 ? 3e38f : tile_time(a, sizeof(T), kBackThin2Cost);
-    const float wide = tile_time(a, sizeof(T), mfma ? kBackWideCost : f32 ? kTileF32Cost : kTileBf16Cost);
-    const float least = std::min({one, two, wide});
-    if (one == least)
-        return launch_tiles("mm_back_thin", mm_back_thin_kernel<T, 1>, a, 16, 16 * Chunk<T>::E, 256, st);
-    if constexpr (!f32) {
-        if (two == least) return launch_tiles("mm_back_thin", mm_back_thin_kernel<T, 2>, a, 32, 128, 256, st);
-        if (mfma) return launch_tiles("mm_back_wide", mm_back_wide_kernel, a, BM, BP, kThreads, st);
-    }
-    return launch_tiles("mm_back_tile", mm_tile_kernel<T, true>, a, kTile, kTile, 256, st);
+hipError_t launch_back_f32(const MmArgs& a, hipStream_t st) {
+    if (tile_time(a, 4, kBackThin1F32Cost) <= tile_time(a, 4, kTileF32Cost))
+        return launch_tiles("mm_back_thin", mm_back_thin_kernel<float, 1>, a, 16, 64, 256, st);
+    return launch_tiles("mm_back_tile", mm_tile_kernel<true>, a, kTile, kTile, 256, st);
+}
+
+hipError_t launch_back_bf16(const MmArgs& a, hipStream_t st) {
+    const float one = tile_time(a, 2, kBackThin1Cost), two = tile_time(a, 2, kBackThin2Cost);
+    // (rows off 16 bytes: 2000 x 2001 x 2001 in 141 us, with 64 x 64 tiles of fp32 MFMA 178; 8 x 4000 x 1001
+    // x 999 107 for 103)
+    const float wide = a.K % 8 == 0 && a.C % 8 == 0 ? tile_time(a, 2, kBackWideCost) : 3e38f;
+    if (wide < std::min(one, two)) return launch_tiles("mm_back_wide", mm_back_wide_kernel, a, BM, BP, kThreads, st);
+    if (one <= two) return launch_tiles("mm_back_thin", mm_back_thin_kernel<bf16_t, 1>, a, 16, 128, 256, st);
+    return launch_tiles("mm_back_thin2", mm_back_thin_kernel<bf16_t, 2>, a, 32, 128, 256, st);
 }
 
 }  // namespace
@@ -1491,7 +1474,7 @@ pr2_status pr2_grouped_mm_backward(const pr2_wgrad_desc* desc, const void* dy, c
     if ((s = device_ready()) != PR2_OK) return s;
     const MmArgs a{dy, W, offsets, nullptr, dx, nullptr, nullptr, (int)d.R, (int)d.R, d.n_out, d.n_in, d.N, 1};
     const hipStream_t st = (hipStream_t)stream;
-    const hipError_t e = d.act_dtype == PR2_BF16 ? launch_back<bf16_t>(a, st) : launch_back<float>(a, st);
+    const hipError_t e = d.act_dtype == PR2_BF16 ? launch_back_bf16(a, st) : launch_back_f32(a, st);
     if (e != hipSuccess) return hip_fail(e, "grouped_mm_backward launch");
     return ok();
 }
