@@ -383,22 +383,27 @@ __device__ __forceinline__ void zero_tile(const MmArgs& a, const RowTile& t, int
 }
 
 // 256 rows x 256 columns per workgroup, eight wavefronts of 64 x 128 (two per SIMD).  K advances in
-// slices of 128 bytes a row, copied into LDS directly, two stages; the slice's only barrier sits
-// between its two sub-steps, so that the fragments of the next sub-step are always read among the
-// MFMAs of the one before.  Chunks past a row's end are copied from zeros, in both operands.  The
+// slices of 128 bytes a row, copied into LDS directly; the slice's only barrier sits between its two
+// sub-steps, so that the fragments of the next sub-step are always read among the MFMAs of the one
+// before.  Three stages of rows and two of weights: rows are copied among a slice's first sub-step and
+// weights among its second, one copy for 8 MFMAs and no branch at any (with two stages of both all
+// copies fall into the second sub-step: zeros, where power does not limit, 131072 x 1536 x 2048 in 633 us for
+// 541, random numbers 700 for 680).  Chunks past a row's end are copied from zeros, in both operands.  The
 // MFMAs take (weights, rows), so that a lane holds four consecutive columns of one row.
+// (bf16 131072 x 1536 x 2048 in 128 experts 706 us, 1169 TFLOP/s, the library's product in one 592 to 630;
+// int8 131072 x 2048 x 2048 1.8 POP/s, the library 1.83.)
 constexpr int BM = 256, BP = 256;
 constexpr int WM = 64, WN = 128;
 constexpr int MI = WM / MT, NJ = WN / MT;
 constexpr int kThreads = 512;
-constexpr int kGroups = 8;                  // copies of 8 rows per wavefront and slice
-constexpr int kStageB = (BM + BP) * kRowB;
+constexpr int kCopy = 4;                    // copies of 8 rows of either operand per wavefront and slice
+constexpr int kOperandB = 256 * kRowB;      // a stage of one operand
 
 template <typename E, typename O, bool STREAM>
 __global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 mm_wide_kernel(MmArgs a) {
     using M = Mma<E>;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * kStageB];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[5 * kOperandB];     // three of rows, two of weights
     RowTile t;
     if (!find_tile(a.offsets, a.N, a.R, BM, (a.C + BP - 1) / BP, block_number(), &t)) return;
     if (t.expert >= a.N) {
@@ -413,53 +418,42 @@ mm_wide_kernel(MmArgs a) {
     const bool active = wr * WM < t.rows && c0 + wc * WN < a.C;
     const int kb = a.K * (int)sizeof(E);
 
-    // wavefronts 0-3 copy the rows, 4-7 the weights: copy i rows wrow0 + 8 i + lane / 8
-    const int wrow0 = (wave & 3) * 64;
-    const unsigned char* base;
-    uint32_t off[kGroups];
+    // wavefront w copies rows 32 w + 8 i + lane / 8 of both operands (past their ends the last one)
+    const int wrow0 = wave * 8 * kCopy;
     const int chunk0 = (lane & 7) ^ swz(lane >> 3);         // of copies 0, 2, ..; the others ^ 1
-    if (wave < 4) {
-        base = (const unsigned char*)a.x + (a.route ? 0 : (int64_t)t.row0 * kb);
-        int src[kGroups];
+    const unsigned char* const xb = (const unsigned char*)a.x + (a.route ? 0 : (int64_t)t.row0 * kb);
+    const unsigned char* const wb = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + c0) * kb;
+    uint32_t xo[kCopy], wo[kCopy];
+    int src[kCopy];
 #pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const int r = min(wrow0 + 8 * i + lane / 8, t.rows - 1);
-            src[i] = a.route ? a.route[t.row0 + r] : r;
-        }
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const int row = a.route ? min(max(src[i], 0) / a.k, a.Rx - 1) : src[i];
-            off[i] = (uint32_t)row * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
-        }
-    } else {
-        base = (const unsigned char*)a.W + ((int64_t)t.expert * a.C + c0) * kb;
-#pragma unroll
-        for (int i = 0; i < kGroups; ++i) {
-            const int r = min(wrow0 + 8 * i + lane / 8, a.C - 1 - c0);
-            off[i] = (uint32_t)r * (uint32_t)kb + ((chunk0 ^ (i & 1)) << 4);
-        }
+    for (int i = 0; i < kCopy; ++i) {
+        const int r = min(wrow0 + 8 * i + lane / 8, t.rows - 1);
+        src[i] = a.route ? a.route[t.row0 + r] : r;
     }
-    // copies of this wavefront per slice, in twos: fewer where the rows end
-    const int rows_here = wave < 4 ? t.rows : a.C - c0;
-    const int ncopy = min(kGroups, max(0, (rows_here - wrow0 + 15) / 16) * 2);
+#pragma unroll
+    for (int i = 0; i < kCopy; ++i) {
+        const int row = a.route ? min(max(src[i], 0) / a.k, a.Rx - 1) : src[i];
+        const int ch = (chunk0 ^ (i & 1)) << 4;
+        xo[i] = (uint32_t)row * (uint32_t)kb + ch;
+        wo[i] = (uint32_t)min(wrow0 + 8 * i + lane / 8, a.C - 1 - c0) * (uint32_t)kb + ch;
+    }
     const int whole = kb / kRowB;                           // slices inside every row
     const int nk = max(2, (kb + kRowB - 1) / kRowB);
-    auto issue = [&](int kt, int q) __attribute__((always_inline)) {
-        if (ncopy <= 2 * q) return;
-        const unsigned char* from = base + kt * kRowB;
-        unsigned char* to = lds + (kt & 1) * kStageB + (wave * kGroups + 2 * q) * 1024;
-        if (kt < whole) {
-            dma16_at(from, off[2 * q], to);
-            dma16_at(from, off[2 * q + 1], to + 1024);
-        } else {
-            const int left = kb - kt * kRowB;
-            dma16(chunk0 * 16 < left ? from + off[2 * q] : kZeros, to);
-            dma16((chunk0 ^ 1) * 16 < left ? from + off[2 * q + 1] : kZeros, to + 1024);
-        }
+    const uint32_t lds0 = lds_address(lds) + wave * (kCopy * 1024);
+    using C0 = std::integral_constant<int, 0>;
+    using C1 = std::integral_constant<int, 1>;
+    // copy i of slice kt; PART: the slice may pass the rows' end
+    auto issue = [&](auto PART, const unsigned char* from, const uint32_t* off, int kt, uint32_t to, int i)
+                     __attribute__((always_inline)) {
+        from += kt * kRowB;
+        if (!decltype(PART)::value) dma16_to(from, off[i], to + i * 1024);
+        else dma16_to((chunk0 ^ (i & 1)) * 16 < kb - kt * kRowB ? from + off[i] : kZeros, to + i * 1024);
     };
-    auto issue_all = [&](int kt) __attribute__((always_inline)) {
-#pragma unroll
-        for (int q = 0; q < kGroups / 2; ++q) issue(kt, q);
+    auto issue_x = [&](auto PART, int kt, int stage, int i) __attribute__((always_inline)) {
+        issue(PART, xb, xo, kt, lds0 + stage * kOperandB, i);
+    };
+    auto issue_w = [&](auto PART, int kt, int i) __attribute__((always_inline)) {
+        issue(PART, wb, wo, kt, lds0 + (3 + (kt & 1)) * kOperandB, i);
     };
 
     typename M::Acc acc[MI][NJ];
@@ -476,23 +470,25 @@ mm_wide_kernel(MmArgs a) {
     int kpos[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
-    const int a0 = wr * WM * kRowB, b0 = (BM + wc * WN) * kRowB;
+    const int a0 = wr * WM * kRowB, b0 = (3 * BM + wc * WN) * kRowB;
     typename M::Frag fa[2][MI], fb[2][NJ];
     auto frag = [&](int at) __attribute__((always_inline)) {
         return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(lds + at));
     };
-    auto sync = [&]() __attribute__((always_inline)) {
-        wait_vmcnt<0>();
-        __syncthreads();
+    // the slice before that of the last n copies has arrived, and this wavefront's LDS reads have ended
+    auto sync = [&](auto N) __attribute__((always_inline)) {
+        wait_vmcnt<decltype(N)::value>();
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        plain_barrier();
     };
-    // MFMAs of a sub-step on fragment set S, among them the reads of the next one's and the copies
-    // of slice kt
-    auto phase = [&](auto S_, auto READ, auto ISSUE, int stage, int ks, int kt) __attribute__((always_inline)) {
+    // MFMAs of a sub-step on fragment set S, among them the reads of the next one's (sub-step ks of the rows'
+    // stage xs and the weights' ws) and copy(0 .. 3)
+    auto phase = [&](auto S_, auto READ, int xs, int ws, int ks, auto copy) __attribute__((always_inline)) {
         constexpr int S = decltype(S_)::value;
-        const int at = stage * kStageB + kpos[ks];
+        const int xa = xs * kOperandB + kpos[ks] + a0, wa = ws * kOperandB + kpos[ks] + b0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            if (decltype(ISSUE)::value) issue(kt, q);
+            copy(q);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 2 * q; j < 2 * q + 2; ++j)
@@ -503,46 +499,60 @@ mm_wide_kernel(MmArgs a) {
                 if (q < 2) {
 #pragma unroll
                     for (int h = 2 * q; h < 2 * q + 2; ++h) {
-                        fa[S ^ 1][h] = frag(at + a0 + h * MT * kRowB);
-                        fb[S ^ 1][h] = frag(at + b0 + h * MT * kRowB);
+                        fa[S ^ 1][h] = frag(xa + h * MT * kRowB);
+                        fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
                     }
                 } else {
 #pragma unroll
-                    for (int h = 4; h < NJ; ++h) fb[S ^ 1][h] = frag(at + b0 + h * MT * kRowB);
+                    for (int h = 4; h < NJ; ++h) fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
                 }
             }
         }
     };
-    using C0 = std::integral_constant<int, 0>;
-    using C1 = std::integral_constant<int, 1>;
-    issue_all(0);
-    issue_all(1);
-    if (ncopy == kGroups) wait_vmcnt<kGroups>();
-    else wait_vmcnt<0>();
+    auto no_copy = [](int) {};
+    using Behind = std::integral_constant<int, kCopy>;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int i = 0; i < kCopy; ++i) {
+            issue_x(C1{}, kt, kt, i);
+            issue_w(C1{}, kt, i);
+        }
+    wait_vmcnt<2 * kCopy>();
     plain_barrier();
-    int kt = 0;
+    int kt = 0, xs = 0;         // the slice and its rows' stage
+    auto next = [](int s) __attribute__((always_inline)) { return s == 2 ? 0 : s + 1; };
     if (active) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) fa[0][i] = frag(kpos[0] + a0 + i * MT * kRowB);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) fb[0][j] = frag(kpos[0] + b0 + j * MT * kRowB);
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        for (; kt + 2 < nk; ++kt) {
-            phase(C0{}, C1{}, C0{}, kt & 1, 1, 0);
-            sync();
-            phase(C1{}, C1{}, C1{}, (kt + 1) & 1, 0, kt + 2);
-        }
-        phase(C0{}, C1{}, C0{}, kt & 1, 1, 0);
-        sync();
-        phase(C1{}, C1{}, C0{}, (kt + 1) & 1, 0, 0);
-        phase(C0{}, C1{}, C0{}, (kt + 1) & 1, 1, 0);
-        phase(C1{}, C0{}, C0{}, 0, 0, 0);
+        // slice kt with the copies of slice kt + 2
+        auto slice = [&](auto PART) __attribute__((always_inline)) {
+            const int x1 = next(xs), x2 = next(x1);
+            phase(C0{}, C1{}, xs, kt & 1, 1, [&](int q) __attribute__((always_inline)) { issue_x(PART, kt + 2, x2, q); });
+            sync(Behind{});
+            phase(C1{}, C1{}, x1, (kt + 1) & 1, 0, [&](int q) __attribute__((always_inline)) { issue_w(PART, kt + 2, q); });
+            xs = x1;
+        };
+        for (; kt + 2 < whole; ++kt) slice(C0{});
+        for (; kt + 2 < nk; ++kt) slice(C1{});
+        phase(C0{}, C1{}, xs, kt & 1, 1, no_copy);
+        sync(C0{});
+        xs = next(xs);
+        phase(C1{}, C1{}, xs, (kt + 1) & 1, 0, no_copy);
+        phase(C0{}, C1{}, xs, (kt + 1) & 1, 1, no_copy);
+        phase(C1{}, C0{}, 0, 0, 0, no_copy);
     } else {
         for (; kt + 2 < nk; ++kt) {
-            sync();
-            issue_all(kt + 2);
+#pragma unroll
+            for (int i = 0; i < kCopy; ++i) issue_x(C1{}, kt + 2, next(next(xs)), i);
+            sync(Behind{});
+#pragma unroll
+            for (int i = 0; i < kCopy; ++i) issue_w(C1{}, kt + 2, i);
+            xs = next(xs);
         }
-        sync();
+        sync(C0{});
     }
 
     // a lane's rows: 16 i + lane % 16 of the wavefront's block
@@ -1126,23 +1136,23 @@ mm_back_wide_kernel(MmArgs a) {
     }
     const int whole = a.K / kBK;
     const int nh = max(kBStages, (a.K + kBK - 1) / kBK);
-    auto issue = [&](int h) __attribute__((always_inline)) {
-        unsigned char* dst = lds + (h % kBStages) * kBStageB + half * kOpB + wq * 4096;
-        if (half == 0) {
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                if (h < whole) dma16_at(xb + h * kBK, off[i], dst + i * 1024);
-                else dma16(h * kBK + xk < a.K ? (const unsigned char*)(xb + h * kBK) + off[i] : kZeros, dst + i * 1024);
-            }
+    const uint32_t lds0 = lds_address(lds) + half * kOpB + wq * 4096;
+    const bf16_t* const from0 = half == 0 ? xb : wb + (int64_t)(8 * wq) * a.C;
+    const int64_t of_step = half == 0 ? kBK : (int64_t)kBK * a.C, of_copy = half == 0 ? 0 : 2 * (int64_t)a.C;
+    // copy i of step h; PART: the step may pass the last K
+    auto issue = [&](auto PART, int h, int i) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + (h % kBStages) * kBStageB + i * 1024;
+        const bf16_t* const from = from0 + h * of_step + i * of_copy;
+        if (!decltype(PART)::value) {
+            dma16_to(from, off[i], to);
         } else {
-            const bf16_t* p = wb + (int64_t)(h * kBK + 8 * wq) * a.C;
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const bf16_t* q = p + (int64_t)(2 * i) * a.C;
-                if (h < whole) dma16_at(q, off[i], dst + i * 1024);
-                else dma16(h * kBK + 8 * wq + 2 * i + hi < a.K ? (const unsigned char*)q + off[i] : kZeros, dst + i * 1024);
-            }
+            const int k = h * kBK + (half == 0 ? xk : 8 * wq + 2 * i + hi);
+            dma16_to(k < a.K ? (const unsigned char*)from + off[i] : kZeros, to);
         }
+    };
+    auto issue_all = [&](auto PART, int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) issue(PART, h, i);
     };
 
     f32x16 acc[BI][BJ];
@@ -1185,12 +1195,13 @@ mm_back_wide_kernel(MmArgs a) {
     auto row_frag = [&](const unsigned char* p) __attribute__((always_inline)) {
         return __builtin_bit_cast(bf16x8, *(const u32x4*)p);
     };
-    // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the other set
-    auto phase = [&](auto S_, int stage, int ks) __attribute__((always_inline)) {
+    // MFMAs on fragment set S, among them the reads of sub-step ks of a stage into the other set and copy(0 .. 3)
+    auto phase = [&](auto S_, int stage, int ks, auto copy) __attribute__((always_inline)) {
         constexpr int S = decltype(S_)::value;
         const unsigned char* st = lds + stage * kBStageB;
 #pragma unroll
         for (int j = 0; j < BJ; ++j) {
+            copy(j);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < BI; ++i)
@@ -1210,27 +1221,37 @@ mm_back_wide_kernel(MmArgs a) {
     using C0 = std::integral_constant<int, 0>;
     using C1 = std::integral_constant<int, 1>;
 #pragma unroll
-    for (int h = 0; h < kBStages; ++h) issue(h);
+    for (int h = 0; h < kBStages; ++h) issue_all(C1{}, h);
     wait_vmcnt<3 * kCopies>();
     barrier();
+    int h = 0;
     if (active) {
 #pragma unroll
         for (int i = 0; i < BI; ++i) fa[0][i] = row_frag(lds + a_pos[i] + kpos[0]);
 #pragma unroll
         for (int j = 0; j < BJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
-        for (int h = 0; h < nh; ++h) {
-            phase(C0{}, h % kBStages, 1);
-            wait_steps(min(nh - 1, h + kBStages - 1) - (h + 1));
+        auto no_copy = [](int) {};
+        // step h with the copies of step h + kBStages
+        auto step = [&](auto PART) __attribute__((always_inline)) {
+            phase(C0{}, h % kBStages, 1, no_copy);
+            wait_vmcnt<2 * kCopies>();
             barrier();
-            if (h + kBStages < nh) issue(h + kBStages);
+            phase(C1{}, (h + 1) % kBStages, 0, [&](int j) __attribute__((always_inline)) { issue(PART, h + kBStages, j); });
+        };
+        for (; h + kBStages < whole; ++h) step(C0{});
+        for (; h + kBStages < nh; ++h) step(C1{});
+        for (; h < nh; ++h) {
+            phase(C0{}, h % kBStages, 1, no_copy);
+            wait_steps(nh - 2 - h);
+            barrier();
             // (past the last step the reads fetch an old stage; unused)
-            phase(C1{}, (h + 1) % kBStages, 0);
+            phase(C1{}, (h + 1) % kBStages, 0, no_copy);
         }
     } else {
-        for (int h = 0; h < nh; ++h) {
+        for (; h < nh; ++h) {
             wait_steps(min(nh - 1, h + kBStages - 1) - (h + 1));
             barrier();
-            if (h + kBStages < nh) issue(h + kBStages);
+            if (h + kBStages < nh) issue_all(C1{}, h + kBStages);
         }
     }
     // Lane l holds row l % 32 of each 32-row block, columns 8 (v / 4) + 4 (l / 32) + v % 4 of each
