@@ -667,21 +667,28 @@ mm_few_kernel(MmArgs a) {
     }
     const int whole = kb / kRowB;
     const int nk = max(2, (kb + kRowB - 1) / kRowB);
-    auto copy = [&](const unsigned char* from, uint32_t off, int chunk, int left, unsigned char* to)
-        __attribute__((always_inline)) {
-        if (left >= kRowB) dma16_at(from, off, to);
-        else dma16(chunk * 16 < left ? from + off : kZeros, to);
-    };
+    const uint32_t lds0 = lds_address(lds), lds_w = lds0 + (kFewM + 32 * wave) * kRowB, lds_x = lds0 + 16 * wave * kRowB;
     const int turn = (5 * t.panel + 3 * t.expert) % nk;
     auto issue = [&](int step) __attribute__((always_inline)) {
         const int kt = step + turn < nk ? step + turn : step + turn - nk;
-        unsigned char* st = lds + (step % kFewStages) * kFewStageB;
-        const int left = kt < whole ? kRowB : kb - kt * kRowB;
+        const uint32_t st = (step % kFewStages) * kFewStageB;
+        const unsigned char* const w = wb + kt * kRowB;
+        const unsigned char* const x = xb + kt * kRowB;
+        if (kt < whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            copy(wb + kt * kRowB, woff[i], chunk0 ^ (i & 1), left, st + (kFewM + 32 * wave + 8 * i) * kRowB);
-        if (nx > 0) copy(xb + kt * kRowB, xoff[0], chunk0, left, st + 16 * wave * kRowB);
-        if (nx > 1) copy(xb + kt * kRowB, xoff[1], chunk0 ^ 1, left, st + (16 * wave + 8) * kRowB);
+            for (int i = 0; i < 4; ++i) dma16_to(w, woff[i], lds_w + st + i * 1024);
+            if (nx > 0) dma16_to(x, xoff[0], lds_x + st);
+            if (nx > 1) dma16_to(x, xoff[1], lds_x + st + 1024);
+        } else {
+            const int left = kb - kt * kRowB;
+            auto part = [&](const unsigned char* p, int i) __attribute__((always_inline)) {
+                return (chunk0 ^ (i & 1)) * 16 < left ? p : kZeros;
+            };
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dma16_to(part(w + woff[i], i), lds_w + st + i * 1024);
+            if (nx > 0) dma16_to(part(x + xoff[0], 0), lds_x + st);
+            if (nx > 1) dma16_to(part(x + xoff[1], 1), lds_x + st + 1024);
+        }
     };
     // a slice has landed, the one after it may still be in flight
     auto wait_one = [&]() __attribute__((always_inline)) {
@@ -782,22 +789,28 @@ mm_mid_kernel(MmArgs a) {
     }
     const int whole = kb / kRowB;
     const int nk = max(2, (kb + kRowB - 1) / kRowB);
-    auto copy = [&](const unsigned char* from, uint32_t off, int chunk, int left, unsigned char* to)
-        __attribute__((always_inline)) {
-        if (left >= kRowB) dma16_at(from, off, to);
-        else dma16(chunk * 16 < left ? from + off : kZeros, to);
-    };
+    const uint32_t lds0 = lds_address(lds) + 32 * wave * kRowB;
     const int turn = (5 * t.panel + 3 * t.expert) % nk;
     auto issue = [&](int step) __attribute__((always_inline)) {
         const int kt = step + turn < nk ? step + turn : step + turn - nk;
-        unsigned char* st = lds + (step % kMidStages) * kMidStageB;
-        const int left = kt < whole ? kRowB : kb - kt * kRowB;
+        const uint32_t st = lds0 + (step % kMidStages) * kMidStageB;
+        const unsigned char* const w = wb + kt * kRowB;
+        const unsigned char* const x = xb + kt * kRowB;
+        if (kt < whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            copy(wb + kt * kRowB, woff[i], chunk0 ^ (i & 1), left, st + (kMidM + 32 * wave + 8 * i) * kRowB);
+            for (int i = 0; i < 4; ++i) dma16_to(w, woff[i], st + kMidM * kRowB + i * 1024);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < nx) copy(xb + kt * kRowB, xoff[i], chunk0 ^ (i & 1), left, st + (32 * wave + 8 * i) * kRowB);
+            for (int i = 0; i < 4; ++i)
+                if (i < nx) dma16_to(x, xoff[i], st + i * 1024);
+        } else {
+            const int left = kb - kt * kRowB;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool on = (chunk0 ^ (i & 1)) * 16 < left;
+                dma16_to(on ? w + woff[i] : kZeros, st + kMidM * kRowB + i * 1024);
+                if (i < nx) dma16_to(on ? x + xoff[i] : kZeros, st + i * 1024);
+            }
+        }
     };
     const int lrow = lane & 15, grp = lane >> 4;
     const int cperm = ((grp & 1) << 1) | (grp >> 1);

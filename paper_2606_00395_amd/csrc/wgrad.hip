@@ -443,22 +443,20 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         whole = __builtin_amdgcn_readfirstlane(any) ? 0 : clen / kBK;
     };
     auto stage_of = [&](int h) __attribute__((always_inline)) { return lds + (h % kStages) * kStageB; };
-    // rows of x: the same places of the other operand, each half wavefront's row by its index
-    auto copy_x = [&](int ct, int h, int i) __attribute__((always_inline)) {
-        unsigned char* dst = stage_of(h) + kOpB + krow * kPitch + i * 1024;
-        const uint32_t row = src[h * kBK + krow + 2 * i + hi];
-        const int c = ct * BN + 8 * ((lane & 31) ^ (4 * (hi + 2 * (i & 1))));
-        const bf16_t* p = (const bf16_t*)a.x + (uint64_t)row * (uint32_t)a.n_in + (c < a.n_in ? c : 0);
-        dma16(row != kNoRow ? p : kZeros, dst);
-    };
-    auto copy_dy = [&](int h, int i) __attribute__((always_inline)) {
-        unsigned char* dst = stage_of(h) + krow * kPitch + i * 1024;
-        const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
-        if (h < whole) {
-            dma16_at(p, doff[i & 1], dst);
+    // Copy i of a step, dy's or rows of x to the same places of the other operand, each half wavefront's row
+    // by its index.  WHOLE: every row of the step has a source.
+    const uint32_t lds0 = lds_address(lds) + (LOADS == LOAD_X ? kOpB : 0) + krow * kPitch;
+    auto row_of = [&](int h, int i) __attribute__((always_inline)) { return src[h * kBK + krow + 2 * i + hi]; };
+    auto copy_row = [&](auto WHOLE, int ct, int h, int i, uint32_t row) __attribute__((always_inline)) {
+        const uint32_t to = lds0 + (h % kStages) * kStageB + i * 1024;
+        if (LOADS == LOAD_X) {
+            const int c = ct * BN + 8 * ((lane & 31) ^ (4 * (hi + 2 * (i & 1))));
+            const bf16_t* p = (const bf16_t*)a.x + (uint64_t)row * (uint32_t)a.n_in + (c < a.n_in ? c : 0);
+            dma16_to(decltype(WHOLE)::value || row != kNoRow ? p : (const bf16_t*)kZeros, to);
         } else {
-            const bool ok = src[h * kBK + krow + 2 * i + hi] != kNoRow;
-            dma16(ok ? (const unsigned char*)p + doff[i & 1] : (const unsigned char*)kZeros, dst);
+            const bf16_t* p = dy + (int64_t)(kc + h * kBK + 2 * i) * a.n_out;
+            if (decltype(WHOLE)::value) dma16_to(p, doff[i & 1], to);
+            else dma16_to(row != kNoRow ? (const unsigned char*)p + doff[i & 1] : (const unsigned char*)kZeros, to);
         }
     };
     // Packed pieces in flight: two steps' worth.  Nothing is computed from them on arrival
@@ -507,10 +505,7 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
         } else {
             for (int h = 0; h < min(nh, kStages); ++h) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) {
-                    if (LOADS == LOAD_X) copy_x(ct, h, i);
-                    else copy_dy(h, i);
-                }
+                for (int i = 0; i < kCopies; ++i) copy_row(C0{}, ct, h, i, row_of(h, i));
             }
         }
     };
@@ -586,6 +581,11 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
             // into a stage whose last reader was a step earlier at least, and h + 4 is fetched.
             // (Past the last step the reads fetch an old stage; unused.)
             auto step = [&](auto S_, int h) __attribute__((always_inline)) {
+                uint32_t rows[kCopies];
+                if (!PACKS && h + kStages < nh) {
+#pragma unroll
+                    for (int i = 0; i < kCopies; ++i) rows[i] = row_of(h + kStages, i);
+                }
                 if (active) phase(C0{}, h % kStages, 1, [](int) __attribute__((always_inline)) {});
                 if (!PACKS) wait_steps(min(nh - 1, h + kStages - 1) - (h + 1));
                 barrier();
@@ -594,8 +594,7 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
                         write_packed(S_, h + 2, j);     // (past the end into a stage nobody reads)
                         if (j == 3) load_packed(S_, ct, h + 4);
                     } else if (h + kStages < nh) {
-                        if (LOADS == LOAD_X) copy_x(ct, h + kStages, j);
-                        else copy_dy(h + kStages, j);
+                        copy_row(C0{}, ct, h + kStages, j, rows[j]);
                     }
                 };
                 if (active) {
@@ -612,11 +611,30 @@ __device__ __forceinline__ void wgrad_tiles(const WgradArgs& a, unsigned char* l
                 for (int j = 0; j < NJ; ++j) fb[0][j] = tr_frag(lds + b_pos[j]);
             }
             int h = 0;
-            for (; h + 1 < nh; h += 2) {
-                step(C0{}, h);
-                step(C1{}, h + 1);
+            if (!PACKS) {
+                // Steps whose copies are of whole steps: no test per copy, and the rows' indexes are read a sub-step
+                // ahead (rows of x, 128 experts of 1024 rows, 2048 x 768: 543 -> 480 us, 1536 x 2048: 1007 -> 907).
+                if (active) {
+                    for (; h + kStages < whole; ++h) {
+                        uint32_t rows[kCopies];
+#pragma unroll
+                        for (int i = 0; i < kCopies; ++i) rows[i] = LOADS == LOAD_X ? row_of(h + kStages, i) : 0u;
+                        phase(C0{}, h % kStages, 1, [](int) __attribute__((always_inline)) {});
+                        wait_vmcnt<2 * kCopies>();
+                        barrier();
+                        phase(C1{}, (h + 1) % kStages, 0, [&](int j) __attribute__((always_inline)) {
+                            copy_row(C1{}, ct, h + kStages, j, rows[j]);
+                        });
+                    }
+                }
+                for (; h < nh; ++h) step(C0{}, h);
+            } else {
+                for (; h + 1 < nh; h += 2) {
+                    step(C0{}, h);
+                    step(C1{}, h + 1);
+                }
+                if (h < nh) step(C0{}, h);
             }
-            if (h < nh) step(C0{}, h);
         }
         barrier();          // (no wavefront reads a stage any more: all hold the last step's fragments)
         if (ct + 1 < ct1 && klen > 0 && klen <= kRowsHeld) fetch(ct + 1);
