@@ -18,6 +18,8 @@ namespace {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef u32x4 u32x4_byte __attribute__((aligned(1)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
 
 struct MmArgs {
     const void* x;              // [Rx, K] rows read (dy, q)
@@ -138,10 +140,9 @@ __global__ void __launch_bounds__(256) mm_tile_kernel(MmArgs a) {
     }
 }
 
-// ------------------------------------------------------- 8-bit rows of any length --
-// 64 x 64 outputs as above, 128 K at a time as bytes, v_mfma_i32_32x32x32_i8.
-constexpr int kStep8 = 128;
-constexpr int kPitch8 = kStep8 + 16;
+// ------------------------------------------------- bf16 and 8-bit rows of any length --
+constexpr int kStepB = 128;
+constexpr int kPitchB = kStepB + 16;
 
 // 16 bytes from any address, by loads of whole words, put together where they are used: a load that is
 // not 4-byte aligned takes several times as long (517 x 1001 outputs of 999 int8 in 32 x 32 tiles: 13.5 us,
@@ -163,116 +164,6 @@ template <bool ANY> struct Piece {
                      __builtin_amdgcn_alignbyte(w[3], w[2], drop), drop ? __builtin_amdgcn_alignbyte(next, w[3], drop) : w[3]};
     }
 };
-
-// 16 bytes of a row from byte c on, those past the row's n as 0
-__device__ __forceinline__ u32x4 load16_bytes(const unsigned char* row, int c, int n) {
-    if (c + 16 <= n) return *(const u32x4_byte*)(row + c);
-    u32x4 w = {0, 0, 0, 0};
-    if (c >= n) return w;
-    if (n >= 16) {
-        // the row's last 16 bytes, moved down
-        const u32x4 v = *(const u32x4_byte*)(row + n - 16);
-        const int drop = c + 16 - n;            // 1 .. 15
-        uint64_t lo = (uint64_t)v[0] | (uint64_t)v[1] << 32, hi = (uint64_t)v[2] | (uint64_t)v[3] << 32;
-        if (drop >= 8) {
-            lo = hi;
-            hi = 0;
-        }
-        const int bits = 8 * (drop & 7);
-        if (bits) {
-            lo = lo >> bits | hi << (64 - bits);
-            hi >>= bits;
-        }
-        return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-        if (c + i < n) w[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i % 4));
-    return w;
-}
-
-template <typename O>
-__global__ void __launch_bounds__(256) mm8_tile_kernel(MmArgs a) {
-    __shared__ __attribute__((aligned(16))) unsigned char A[kTile * kPitch8], B[kTile * kPitch8];
-    __shared__ int s_src[kTile];
-    RowTile t;
-    if (!find_tile(a.offsets, a.N, a.R, kTile, (a.C + kTile - 1) / kTile, block_number(), &t)) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int c0 = t.panel * kTile;
-    if (tid < kTile) s_src[tid] = tid < t.rows && t.expert < a.N ? source(a, t.row0 + tid) : -1;
-    __syncthreads();
-    const bool real = t.expert < a.N;
-    const int len = real ? a.K : 0;
-    const int expert = real ? t.expert : 0;
-    const int8_t* W = (const int8_t*)a.W + (int64_t)expert * a.K * a.C;
-    struct Set {
-        u32x4 a[2], b[2];
-    };
-    const unsigned char *xr[2], *wr[2];             // rows tid / 8 and + 32
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = tid / 8 + 32 * i;
-        xr[i] = (const unsigned char*)a.x + (int64_t)max(s_src[r], 0) * a.K;
-        wr[i] = (const unsigned char*)W + (int64_t)min(c0 + r, a.C - 1) * a.K;
-    }
-    auto fetch = [&](Set& s, int k0) __attribute__((always_inline)) {
-        const int c = k0 + (tid % 8) * 16;
-        if (k0 + kStep8 <= a.K) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                s.a[i] = *(const u32x4_byte*)(xr[i] + c);
-                s.b[i] = *(const u32x4_byte*)(wr[i] + c);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                s.a[i] = load16_bytes(xr[i], c, a.K);
-                s.b[i] = load16_bytes(wr[i], c, a.K);
-            }
-        }
-    };
-    const int half = lane >> 5, l32 = lane & 31;
-    const int ao = 32 * (wave >> 1) + l32, bo = 32 * (wave & 1) + l32;
-    i32x16 acc;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) acc[v] = 0;
-    // two steps in flight behind the one that is multiplied
-    auto step = [&](Set& s, int k0) __attribute__((always_inline)) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int at = (tid / 8 + 32 * i) * kPitch8 + (tid % 8) * 16;
-            *(u32x4*)(A + at) = s.a[i];
-            *(u32x4*)(B + at) = s.b[i];
-        }
-        __syncthreads();
-        if (k0 + 2 * kStep8 < len) fetch(s, k0 + 2 * kStep8);
-#pragma unroll
-        for (int k = 0; k < kStep8; k += 32) {
-            const i32x4 fa = *(const i32x4*)(A + ao * kPitch8 + k + 16 * half);
-            const i32x4 fb = *(const i32x4*)(B + bo * kPitch8 + k + 16 * half);
-            acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa, fb, acc, 0, 0, 0);
-        }
-    };
-    Set s0, s1;
-    if (len) fetch(s0, 0);
-    if (kStep8 < len) fetch(s1, kStep8);
-    for (int k0 = 0; k0 < len; k0 += 2 * kStep8) {
-        step(s0, k0);
-        if (k0 + kStep8 < len) step(s1, k0 + kStep8);
-    }
-    const int c = c0 + bo;
-    if (c >= a.C) return;
-    const float sw = a.w_scale[(int64_t)expert * a.C + c];
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        const int r = 32 * (wave >> 1) + 8 * (v / 4) + 4 * half + v % 4;
-        if (r >= t.rows) continue;
-        const int src = s_src[r];
-        const float y = src >= 0 ? (float)acc[v] * a.row_scale[src] * sw : 0.0f;
-        ((O*)a.out)[(int64_t)(t.row0 + r) * a.C + c] = Act<O>::from_f32(y);
-    }
-}
 
 // --------------------------------------------------------- matrix instructions --
 // bf16 rows of a multiple of 16 bytes on v_mfma_f32_16x16x32_bf16, 8-bit ones on
@@ -307,6 +198,153 @@ template <> struct Mma<float> {
         return __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
     }
 };
+
+// 16 bytes of a row from byte c on, those past the row's n as 0
+__device__ __forceinline__ u32x4 load16_bytes(const unsigned char* row, int c, int n) {
+    if (c + 16 <= n) return *(const u32x4_byte*)(row + c);
+    u32x4 w = {0, 0, 0, 0};
+    if (c >= n) return w;
+    if (n >= 16) {
+        // the row's last 16 bytes, moved down
+        const u32x4 v = *(const u32x4_byte*)(row + n - 16);
+        const int drop = c + 16 - n;            // 1 .. 15
+        uint64_t lo = (uint64_t)v[0] | (uint64_t)v[1] << 32, hi = (uint64_t)v[2] | (uint64_t)v[3] << 32;
+        if (drop >= 8) {
+            lo = hi;
+            hi = 0;
+        }
+        const int bits = 8 * (drop & 7);
+        if (bits) {
+            lo = lo >> bits | hi << (64 - bits);
+            hi >>= bits;
+        }
+        return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (c + i < n) w[i / 4] |= (uint32_t)(uint8_t)row[c + i] << (8 * (i % 4));
+    return w;
+}
+
+// the same two types on blocks of 32 x 32
+template <typename E> struct Wide;
+template <> struct Wide<bf16_t> {
+    using Acc = f32x16;
+    __device__ __forceinline__ static Acc mul(const u32x4& a, const u32x4& b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Wide<int8_t> {
+    using Acc = i32x16;
+    __device__ __forceinline__ static Acc mul(const u32x4& a, const u32x4& b, Acc c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+
+// Rows off 16 bytes: 64 x 64 outputs, 128 bytes of K at a time through registers (unaligned 16-byte
+// loads) into LDS, two steps in flight.  BACK: out = x W, bf16, the weights' 64 K rows of 64 columns read as
+// fragments by the transposing LDS read.  (bf16, 128 experts of 1024 rows, 1535 x 2047 2.45 ms, 2000 x 2001
+// x 2001 55 us; in 32 x 32 tiles 7.77 ms and 162 us.  The row gradients of one row of
+// 1001 20 us, of 128 x 1024 rows 2.65 ms; in tiles of 16 to 32 rows straight from memory 24 us and 9.3 ms.)
+template <typename E, typename O, bool BACK>
+__global__ void __launch_bounds__(256) mm_any_kernel(MmArgs a) {
+    __shared__ __attribute__((aligned(16))) unsigned char A[kTile * kPitchB], B[kTile * kPitchB];
+    __shared__ int s_src[kTile];
+    RowTile t;
+    if (!find_tile(a.offsets, a.N, a.R, kTile, (a.C + kTile - 1) / kTile, block_number(), &t)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int c0 = t.panel * kTile;
+    if (tid < kTile) s_src[tid] = tid < t.rows && t.expert < a.N ? source(a, t.row0 + tid) : -1;
+    __syncthreads();
+    const bool real = t.expert < a.N;
+    const int kb = a.K * (int)sizeof(E), len = real ? kb : 0;
+    const int expert = real ? t.expert : 0;
+    const unsigned char* W = (const unsigned char*)a.W + (int64_t)expert * a.C * kb;
+    struct Set {
+        u32x4 a[2], b[2];
+    };
+    const int wb = BACK ? a.C * (int)sizeof(E) : kb;        // bytes of a row of the weights
+    const unsigned char *xr[2], *wr[2];             // rows tid / 8 and + 32 (BACK: of the step's weights)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = tid / 8 + 32 * i;
+        xr[i] = (const unsigned char*)a.x + (int64_t)max(s_src[r], 0) * kb;
+        wr[i] = BACK ? W + (int64_t)r * wb : W + (int64_t)min(c0 + r, a.C - 1) * wb;
+    }
+    auto fetch = [&](Set& s, int k0) __attribute__((always_inline)) {
+        const int c = k0 + (tid % 8) * 16;
+        if (BACK) {
+            const int first = k0 / (int)sizeof(E), col = c0 * (int)sizeof(E) + (tid % 8) * 16;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s.a[i] = load16_bytes(xr[i], c, kb);
+                s.b[i] = load16_bytes(wr[i] + (int64_t)first * wb, first + tid / 8 + 32 * i < a.K ? col : wb, wb);
+            }
+        } else if (k0 + kStepB <= kb) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s.a[i] = *(const u32x4_byte*)(xr[i] + c);
+                s.b[i] = *(const u32x4_byte*)(wr[i] + c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                s.a[i] = load16_bytes(xr[i], c, kb);
+                s.b[i] = load16_bytes(wr[i], c, kb);
+            }
+        }
+    };
+    const int half = lane >> 5, l32 = lane & 31;
+    const int ao = 32 * (wave >> 1) + l32, bo = 32 * (wave & 1) + l32;
+    typename Wide<E>::Acc acc;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[v] = 0;
+    // (BACK) 8 K values of column bo from K row k + 8 half on, four of them a read
+    const int s16 = lane & 15, nl = 16 * ((lane >> 4) & 1) + 4 * (s16 & 3), kl = 8 * half + (s16 >> 2);
+    auto columns = [&](int k) __attribute__((always_inline)) {
+        const unsigned char* p = B + (k + kl) * kPitchB + (32 * (wave & 1) + nl) * 2;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * kPitchB));
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // two steps in flight behind the one that is multiplied
+    auto step = [&](Set& s, int k0) __attribute__((always_inline)) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = (tid / 8 + 32 * i) * kPitchB + (tid % 8) * 16;
+            *(u32x4*)(A + at) = s.a[i];
+            *(u32x4*)(B + at) = s.b[i];
+        }
+        __syncthreads();
+        if (k0 + 2 * kStepB < len) fetch(s, k0 + 2 * kStepB);
+#pragma unroll
+        for (int k = 0; k < kStepB; k += 32) {
+            const u32x4 fa = *(const u32x4*)(A + ao * kPitchB + k + 16 * half);
+            const u32x4 fb = BACK ? columns(k / 2) : *(const u32x4*)(B + bo * kPitchB + k + 16 * half);
+            acc = Wide<E>::mul(fa, fb, acc);
+        }
+    };
+    Set s0, s1;
+    if (len) fetch(s0, 0);
+    if (kStepB < len) fetch(s1, kStepB);
+    for (int k0 = 0; k0 < len; k0 += 2 * kStepB) {
+        step(s0, k0);
+        if (k0 + kStepB < len) step(s1, k0 + kStepB);
+    }
+    const int c = c0 + bo;
+    if (c >= a.C) return;
+    const float sw = sizeof(E) == 1 ? a.w_scale[(int64_t)expert * a.C + c] : 1.0f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int r = 32 * (wave >> 1) + 8 * (v / 4) + 4 * half + v % 4;
+        if (r >= t.rows) continue;
+        const int src = s_src[r];
+        float y = 0.0f;         // (without a source, also where the weights are not finite)
+        if (src >= 0) y = sizeof(E) == 1 ? (float)acc[v] * a.row_scale[src] * sw : (float)acc[v];
+        ((O*)a.out)[(int64_t)(t.row0 + r) * a.C + c] = Act<O>::from_f32(y);
+    }
+}
 
 constexpr int kRowB = 128;                  // bytes of a row per K slice
 constexpr int MT = 16;
@@ -1104,8 +1142,6 @@ constexpr int kBStages = 4, kCopies = 4;
 constexpr int kOpB = kBK * 512;
 constexpr int kBStageB = 2 * kOpB;
 constexpr int BI = WM / 32, BJ = WN / 32;
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4s lds_v4s;
 
 // chunk c of a 64-byte LDS row r lies at c ^ rswz(r)
 __device__ __forceinline__ int rswz(int r) { return (r >> 2) & 3; }
@@ -1383,8 +1419,8 @@ bool mfma_ok(const MmArgs& a, int64_t element) {
 // at each of the 190 sizes (378 for both types): alone on its CU a tile takes start + chain a slice of 128
 // bytes of K, and where all CUs are busy a CU takes 1 + busy a slice for each of its tiles (wide
 // tiles, one on a CU, in whole rounds).
-// By this rule the products take 1.5 % more than by the best kernel at each size, 20 % at most; with the
-// 256-row tile alone 2.4 times as long at the sizes of one expert.
+// By this rule the products take 0.9 % more than by the best kernel at each of 147 sizes, 35 % (7.1 us for
+// 5.2) at most; with the 256-row tile alone 2.4 times as long at the sizes of one expert.
 struct TileCost {
     int rows, columns;
     float start, chain, busy;
@@ -1397,7 +1433,7 @@ constexpr TileCost kFewCost{kFewM, kFewP, 0.95f, 0.645f, 0.535f, false};
 constexpr TileCost kMidCost{kMidM, kMidP, 1.4f, 0.68f, 0.74f, false};
 constexpr TileCost kWideCost{BM, BP, 3.5f, 0.75f, 2.0f, true};
 constexpr TileCost kTileF32Cost{kTile, kTile, 1.5f, 0.72f, 0.55f, false};
-constexpr TileCost kTile8Cost{kTile, kTile, 1.5f, 0.7f, 0.45f, false};
+constexpr TileCost kTileAnyCost{kTile, kTile, 1.5f, 0.7f, 0.45f, false};
 constexpr TileCost kBackThin1Cost{16, 128, 1.4f, 0.5f, 0.286f, false};
 constexpr TileCost kBackThin2Cost{32, 128, 1.0f, 0.62f, 0.477f, false};
 constexpr TileCost kBackThin1F32Cost{16, 64, 1.4f, 0.25f, 0.2f, false};
@@ -1432,10 +1468,8 @@ hipError_t launch_product(const MmArgs& a, hipStream_t st) {
         few = tile_time(a, sizeof(E), kFewCost);
         mid = tile_time(a, sizeof(E), kMidCost);
         wide = tile_time(a, sizeof(E), kWideCost);
-    } else if (f32 || i8) {
-        // (bf16 rows off 16 bytes take 32 x 32 tiles: against 64 x 64 of fp32 MFMA 2000 x 2002 x 2002 in
-        // 100 us for 153, 2000 x 2001 x 2001 in 166 for 163, 8 x 4000 x 1001 x 999 in 77 for 80)
-        tile = tile_time(a, sizeof(E), f32 ? kTileF32Cost : kTile8Cost);
+    } else {
+        tile = tile_time(a, sizeof(E), f32 ? kTileF32Cost : kTileAnyCost);
     }
     const float least = std::min({thin, few, mid, wide, tile});
     if constexpr (!f32) {
@@ -1448,8 +1482,8 @@ hipError_t launch_product(const MmArgs& a, hipStream_t st) {
         if (thin == least && !words) return launch_tiles("mm_thin", mm_thin_kernel<E, O, true>, a, 32, 32, 256, st);
     }
     if (thin == least) return launch_tiles("mm_thin", mm_thin_kernel<E, O, false>, a, 32, 32, 256, st);
-    if constexpr (i8) return launch_tiles("mm_tile", mm8_tile_kernel<O>, a, kTile, kTile, 256, st);
-    return launch_tiles("mm_tile", mm_tile_kernel<false>, a, kTile, kTile, 256, st);
+    if constexpr (f32) return launch_tiles("mm_tile", mm_tile_kernel<false>, a, kTile, kTile, 256, st);
+    else return launch_tiles("mm_tile", mm_any_kernel<E, O, false>, a, kTile, kTile, 256, st);
 }
 
 hipError_t launch_back_f32(const MmArgs& a, hipStream_t st) {
@@ -1459,11 +1493,11 @@ hipError_t launch_back_f32(const MmArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_back_bf16(const MmArgs& a, hipStream_t st) {
+    if (a.K % 8 || a.C % 8)
+        return launch_tiles("mm_back_tile", mm_any_kernel<bf16_t, bf16_t, true>, a, kTile, kTile, 256, st);
     const float one = tile_time(a, 2, kBackThin1Cost), two = tile_time(a, 2, kBackThin2Cost);
-    // (rows off 16 bytes: 2000 x 2001 x 2001 in 141 us, with 64 x 64 tiles of fp32 MFMA 178; 8 x 4000 x 1001
-    // x 999 107 for 103)
-    const float wide = a.K % 8 == 0 && a.C % 8 == 0 ? tile_time(a, 2, kBackWideCost) : 3e38f;
-    if (wide < std::min(one, two)) return launch_tiles("mm_back_wide", mm_back_wide_kernel, a, BM, BP, kThreads, st);
+    if (tile_time(a, 2, kBackWideCost) < std::min(one, two))
+        return launch_tiles("mm_back_wide", mm_back_wide_kernel, a, BM, BP, kThreads, st);
     if (one <= two) return launch_tiles("mm_back_thin", mm_back_thin_kernel<bf16_t, 1>, a, 16, 128, 256, st);
     return launch_tiles("mm_back_thin2", mm_back_thin_kernel<bf16_t, 2>, a, 32, 128, 256, st);
 }

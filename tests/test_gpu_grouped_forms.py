@@ -70,7 +70,7 @@ def setup(N, mean, C, K, dt, seed=0, k=3):
 PRODUCTS = [
     # name, type, N, mean rows, C, K
     ("mm_thin", "bf16", 3, 30, 130, 136), ("mm_thin", "bf16", 1, 77, 1001, 1032), ("mm_thin", "bf16", 5, 40, 333, 131),
-    ("mm_thin", "bf16", 16, 200, 515, 517),
+    ("mm_tile", "bf16", 16, 200, 515, 517), ("mm_tile", "bf16", 8, 500, 333, 130), ("mm_thin", "bf16", 5, 900, 135, 1001),
     ("mm_few", "bf16", 64, 40, 520, 200), ("mm_few", "bf16", 64, 45, 1001, 1032), ("mm_few", "bf16", 9, 300, 1000, 136),
     ("mm_mid", "bf16", 64, 200, 1000, 520), ("mm_mid", "bf16", 64, 210, 901, 200),
     ("mm_wide", "bf16", 16, 700, 1400, 136), ("mm_wide", "bf16", 16, 650, 1303, 520), ("mm_wide", "bf16", 3, 5000, 2000, 1032),
@@ -131,8 +131,10 @@ def test_product_in_8_bits(name, N, mean, C, K, bf16):
 
 
 BACK = [
-    ("mm_back_thin2", "bf16", 2, 8, 136, 264), ("mm_back_thin", "bf16", 4, 20, 333, 131),
-    ("mm_back_thin2", "bf16", 8, 300, 520, 1000), ("mm_back_thin2", "bf16", 16, 700, 333, 517),
+    ("mm_back_thin2", "bf16", 2, 8, 136, 264), ("mm_back_tile", "bf16", 4, 20, 333, 131), ("mm_back_thin", "bf16", 4, 6, 1000, 136),
+    ("mm_back_thin2", "bf16", 8, 300, 520, 1000), ("mm_back_tile", "bf16", 2, 60, 333, 517),
+    ("mm_back_tile", "bf16", 16, 700, 333, 517), ("mm_back_tile", "bf16", 5, 900, 1001, 135), ("mm_back_tile", "bf16", 3, 2000, 66, 1004),
+   
     ("mm_back_wide", "bf16", 64, 500, 520, 1000), ("mm_back_wide", "bf16", 16, 2000, 72, 520),
     ("mm_back_wide", "bf16", 40, 900, 1048, 776),
     ("mm_back_thin", "f32", 7, 90, 135, 203), ("mm_back_tile", "f32", 16, 900, 250, 333),
