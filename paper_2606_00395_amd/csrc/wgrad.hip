@@ -12,6 +12,9 @@
 namespace pr2 {
 namespace {
 
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+
 struct WgradArgs {
     const void* dy;             // [R, n_out]
     const int8_t* q;            // [Rx, n_in]; null: x is not packed
@@ -57,7 +60,9 @@ __device__ __forceinline__ int source_row(const WgradArgs& a, int r) {
 // fp32 at a time, the next 32 in flight meanwhile.  Small layers are bound by the latency of
 // that chain (with the packing 15.5 us at 1226 rows, 7 experts of 135 x 203; 17.7 where the
 // operands were opened on arrival), large ones by the fp32 MFMA and the LDS (112 TFLOP/s at
-// 4096 x 4096 over 32768 rows, where the library's fp32 product reaches 154).
+// 4096 x 4096 over 32768 rows, where the library's fp32 product reaches 154).  dy and rows of x in bf16
+// stay so: v_mfma_f32_32x32x16_bf16 with the transposing LDS read (4096 x 1001 x 999 in 90 us, opened to
+// fp32 119).
 constexpr int kTile = 64;
 constexpr int kStep = 32;
 constexpr int kTilePitch = kTile + 32;      // the two halves of a wavefront read other banks
@@ -134,10 +139,35 @@ __global__ void __launch_bounds__(256) wgrad_tile_kernel(WgradArgs a) {
         }
     };
     const int ao = 32 * (wave >> 1) + (lane & 31), bo = 32 * (wave & 1) + (lane & 31), k2 = lane >> 5;
+    // bf16: 8 rows' values of a wavefront's column, from row k + 8 (lane / 32) on, four of them a read
+    constexpr bool kBf16 = !PACKED && sizeof(T) == 2;
+    constexpr int kPitch16 = 2 * kTile + 16;
+    unsigned char* const A16 = (unsigned char*)A;
+    unsigned char* const B16 = (unsigned char*)B;
+    const int s16 = lane & 15, nl = 16 * ((lane >> 4) & 1) + 4 * (s16 & 3), kl = 8 * k2 + (s16 >> 2);
+    auto columns = [&](const unsigned char* from, int k, int col) __attribute__((always_inline)) {
+        const unsigned char* p = from + (k + kl) * kPitch16 + (col + nl) * 2;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)p);
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * kPitch16));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
     if (a.Rx == 0) last = first;        // no row has a source
     if (first < last) fetch(first);
     for (int r0 = first; r0 < last; r0 += kStep) {
         // a row without a source is zeros in both operands: nothing of it multiplies
+        if constexpr (kBf16) {
+            const u32x4 none = {0, 0, 0, 0};
+            __syncthreads();
+            *(u32x4*)(A16 + sr * kPitch16 + sc * 2) = on ? wa[0] : none;
+            *(u32x4*)(B16 + sr * kPitch16 + sc * 2) = on ? wx[0] : none;
+            __syncthreads();
+            if (r0 + kStep < last) fetch(r0 + kStep);
+#pragma unroll
+            for (int k = 0; k < kStep; k += 16)
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(columns(A16, k, 32 * (wave >> 1)),
+                                                              columns(B16, k, 32 * (wave & 1)), acc, 0, 0, 0);
+            continue;
+        }
         float va[8], vb[8];
 #pragma unroll
         for (int i = 0; i < 8 / E; ++i) {
@@ -299,8 +329,6 @@ constexpr int kRowsHeld = 8128;             // row indexes held in LDS
 constexpr int kNumXcd = 8;
 constexpr uint32_t kNoRow = 0xffffffffu;
 
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) v4s lds_v4s;
 __device__ __attribute__((aligned(16))) const bf16_t kZeros[8] = {};
 
 template <int n>
@@ -801,10 +829,11 @@ bool order_pays(const pr2_wgrad_desc& d, int64_t items) {
 }
 
 // Few rows an expert and few outputs: 7 experts of 135 x 203 over 175 rows each 8.7 -> 6.2 us, one of 32 x 32 over
-// 175 9.5 -> 6.2 (over 1226 9.7 -> 15.1), 7 of 400 x 390 over 175 13.3 -> 11.6, of 1001 x 999 41 -> 50.
+// 175 9.5 -> 6.2 (over 1226 9.7 -> 15.1), 7 of 400 x 390 over 175 13.3 -> 11.6, of 1001 x 999 41 -> 50.  In bf16,
+// whose 64 x 64 tiles are faster, 8.4 -> 7.4 and 8.4 -> 7.5, but 9.4 -> 13.0.
 bool thin_ok(const pr2_wgrad_desc& d, bool packed) {
     return !packed && d.R > 0 && !mfma_ok(d, packed) && d.R <= 512 * (int64_t)d.N &&
-           wgrad_tile_count(d, kThin) <= 5 * kCus;
+           wgrad_tile_count(d, kThin) <= (d.act_dtype == PR2_BF16 ? 1 : 5) * kCus;
 }
 
 struct WgradWs {
