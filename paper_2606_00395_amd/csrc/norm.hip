@@ -285,7 +285,10 @@ __global__ void __launch_bounds__(back_threads<NW>()) norm_backward_kernel(NormB
                 const float v = r * (y[j] * w[i * E + j] - h[j] * r * mean);
                 y[j] = a.dh ? v + e[j] : v;
             }
-            g.store((T*)a.dx + row * a.d, i, Chunk<T>::close(y));
+            // (dx may lie on dh, of which another wavefront may not yet hold what a moved-back piece shares
+            // with it: h and dy have been summed before the barrier)
+            if (NW > 1) g.store_own((T*)a.dx + row * a.d, i, Chunk<T>::close(y));
+            else g.store((T*)a.dx + row * a.d, i, Chunk<T>::close(y));
         }
         if (NW == 16) cur = next;
     }

@@ -39,6 +39,16 @@ template <typename T, int NW, int F> struct RowGroup {
         if (narrow()) copy_chunk<T>(row, 0, 0, d, w);
         else store16<false>(row + start(i), w);
     }
+    // without the elements that another piece counts
+    __device__ __forceinline__ void store_own(T* row, int i, const u32x4& w) const {
+        const int n = skip(i);
+        if (n <= 0 || !on(i)) return store(row, i, w);
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+            if (j >= n)
+                row[start(i) + j] =
+                    __builtin_bit_cast(T, (typename Chunk<T>::Bits)(E == 8 ? w[j / 2] >> (16 * (j & 1)) : w[j]));
+    }
     // the same of an fp32 row beside it (which starts at any float)
     __device__ __forceinline__ void load_f32(const float* row, int i, float* v) const {
         typedef f32x4 f32x4_any __attribute__((aligned(4)));

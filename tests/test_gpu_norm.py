@@ -194,6 +194,25 @@ def test_backward(T, d, bf16):
             assert torch.equal(to, dx), on
 
 
+@TYPES
+@pytest.mark.parametrize("T,d", [(9, 40), (70, 333), (700, 2049), (300, 2055), (600, 4099), (300, 8191), (520, 8193), (40, 16387)])
+def test_backward_in_place(T, d, bf16):
+    """dx on each of its inputs, also where a row's last piece is moved back over another wavefront's."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T)
+    D = torch.bfloat16 if bf16 else torch.float32
+    at = {n: torch.randn((T, d), generator=g, device="cuda").to(D) for n in ("dy", "h", "dh")}
+    w, r = torch.rand(d, generator=g, device="cuda"), torch.rand(T, generator=g, device="cuda")
+    want, dw = torch.empty_like(at["h"]), torch.empty(d, device="cuda")
+    B.rms_norm_backward(at["dy"], at["h"], r, w, want, at["dh"], dw)
+    for n in at:
+        now = {k: v.clone() for k, v in at.items()}
+        dw2 = torch.empty(d, device="cuda")
+        B.rms_norm_backward(now["dy"], now["h"], r, w, now[n], now["dh"], dw2)
+        assert torch.equal(now[n], want) and torch.equal(dw, dw2), n
+
+
 def test_backward_against_differences():
     import torch
     from paper_2606_00395_amd import binding as B
