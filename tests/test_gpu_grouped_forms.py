@@ -188,3 +188,61 @@ def test_weight_gradients(name, dt, N, mean, n_out, n_in):
         y, xr = dy[r][on].double(), x[src[r][on]].double()
         want, mag = y.T @ xr, y.abs().T @ xr.abs()
         assert ((dW[e].double() - want).abs() <= (y.shape[0] + 2) * 2.0 ** -23 * mag).all()
+
+
+@pytest.mark.parametrize("name,dt,N,mean,C,K", [p for p in PRODUCTS if p[0] != "mm_thin"][:-4] + PRODUCTS[-2:],
+                         ids=lambda v: str(v))
+def test_no_number_reaches_another_row_or_column(name, dt, N, mean, C, K):
+    """A NaN in two rows of x, an infinity in one row of an expert's weights, both at their first and last K, and
+    rows without a source beside them."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    D = torch.bfloat16 if dt == "bf16" else torch.float32
+    off, R, route, src, x, W, k = setup(N, mean, C, K, D)
+    dy = torch.randn((R, C), device="cuda").to(D)
+    clean, back = torch.empty((R, C), dtype=D, device="cuda"), torch.empty((R, K), dtype=D, device="cuda")
+    B.grouped_mm(x, W, clean, offsets=off, route_of_row=route, k=k)
+    B.grouped_mm_backward(dy, W, back, offsets=off)
+    e = N - 1
+    own = torch.zeros(R, dtype=torch.bool, device="cuda")
+    own[int(off[e]):int(off[e + 1])] = True
+    bad_tokens = [int(src[src >= 0][0]), int(src[src >= 0][-1])]
+    x[bad_tokens[0], K - 1] = x[bad_tokens[1], 0] = float("nan")
+    W[e, C // 2, K - 1] = float("inf")
+    W[e, C // 2, 0] = float("inf")
+    rows = (src == bad_tokens[0]) | (src == bad_tokens[1])
+    rows[int(off[-1]):] = False
+    column = torch.zeros(C, dtype=torch.bool, device="cuda")
+    column[C // 2] = True
+    out = torch.empty_like(clean)
+    B.grouped_mm(x, W, out, offsets=off, route_of_row=route, k=k)
+    may = rows.unsqueeze(1) | (own & (src >= 0)).unsqueeze(1) & column
+    assert torch.equal(out[~may], clean[~may]) and torch.isnan(out[rows]).all()
+    # the rows' gradients: of those weights, columns 0 and K - 1 of the expert's rows; a NaN of dy its row
+    dy[3 if N == 1 else int(off[1]) + 3, C - 1] = float("nan")
+    dx = torch.empty_like(back)
+    B.grouped_mm_backward(dy, W, dx, offsets=off)
+    may = torch.zeros((R, K), dtype=torch.bool, device="cuda")
+    may[own, 0] = may[own, K - 1] = True
+    may[3 if N == 1 else int(off[1]) + 3] = True
+    assert torch.equal(dx[~may], back[~may])
+
+
+@pytest.mark.parametrize("C,K,mean", [(1400, 136, 700), (901, 200, 210), (333, 131, 900)], ids=["wide", "mid", "tile"])
+def test_offsets_that_fall_or_overrun(C, K, mean):
+    """Any offsets: no fault, nothing behind the outputs."""
+    import torch
+    from paper_2606_00395_amd import binding as B
+    N = 16
+    off, R, route, src, x, W, k = setup(N, mean, C, K, torch.bfloat16)
+    dy = torch.randn((R, C), device="cuda").to(torch.bfloat16)
+    g = torch.Generator().manual_seed(0)
+    for t in range(4):
+        o = torch.randint(-3 * R, 3 * R, (N + 1,), generator=g).to(torch.int32).cuda()
+        if t == 3:
+            o[::2], o[1::2] = 0, R
+        out = torch.full((R + 300, C), 9.0, dtype=torch.bfloat16, device="cuda")
+        dx = torch.full((R + 300, K), 9.0, dtype=torch.bfloat16, device="cuda")
+        B.grouped_mm(x, W, out[:R], offsets=o, route_of_row=route, k=k)
+        B.grouped_mm_backward(dy, W, dx[:R], offsets=o)
+        assert torch.all(out[R:] == 9) and torch.all(dx[R:] == 9)
