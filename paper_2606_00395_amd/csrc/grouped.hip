@@ -52,7 +52,7 @@ __device__ __forceinline__ int source(const MmArgs& a, int r) {
 // staged in LDS, the next 32 in flight meanwhile.  An operand whose rows run along K is read four K at a time; the
 // weights of dy W, whose rows run along the columns, one K at a time.  A step's four K of either half
 // wavefront are the same in both operands, so that any order of them gives the sum.  (2000 x 2000 x 2000
-// in 144 us, 111 TFLOP/s; the library's product 121.)
+// in 171 us, 4096 x 4096 x 4096 in 1214, 113 TFLOP/s; the library's products 144 and 915.)
 constexpr int kTile = 64;
 constexpr int kStep = 32;
 constexpr int kRowPitch = kStep + 4;        // 16-byte reads of 32 rows: every bank equally often
