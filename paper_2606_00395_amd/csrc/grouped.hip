@@ -452,8 +452,8 @@ mm_wide_kernel(MmArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave >> 1, wc = wave & 1;
     const int c0 = t.panel * BP;
-    // blocks past the tile's rows or the matrix only help copy
-    const bool active = wr * WM < t.rows && c0 + wc * WN < a.C;
+    // wavefronts past the tile's rows or the matrix only help copy
+    const bool active = wr * MT < t.rows && c0 + wc * WN < a.C;
     const int kb = a.K * (int)sizeof(E);
 
     // wavefront w copies rows 32 w + 8 i + lane / 8 of both operands (past their ends the last one)
@@ -487,6 +487,7 @@ mm_wide_kernel(MmArgs a) {
         if (!decltype(PART)::value) dma16_to(from, off[i], to + i * 1024);
         else dma16_to((chunk0 ^ (i & 1)) * 16 < kb - kt * kRowB ? from + off[i] : kZeros, to + i * 1024);
     };
+    const bool has_x = wrow0 < t.rows;      // (asked where the tile has up to 128 rows)
     auto issue_x = [&](auto PART, int kt, int stage, int i) __attribute__((always_inline)) {
         issue(PART, xb, xo, kt, lds0 + stage * kOperandB, i);
     };
@@ -494,9 +495,15 @@ mm_wide_kernel(MmArgs a) {
         issue(PART, wb, wo, kt, lds0 + (3 + (kt & 1)) * kOperandB, i);
     };
 
-    typename M::Acc acc[MI][NJ];
+    // The tile's rows in BLOCKS times 64: block i of a wavefront is rows 64 i + 16 wr on, so that a tile of fewer rows
+    // takes fewer MFMAs of all (16384 tokens, 8 of 128 experts unevenly, 1536 x 2048: 797 -> 783 us; a tile of up to 64
+    // rows still costs half of a full one, for the latency of its slices' copies).
+    auto run = [&](auto BLOCKS) __attribute__((always_inline)) {
+    constexpr int MB = decltype(BLOCKS)::value;
+    constexpr bool kFewRows = MB <= 2;
+    typename M::Acc acc[MB][NJ];
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -508,14 +515,15 @@ mm_wide_kernel(MmArgs a) {
     int kpos[2];
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
-    const int a0 = wr * WM * kRowB, b0 = (3 * BM + wc * WN) * kRowB;
-    typename M::Frag fa[2][MI], fb[2][NJ];
+    const int a0 = wr * MT * kRowB, b0 = (3 * BM + wc * WN) * kRowB;
+    typename M::Frag fa[2][MB], fb[2][NJ];
     auto frag = [&](int at) __attribute__((always_inline)) {
         return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(lds + at));
     };
     // the slice before that of the last n copies has arrived, and this wavefront's LDS reads have ended
     auto sync = [&](auto N) __attribute__((always_inline)) {
-        wait_vmcnt<decltype(N)::value>();
+        if (!kFewRows || has_x) wait_vmcnt<decltype(N)::value>();
+        else wait_vmcnt<0>();
         __builtin_amdgcn_s_waitcnt(0xc07f);
         plain_barrier();
     };
@@ -531,13 +539,13 @@ mm_wide_kernel(MmArgs a) {
 #pragma unroll
             for (int j = 2 * q; j < 2 * q + 2; ++j)
 #pragma unroll
-                for (int i = 0; i < MI; ++i) acc[i][j] = M::mul(fb[S][j], fa[S][i], acc[i][j]);
+                for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(fb[S][j], fa[S][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
             if (decltype(READ)::value && q < 3) {
                 if (q < 2) {
 #pragma unroll
                     for (int h = 2 * q; h < 2 * q + 2; ++h) {
-                        fa[S ^ 1][h] = frag(xa + h * MT * kRowB);
+                        if (h < MB) fa[S ^ 1][h < MB ? h : 0] = frag(xa + h * 4 * MT * kRowB);
                         fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
                     }
                 } else {
@@ -553,22 +561,25 @@ mm_wide_kernel(MmArgs a) {
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i = 0; i < kCopy; ++i) {
-            issue_x(C1{}, kt, kt, i);
+            if (!kFewRows || has_x) issue_x(C1{}, kt, kt, i);
             issue_w(C1{}, kt, i);
         }
-    wait_vmcnt<2 * kCopy>();
+    if (!kFewRows || has_x) wait_vmcnt<2 * kCopy>();
+    else wait_vmcnt<kCopy>();
     plain_barrier();
     int kt = 0, xs = 0;         // the slice and its rows' stage
     auto next = [](int s) __attribute__((always_inline)) { return s == 2 ? 0 : s + 1; };
     if (active) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) fa[0][i] = frag(kpos[0] + a0 + i * MT * kRowB);
+        for (int i = 0; i < MB; ++i) fa[0][i] = frag(kpos[0] + a0 + i * 4 * MT * kRowB);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) fb[0][j] = frag(kpos[0] + b0 + j * MT * kRowB);
         // slice kt with the copies of slice kt + 2
         auto slice = [&](auto PART) __attribute__((always_inline)) {
             const int x1 = next(xs), x2 = next(x1);
-            phase(C0{}, C1{}, xs, kt & 1, 1, [&](int q) __attribute__((always_inline)) { issue_x(PART, kt + 2, x2, q); });
+            phase(C0{}, C1{}, xs, kt & 1, 1, [&](int q) __attribute__((always_inline)) {
+                if (!kFewRows || has_x) issue_x(PART, kt + 2, x2, q);
+            });
             sync(Behind{});
             phase(C1{}, C1{}, x1, (kt + 1) & 1, 0, [&](int q) __attribute__((always_inline)) { issue_w(PART, kt + 2, q); });
             xs = x1;
@@ -584,7 +595,8 @@ mm_wide_kernel(MmArgs a) {
     } else {
         for (; kt + 2 < nk; ++kt) {
 #pragma unroll
-            for (int i = 0; i < kCopy; ++i) issue_x(C1{}, kt + 2, next(next(xs)), i);
+            for (int i = 0; i < kCopy; ++i)
+                if (!kFewRows || has_x) issue_x(C1{}, kt + 2, next(next(xs)), i);
             sync(Behind{});
 #pragma unroll
             for (int i = 0; i < kCopy; ++i) issue_w(C1{}, kt + 2, i);
@@ -593,14 +605,15 @@ mm_wide_kernel(MmArgs a) {
         sync(C0{});
     }
 
-    // a lane's rows: 16 i + lane % 16 of the wavefront's block
+    // a lane's rows: lane % 16 of the wavefront's blocks
+    auto row_of = [&](int i) __attribute__((always_inline)) { return 4 * MT * i + wr * MT + lrow; };
     const int col0 = c0 + wc * WN + 4 * grp;
-    bool on[MI];
-    float sr[MI];
+    bool on[MB];
+    float sr[MB];
     if (active) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int src = source(a, t.row0 + min(wr * WM + i * MT + lrow, t.rows - 1));
+        for (int i = 0; i < MB; ++i) {
+            const int src = source(a, t.row0 + min(row_of(i), t.rows - 1));
             on[i] = src >= 0;
             sr[i] = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
         }
@@ -614,8 +627,8 @@ mm_wide_kernel(MmArgs a) {
         for (int j = 0; j < NJ; ++j) {
             const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int r = wr * WM + i * MT + lrow;
+            for (int i = 0; i < MB; ++i) {
+                const int r = row_of(i);
                 if (r < t.rows)
                     store_four((O*)a.out + (int64_t)(t.row0 + r) * a.C, col0 + j * MT, a.C,
                                finish<E>(acc[i][j], on[i], sr[i], s4));
@@ -634,7 +647,7 @@ mm_wide_kernel(MmArgs a) {
     for (int j = 0; j < NJ; ++j) {
         const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
+        for (int i = 0; i < MB; ++i) {
             const int row = i * MT + lrow, col = j * MT + 4 * grp;
             const f32x4 y = finish<E>(acc[i][j], on[i], sr[i], s4);
             const uint32_t lo = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16;
@@ -649,9 +662,9 @@ mm_wide_kernel(MmArgs a) {
     const int ch = lane % NCH;
     const int col = c0 + wc * WN + ch * 8, left = a.C - col;
 #pragma unroll
-    for (int p = 0; p < WM / (64 / NCH); ++p) {
+    for (int p = 0; p < MB * MT / (64 / NCH); ++p) {
         const int row = p * (64 / NCH) + lane / NCH;
-        const int r = wr * WM + row;
+        const int r = 4 * MT * (row / MT) + wr * MT + row % MT;
         u32x4 v = *(const u32x4*)(stage_w + row * RB + ((ch ^ (row & (NCH - 1))) << 4));
         if (row & 8) v = u32x4{v[2], v[3], v[0], v[1]};
         if (r >= t.rows) continue;
@@ -664,6 +677,12 @@ mm_wide_kernel(MmArgs a) {
                 if (e < left) to[e] = (bf16_t)(v[e / 2] >> (16 * (e & 1)));
         }
     }
+    };
+    const int blocks = (t.rows + 4 * MT - 1) / (4 * MT);
+    if (blocks == 4) run(std::integral_constant<int, 4>{});
+    else if (blocks == 3) run(std::integral_constant<int, 3>{});
+    else if (blocks == 2) run(std::integral_constant<int, 2>{});
+    else run(std::integral_constant<int, 1>{});
 }
 
 // Few rows per expert: the weights' bytes in flight are what matters.  64 rows x 128 columns per
