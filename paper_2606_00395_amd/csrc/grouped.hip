@@ -499,184 +499,184 @@ mm_wide_kernel(MmArgs a) {
     // takes fewer MFMAs of all (16384 tokens, 8 of 128 experts unevenly, 1536 x 2048: 797 -> 783 us; a tile of up to 64
     // rows still costs half of a full one, for the latency of its slices' copies).
     auto run = [&](auto BLOCKS) __attribute__((always_inline)) {
-    constexpr int MB = decltype(BLOCKS)::value;
-    constexpr bool kFewRows = MB <= 2;
-    typename M::Acc acc[MB][NJ];
+        constexpr int MB = decltype(BLOCKS)::value;
+        constexpr bool kFewRows = MB <= 2;
+        typename M::Acc acc[MB][NJ];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+            for (int j = 0; j < NJ; ++j)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
-    // fragments: lane l reads row l % 16 of a block, chunk 4 ks + (0, 2, 1, 3)[l / 16] (both operands
-    // alike, and so that the two halves of a read cycle hit disjoint banks)
-    const int lrow = lane & 15, grp = lane >> 4;
-    const int cperm = ((grp & 1) << 1) | (grp >> 1);
-    int kpos[2];
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = 0;
+        // fragments: lane l reads row l % 16 of a block, chunk 4 ks + (0, 2, 1, 3)[l / 16] (both operands
+        // alike, and so that the two halves of a read cycle hit disjoint banks)
+        const int lrow = lane & 15, grp = lane >> 4;
+        const int cperm = ((grp & 1) << 1) | (grp >> 1);
+        int kpos[2];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
-    const int a0 = wr * MT * kRowB, b0 = (3 * BM + wc * WN) * kRowB;
-    typename M::Frag fa[2][MB], fb[2][NJ];
-    auto frag = [&](int at) __attribute__((always_inline)) {
-        return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(lds + at));
-    };
-    // the slice before that of the last n copies has arrived, and this wavefront's LDS reads have ended
-    auto sync = [&](auto N) __attribute__((always_inline)) {
-        if (!kFewRows || has_x) wait_vmcnt<decltype(N)::value>();
-        else wait_vmcnt<0>();
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        plain_barrier();
-    };
-    // MFMAs of a sub-step on fragment set S, among them the reads of the next one's (sub-step ks of the rows'
-    // stage xs and the weights' ws) and copy(0 .. 3)
-    auto phase = [&](auto S_, auto READ, int xs, int ws, int ks, auto copy) __attribute__((always_inline)) {
-        constexpr int S = decltype(S_)::value;
-        const int xa = xs * kOperandB + kpos[ks] + a0, wa = ws * kOperandB + kpos[ks] + b0;
+        for (int ks = 0; ks < 2; ++ks) kpos[ks] = lrow * kRowB + (((4 * ks + cperm) ^ swz(lrow)) << 4);
+        const int a0 = wr * MT * kRowB, b0 = (3 * BM + wc * WN) * kRowB;
+        typename M::Frag fa[2][MB], fb[2][NJ];
+        auto frag = [&](int at) __attribute__((always_inline)) {
+            return __builtin_bit_cast(typename M::Frag, *(const u32x4*)(lds + at));
+        };
+        // the slice before that of the last n copies has arrived, and this wavefront's LDS reads have ended
+        auto sync = [&](auto N) __attribute__((always_inline)) {
+            if (!kFewRows || has_x) wait_vmcnt<decltype(N)::value>();
+            else wait_vmcnt<0>();
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            plain_barrier();
+        };
+        // MFMAs of a sub-step on fragment set S, among them the reads of the next one's (sub-step ks of the rows'
+        // stage xs and the weights' ws) and copy(0 .. 3)
+        auto phase = [&](auto S_, auto READ, int xs, int ws, int ks, auto copy) __attribute__((always_inline)) {
+            constexpr int S = decltype(S_)::value;
+            const int xa = xs * kOperandB + kpos[ks] + a0, wa = ws * kOperandB + kpos[ks] + b0;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            copy(q);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int q = 0; q < 4; ++q) {
+                copy(q);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 2 * q; j < 2 * q + 2; ++j)
+                for (int j = 2 * q; j < 2 * q + 2; ++j)
 #pragma unroll
-                for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(fb[S][j], fa[S][i], acc[i][j]);
-            __builtin_amdgcn_sched_barrier(0);
-            if (decltype(READ)::value && q < 3) {
-                if (q < 2) {
+                    for (int i = 0; i < MB; ++i) acc[i][j] = M::mul(fb[S][j], fa[S][i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (decltype(READ)::value && q < 3) {
+                    if (q < 2) {
 #pragma unroll
-                    for (int h = 2 * q; h < 2 * q + 2; ++h) {
-                        if (h < MB) fa[S ^ 1][h < MB ? h : 0] = frag(xa + h * 4 * MT * kRowB);
-                        fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
+                        for (int h = 2 * q; h < 2 * q + 2; ++h) {
+                            if (h < MB) fa[S ^ 1][h < MB ? h : 0] = frag(xa + h * 4 * MT * kRowB);
+                            fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 4; h < NJ; ++h) fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
                     }
-                } else {
-#pragma unroll
-                    for (int h = 4; h < NJ; ++h) fb[S ^ 1][h] = frag(wa + h * MT * kRowB);
                 }
             }
-        }
-    };
-    auto no_copy = [](int) {};
-    using Behind = std::integral_constant<int, kCopy>;
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < kCopy; ++i) {
-            if (!kFewRows || has_x) issue_x(C1{}, kt, kt, i);
-            issue_w(C1{}, kt, i);
-        }
-    if (!kFewRows || has_x) wait_vmcnt<2 * kCopy>();
-    else wait_vmcnt<kCopy>();
-    plain_barrier();
-    int kt = 0, xs = 0;         // the slice and its rows' stage
-    auto next = [](int s) __attribute__((always_inline)) { return s == 2 ? 0 : s + 1; };
-    if (active) {
-#pragma unroll
-        for (int i = 0; i < MB; ++i) fa[0][i] = frag(kpos[0] + a0 + i * 4 * MT * kRowB);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) fb[0][j] = frag(kpos[0] + b0 + j * MT * kRowB);
-        // slice kt with the copies of slice kt + 2
-        auto slice = [&](auto PART) __attribute__((always_inline)) {
-            const int x1 = next(xs), x2 = next(x1);
-            phase(C0{}, C1{}, xs, kt & 1, 1, [&](int q) __attribute__((always_inline)) {
-                if (!kFewRows || has_x) issue_x(PART, kt + 2, x2, q);
-            });
-            sync(Behind{});
-            phase(C1{}, C1{}, x1, (kt + 1) & 1, 0, [&](int q) __attribute__((always_inline)) { issue_w(PART, kt + 2, q); });
-            xs = x1;
         };
-        for (; kt + 2 < whole; ++kt) slice(C0{});
-        for (; kt + 2 < nk; ++kt) slice(C1{});
-        phase(C0{}, C1{}, xs, kt & 1, 1, no_copy);
-        sync(C0{});
-        xs = next(xs);
-        phase(C1{}, C1{}, xs, (kt + 1) & 1, 0, no_copy);
-        phase(C0{}, C1{}, xs, (kt + 1) & 1, 1, no_copy);
-        phase(C1{}, C0{}, 0, 0, 0, no_copy);
-    } else {
-        for (; kt + 2 < nk; ++kt) {
+        auto no_copy = [](int) {};
+        using Behind = std::integral_constant<int, kCopy>;
 #pragma unroll
-            for (int i = 0; i < kCopy; ++i)
-                if (!kFewRows || has_x) issue_x(C1{}, kt + 2, next(next(xs)), i);
-            sync(Behind{});
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int i = 0; i < kCopy; ++i) issue_w(C1{}, kt + 2, i);
+            for (int i = 0; i < kCopy; ++i) {
+                if (!kFewRows || has_x) issue_x(C1{}, kt, kt, i);
+                issue_w(C1{}, kt, i);
+            }
+        if (!kFewRows || has_x) wait_vmcnt<2 * kCopy>();
+        else wait_vmcnt<kCopy>();
+        plain_barrier();
+        int kt = 0, xs = 0;         // the slice and its rows' stage
+        auto next = [](int s) __attribute__((always_inline)) { return s == 2 ? 0 : s + 1; };
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) fa[0][i] = frag(kpos[0] + a0 + i * 4 * MT * kRowB);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) fb[0][j] = frag(kpos[0] + b0 + j * MT * kRowB);
+            // slice kt with the copies of slice kt + 2
+            auto slice = [&](auto PART) __attribute__((always_inline)) {
+                const int x1 = next(xs), x2 = next(x1);
+                phase(C0{}, C1{}, xs, kt & 1, 1, [&](int q) __attribute__((always_inline)) {
+                    if (!kFewRows || has_x) issue_x(PART, kt + 2, x2, q);
+                });
+                sync(Behind{});
+                phase(C1{}, C1{}, x1, (kt + 1) & 1, 0, [&](int q) __attribute__((always_inline)) { issue_w(PART, kt + 2, q); });
+                xs = x1;
+            };
+            for (; kt + 2 < whole; ++kt) slice(C0{});
+            for (; kt + 2 < nk; ++kt) slice(C1{});
+            phase(C0{}, C1{}, xs, kt & 1, 1, no_copy);
+            sync(C0{});
             xs = next(xs);
-        }
-        sync(C0{});
-    }
-
-    // a lane's rows: lane % 16 of the wavefront's blocks
-    auto row_of = [&](int i) __attribute__((always_inline)) { return 4 * MT * i + wr * MT + lrow; };
-    const int col0 = c0 + wc * WN + 4 * grp;
-    bool on[MB];
-    float sr[MB];
-    if (active) {
+            phase(C1{}, C1{}, xs, (kt + 1) & 1, 0, no_copy);
+            phase(C0{}, C1{}, xs, (kt + 1) & 1, 1, no_copy);
+            phase(C1{}, C0{}, 0, 0, 0, no_copy);
+        } else {
+            for (; kt + 2 < nk; ++kt) {
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
-            const int src = source(a, t.row0 + min(row_of(i), t.rows - 1));
-            on[i] = src >= 0;
-            sr[i] = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+                for (int i = 0; i < kCopy; ++i)
+                    if (!kFewRows || has_x) issue_x(C1{}, kt + 2, next(next(xs)), i);
+                sync(Behind{});
+#pragma unroll
+                for (int i = 0; i < kCopy; ++i) issue_w(C1{}, kt + 2, i);
+                xs = next(xs);
+            }
+            sync(C0{});
         }
-    }
-    const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
-    const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (sizeof(O) == 4) {
-        // 64 bytes of a row per store and 16 lanes, straight from the registers
+
+        // a lane's rows: lane % 16 of the wavefront's blocks
+        auto row_of = [&](int i) __attribute__((always_inline)) { return 4 * MT * i + wr * MT + lrow; };
+        const int col0 = c0 + wc * WN + 4 * grp;
+        bool on[MB];
+        float sr[MB];
+        if (active) {
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const int src = source(a, t.row0 + min(row_of(i), t.rows - 1));
+                on[i] = src >= 0;
+                sr[i] = sizeof(E) == 1 ? a.row_scale[max(src, 0)] : 0.0f;
+            }
+        }
+        const float* sw = sizeof(E) == 1 ? a.w_scale + (int64_t)t.expert * a.C : nullptr;
+        const f32x4 none = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (sizeof(O) == 4) {
+            // 64 bytes of a row per store and 16 lanes, straight from the registers
+            if (!active) return;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {
+                    const int r = row_of(i);
+                    if (r < t.rows)
+                        store_four((O*)a.out + (int64_t)(t.row0 + r) * a.C, col0 + j * MT, a.C,
+                                   finish<E>(acc[i][j], on[i], sr[i], s4));
+                }
+            }
+            return;
+        }
+        // bf16: through this wavefront's share of the freed stages (16-byte chunks XOR-swizzled by row, the
+        // halves of a chunk swapped in rows with bit 3 set: every write cycle's rows in other banks), so
+        // that a store covers whole 256-byte row segments
+        __syncthreads();
         if (!active) return;
+        constexpr int RB = WN * 2, NCH = RB / 16;
+        unsigned char* stage_w = lds + wave * (WM * RB);
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
             const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const int r = row_of(i);
-                if (r < t.rows)
-                    store_four((O*)a.out + (int64_t)(t.row0 + r) * a.C, col0 + j * MT, a.C,
-                               finish<E>(acc[i][j], on[i], sr[i], s4));
+                const int row = i * MT + lrow, col = j * MT + 4 * grp;
+                const f32x4 y = finish<E>(acc[i][j], on[i], sr[i], s4);
+                const uint32_t lo = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16;
+                const uint32_t hi = (uint32_t)f32_to_bf16(y[2]) | (uint32_t)f32_to_bf16(y[3]) << 16;
+                *(uint2*)(stage_w + row * RB + (((col >> 3) ^ (row & (NCH - 1))) << 4) + (((col & 4) << 1) ^ (row & 8))) =
+                    make_uint2(lo, hi);
             }
         }
-        return;
-    }
-    // bf16: through this wavefront's share of the freed stages (16-byte chunks XOR-swizzled by row, the
-    // halves of a chunk swapped in rows with bit 3 set: every write cycle's rows in other banks), so
-    // that a store covers whole 256-byte row segments
-    __syncthreads();
-    if (!active) return;
-    constexpr int RB = WN * 2, NCH = RB / 16;
-    unsigned char* stage_w = lds + wave * (WM * RB);
+        // (one wavefront's own region: its LDS operations complete in order)
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_wave_barrier();
+        const int ch = lane % NCH;
+        const int col = c0 + wc * WN + ch * 8, left = a.C - col;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const f32x4 s4 = sizeof(E) == 1 ? four_scales(sw, col0 + j * MT, a.C) : none;
+        for (int p = 0; p < MB * MT / (64 / NCH); ++p) {
+            const int row = p * (64 / NCH) + lane / NCH;
+            const int r = 4 * MT * (row / MT) + wr * MT + row % MT;
+            u32x4 v = *(const u32x4*)(stage_w + row * RB + ((ch ^ (row & (NCH - 1))) << 4));
+            if (row & 8) v = u32x4{v[2], v[3], v[0], v[1]};
+            if (r >= t.rows) continue;
+            bf16_t* to = (bf16_t*)a.out + (int64_t)(t.row0 + r) * a.C + col;
+            if (left >= 8) {
+                store16<STREAM>(to, v);
+            } else {
 #pragma unroll
-        for (int i = 0; i < MB; ++i) {
-            const int row = i * MT + lrow, col = j * MT + 4 * grp;
-            const f32x4 y = finish<E>(acc[i][j], on[i], sr[i], s4);
-            const uint32_t lo = (uint32_t)f32_to_bf16(y[0]) | (uint32_t)f32_to_bf16(y[1]) << 16;
-            const uint32_t hi = (uint32_t)f32_to_bf16(y[2]) | (uint32_t)f32_to_bf16(y[3]) << 16;
-            *(uint2*)(stage_w + row * RB + (((col >> 3) ^ (row & (NCH - 1))) << 4) + (((col & 4) << 1) ^ (row & 8))) =
-                make_uint2(lo, hi);
+                for (int e = 0; e < 8; ++e)
+                    if (e < left) to[e] = (bf16_t)(v[e / 2] >> (16 * (e & 1)));
+            }
         }
-    }
-    // (one wavefront's own region: its LDS operations complete in order)
-    __builtin_amdgcn_s_waitcnt(0xc07f);
-    __builtin_amdgcn_wave_barrier();
-    const int ch = lane % NCH;
-    const int col = c0 + wc * WN + ch * 8, left = a.C - col;
-#pragma unroll
-    for (int p = 0; p < MB * MT / (64 / NCH); ++p) {
-        const int row = p * (64 / NCH) + lane / NCH;
-        const int r = 4 * MT * (row / MT) + wr * MT + row % MT;
-        u32x4 v = *(const u32x4*)(stage_w + row * RB + ((ch ^ (row & (NCH - 1))) << 4));
-        if (row & 8) v = u32x4{v[2], v[3], v[0], v[1]};
-        if (r >= t.rows) continue;
-        bf16_t* to = (bf16_t*)a.out + (int64_t)(t.row0 + r) * a.C + col;
-        if (left >= 8) {
-            store16<STREAM>(to, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < left) to[e] = (bf16_t)(v[e / 2] >> (16 * (e & 1)));
-        }
-    }
     };
     const int blocks = (t.rows + 4 * MT - 1) / (4 * MT);
     if (blocks == 4) run(std::integral_constant<int, 4>{});
