@@ -432,7 +432,7 @@ __device__ __forceinline__ void zero_tile(const MmArgs& a, const RowTile& t, int
 // int8 131072 x 2048 x 2048 1.8 POP/s, the library 1.83.)
 constexpr int BM = 256, BP = 256;
 constexpr int WM = 64, WN = 128;
-constexpr int MI = WM / MT, NJ = WN / MT;
+constexpr int NJ = WN / MT;
 constexpr int kThreads = 512;
 constexpr int kCopy = 4;                    // copies of 8 rows of either operand per wavefront and slice
 constexpr int kOperandB = 256 * kRowB;      // a stage of one operand
