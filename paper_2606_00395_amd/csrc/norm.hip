@@ -44,28 +44,6 @@ __device__ __forceinline__ uint32_t pack_scale(uint32_t m) {
     return e == 255 ? 255u : (uint32_t)max(e - 6, 1);
 }
 
-// (mean + eps)^-1/2 in two parts, so that y has one fp32 rounding before its own: a y that is rounded to the
-// other side is a whole step of act_dtype off, and may move its packed group's values by a step of theirs.
-struct Root {
-    float hi, lo;
-    bool one;               // no second part
-    // h r w
-    __device__ __forceinline__ float times(float h, float w) const {
-        if (one) return h * hi * w;
-        const float p = hi * w;
-        const float rest = __builtin_fmaf(lo, w, __builtin_fmaf(hi, w, -p));
-        return __builtin_fmaf(h, p, h * rest);
-    }
-};
-__device__ __forceinline__ Root root_of(double x) {
-    const float r0 = 1.0f / sqrtf((float)x);
-    // (sums past fp32's range, no number, or r w past the range where h r w is not)
-    if (!(r0 > 1e-18f && r0 < 1e18f)) return Root{r0, 0.0f, true};
-    const double a = (double)r0, r = a + 0.5 * a * __builtin_fma(-x * a, a, 1.0);       // a Newton step
-    const float hi = (float)r;
-    return Root{hi, (float)(r - (double)hi), false};
-}
-
 // STREAM: the rows are read past the caches.  AHEAD: a wavefront's next row is loaded one ahead.
 template <typename T, int NW, int F, bool STREAM, bool AHEAD>
 __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a) {
@@ -127,8 +105,11 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             part[i] = __float_as_uint(s);
         }
         const float sum = __uint_as_float(row_reduce<NW, P, P>(part, red, turn, AddF32()));
-        const Root root = root_of((double)sum * inv_d + (double)a.eps);
-        const float r = root.hi;
+        // The root and h r w in fp64, so that y has one fp32 rounding before its own (a y that is rounded to the
+        // other side is a whole step of act_dtype off, and may move its packed group's values by a step of
+        // theirs) and r w may lie anywhere.
+        const double root = rsqrt((double)sum * inv_d + (double)a.eps);
+        const float r = (float)root;
         // (behind the reduction: every element has been read, h may lie where x or the residual does)
         if (a.h) {
 #pragma unroll
@@ -170,7 +151,11 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             if (!g.any(i)) continue;
             float v[E];
 #pragma unroll
-            for (int j = 0; j < E; ++j) v[j] = root.times(h[i * E + j], w[i * E + j]);
+            for (int j = 0; j < E; ++j) {
+                float u = w[i * E + j];
+                asm volatile("" : "+v"(u));     // (widened here: two registers for each weight held else)
+                v[j] = (float)((double)h[i * E + j] * root * (double)u);
+            }
             const u32x4 out = Chunk<T>::close(v);
             if (a.y) g.store((T*)a.y + row * a.d, i, out);
             if (!a.scale) continue;
