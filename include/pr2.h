@@ -661,7 +661,7 @@ pr2_status pr2_swiglu_quant(int64_t R, int32_t m, int act_dtype, const void* au,
 /* ------------------------------------------------------------------------------------------
  * Root-mean-square norm in front of the layer, the residual's addition in the same pass.
  *   h = round(x + residual)  (the sum in fp32; x itself without residual),  r = (mean_i h_i^2 + eps)^(-1/2),
- *   y_i = round(h_i r w_i)                                  round: to act_dtype
+ *   y_i = round(h_i r w_i)                                  round: to act_dtype, of y through fp32
  *   x, residual [T, d] act_dtype; weight [d] fp32; residual may be NULL
  *   h_out [T, d], y [T, d] act_dtype; rstd_out [T] fp32 (what the backward call reads)
  *   q [T, d] int8 with scale [T, ceil(d / 32)] uint8: the packed form of y, the bits of pr2_act_pack
@@ -669,9 +669,10 @@ pr2_status pr2_swiglu_quant(int64_t R, int32_t m, int act_dtype, const void* au,
  *     fp32(h w) under pr2_act_quant and row_scale = r times its scale
  * Each output may be NULL, q goes with one of scale and row_scale.  h_out and y may lie on x or
  * residual (not both on the same); other overlaps are not allowed.  d <= 32768, T < 2^31, 16-byte
- * alignment of all but the fp32 tensors.  Sums in fp32: rows whose mean h^2 passes fp32's range
- * (magnitudes near 2^64) get r = 0.  A row's results have the same bits in any batch, and a NaN or an
- * infinity in a row reaches that row alone.  T = 0 is a no-op.
+ * alignment of all but the fp32 tensors.  The sum of squares, r and h r w are formed
+ * in fp64: y and rstd_out are the roundings of the exact values, also where the squares or r w pass
+ * fp32's range.  A row's results have the same bits in any batch, and a NaN or an infinity in a row
+ * reaches that row alone.  T = 0 is a no-op.
  */
 pr2_status pr2_rms_norm(int64_t T, int32_t d, int act_dtype, float eps, const void* x,
                         const void* residual, const float* weight, void* h_out, void* y,

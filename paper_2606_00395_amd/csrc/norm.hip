@@ -44,13 +44,26 @@ __device__ __forceinline__ uint32_t pack_scale(uint32_t m) {
     return e == 255 ? 255u : (uint32_t)max(e - 6, 1);
 }
 
+// Rounded to fp32, and never to bf16 in the same step (which a compiler that may contract makes of the two): bf16
+// results are rounded through fp32, as torch rounds a 64-bit value to bf16.
+__device__ __forceinline__ float to_f32(double v) {
+#pragma clang fp contract(off)
+    return (float)v;
+}
+// The same number, to be widened where it is used: the compiler else widens h and w ahead and holds them in twice the
+// registers (32 elements a lane with the next row's: 217 for 168).
+__device__ __forceinline__ float own_copy(float v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // STREAM: the rows are read past the caches.  AHEAD: a wavefront's next row is loaded one ahead.
 template <typename T, int NW, int F, bool STREAM, bool AHEAD>
 __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a) {
     using G = RowGroup<T, NW, F>;
     constexpr int E = G::E, P = G::kPieces;
     constexpr int kRows = NW == 1 ? 4 : 1;          // rows of a workgroup at a time
-    __shared__ uint32_t red[8 * NW * P];
+    __shared__ double red[8 * NW * P];
     int turn = 0;
     const int sub = NW == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
     const G g(a.d, NW == 1 ? threadIdx.x & 63 : threadIdx.x);
@@ -92,23 +105,24 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
                 raw[i] = Chunk<T>::close(h + i * E);        // the norm is taken of what h_out holds
             }
         }
-        uint32_t part[P];
+        // The squares (exact), their sum, the root and h r w in fp64, so that y is the definition's value with one fp32
+        // rounding before its own: from an fp32 sum a fifth of the fp32 y are a last place off, and a y that is
+        // rounded to the other side is a whole step of act_dtype off and may move a packed value by its step.
+        // Squares and r w may lie anywhere, too.
+        double square[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             Chunk<T>::open(raw[i], h + i * E);
-            float v[E], s = 0.0f;
+            float v[E];
+            double s = 0.0;
 #pragma unroll
             for (int j = 0; j < E; ++j) v[j] = h[i * E + j];
             g.mask(i, v);
 #pragma unroll
-            for (int j = 0; j < E; ++j) s += v[j] * v[j];
-            part[i] = __float_as_uint(s);
+            for (int j = 0; j < E; ++j) s = __builtin_fma((double)v[j], (double)v[j], s);
+            square[i] = s;
         }
-        const float sum = __uint_as_float(row_reduce<NW, P, P>(part, red, turn, AddF32()));
-        // The root and h r w in fp64, so that y has one fp32 rounding before its own (a y that is rounded to the
-        // other side is a whole step of act_dtype off, and may move its packed group's values by a step of
-        // theirs) and r w may lie anywhere.
-        const double root = rsqrt((double)sum * inv_d + (double)a.eps);
+        const double root = rsqrt(row_reduce<NW, P, P>(square, red, turn, AddF64()) * inv_d + (double)a.eps);
         const float r = (float)root;
         // (behind the reduction: every element has been read, h may lie where x or the residual does)
         if (a.h) {
@@ -118,6 +132,7 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
         if (a.rstd && g.lane == 0) a.rstd[row] = r;
         if (a.q && !a.scale) {
             // the row form: of h w, the row's r goes into its scale
+            uint32_t part[P];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
                 part[i] = 0;
@@ -125,7 +140,7 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
                 for (int j = 0; j < E; ++j)
                     part[i] = max(part[i], __float_as_uint(h[i * E + j] * w[i * E + j]) & 0x7fffffffu);
             }
-            const RowStep s = row_step(row_max<NW, P, P>(part, red, turn));
+            const RowStep s = row_step(row_max<NW, P, 2 * P>(part, (uint32_t*)red, turn));
             if (g.lane == 0) a.row_scale[row] = r * s.step;
 #pragma unroll
             for (int i = 0; i < P; ++i) {
@@ -152,9 +167,7 @@ __global__ void __launch_bounds__(NW == 16 ? 1024 : 256) norm_kernel(NormArgs a)
             float v[E];
 #pragma unroll
             for (int j = 0; j < E; ++j) {
-                float u = w[i * E + j];
-                asm volatile("" : "+v"(u));     // (widened here: two registers for each weight held else)
-                v[j] = (float)((double)h[i * E + j] * root * (double)u);
+                v[j] = to_f32((double)own_copy(h[i * E + j]) * root * (double)own_copy(w[i * E + j]));
             }
             const u32x4 out = Chunk<T>::close(v);
             if (a.y) g.store((T*)a.y + row * a.d, i, out);

@@ -83,17 +83,30 @@ template <int ctrl>
 __device__ __forceinline__ uint32_t from_lane(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, false);
 }
+template <int ctrl>
+__device__ __forceinline__ double from_lane(double v) {
+    return __hiloint2double((int)from_lane<ctrl>((uint32_t)__double2hiint(v)),
+                            (int)from_lane<ctrl>((uint32_t)__double2loint(v)));
+}
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ double of_lane(double v, int lane) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                            __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
 struct AddF32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const {
         return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
     }
 };
+struct AddF64 {
+    __device__ __forceinline__ double operator()(double a, double b) const { return a + b; }
+};
 struct MaxU32 {
     __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
 };
 // over 16 lanes, as a tree of neighbours
-template <typename Op>
-__device__ __forceinline__ uint32_t reduce16(uint32_t v, Op op) {
+template <typename V, typename Op>
+__device__ __forceinline__ V reduce16(V v, Op op) {
     v = op(v, from_lane<XOR1>(v));
     v = op(v, from_lane<XOR2>(v));
     v = op(v, from_lane<MIRROR8>(v));
@@ -103,14 +116,14 @@ __device__ __forceinline__ uint32_t reduce16(uint32_t v, Op op) {
 // Over a row of NW wavefronts with P pieces in each lane: every piece over its groups of 16 lanes, each
 // group's NW P pieces as a tree of neighbours in the row's order, then the four groups.  Pieces behind the
 // row's end are zeros, so the result does not depend on how many wavefronts and pieces hold the row: a
-// row's norm has the same bits in any batch.  `red` holds 8 NW MOST words (MOST: the most pieces of a
-// reduction in the kernel); `turn` alternates, so that one barrier is enough: the words of a turn are
-// written again only behind the next turn's barrier, which every wavefront reaches after it read them.
-template <int NW, int P, int MOST, typename Op>
-__device__ __forceinline__ uint32_t row_reduce(uint32_t (&v)[P], uint32_t* red, int& turn, Op op) {
+// row's norm has the same bits in any batch.  `red` holds 8 NW MOST values (MOST: the most pieces of a
+// reduction in the kernel, in values of this one's type); `turn` alternates, so that one barrier is enough: the values
+// of a turn are written again only behind the next turn's barrier, which every wavefront reaches after it read them.
+template <int NW, int P, int MOST, typename V, typename Op>
+__device__ __forceinline__ V row_reduce(V (&v)[P], V* red, int& turn, Op op) {
 #pragma unroll
     for (int i = 0; i < P; ++i) v[i] = reduce16(v[i], op);
-    uint32_t w;
+    V w;
     if (NW == 1) {
 #pragma unroll
         for (int n = 1; n < P; n *= 2)
@@ -119,7 +132,7 @@ __device__ __forceinline__ uint32_t row_reduce(uint32_t (&v)[P], uint32_t* red, 
         w = v[0];
     } else {
         constexpr int n = NW * P, M = n < 16 ? 1 : n / 16;      // pieces, and those that a lane joins
-        uint32_t* r = red + turn * (4 * NW * MOST);
+        V* r = red + turn * (4 * NW * MOST);
         turn ^= 1;
         const int group = (threadIdx.x & 63) >> 4, at = threadIdx.x & 15;
         if (at == 0) {
@@ -127,18 +140,16 @@ __device__ __forceinline__ uint32_t row_reduce(uint32_t (&v)[P], uint32_t* red, 
             for (int i = 0; i < P; ++i) r[4 * (i * NW + (threadIdx.x >> 6)) + group] = v[i];
         }
         __syncthreads();
-        uint32_t u[M];
+        V u[M];
 #pragma unroll
-        for (int m = 0; m < M; ++m) u[m] = at * M + m < n ? r[4 * (at * M + m) + group] : 0u;
+        for (int m = 0; m < M; ++m) u[m] = at * M + m < n ? r[4 * (at * M + m) + group] : V(0);
 #pragma unroll
         for (int q = 1; q < M; q *= 2)
 #pragma unroll
             for (int m = 0; m < M; m += 2 * q) u[m] = op(u[m], u[m + q]);
         w = reduce16(u[0], op);
     }
-    const uint32_t a = __builtin_amdgcn_readlane(w, 0), b = __builtin_amdgcn_readlane(w, 16);
-    const uint32_t c = __builtin_amdgcn_readlane(w, 32), d = __builtin_amdgcn_readlane(w, 48);
-    return op(op(a, b), op(c, d));
+    return op(op(of_lane(w, 0), of_lane(w, 16)), op(of_lane(w, 32), of_lane(w, 48)));
 }
 
 // the row's largest magnitude (bits), of its pieces'
