@@ -653,7 +653,7 @@ pr2_status pr2_grouped_mm_quant(const pr2_wgrad_desc* desc, const int8_t* q, con
  */
 pr2_status pr2_act_quant(int64_t R, int32_t C, int act_dtype, const void* x, int8_t* q,
                          float* row_scale, pr2_stream_t stream);
-/* The row form of silu(a) u (fp32, not rounded in between), au [R, 2m] as for pr2_swiglu_pack;
+/* The row form of a / (1 + exp(-a)) u (fp32 operations, to a few last places), au [R, 2m] as for pr2_swiglu_pack;
  * q [R, m]. */
 pr2_status pr2_swiglu_quant(int64_t R, int32_t m, int act_dtype, const void* au, int8_t* q,
                             float* row_scale, pr2_stream_t stream);
