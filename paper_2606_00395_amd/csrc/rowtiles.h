@@ -123,7 +123,8 @@ __device__ __forceinline__ bool find_tile(const int* offsets, int N, int R, int 
         which = tile - before;
         t->panel = (int)(in - (uint32_t)which * (uint32_t)panels);
     }
-    if (which < 0 || which >= n || t->panel >= panels) return false;    // (the same)
+    // (the same; a panel may be below 0 then, too)
+    if (which < 0 || which >= n || (uint32_t)t->panel >= (uint32_t)panels) return false;
     t->row0 = first + which * tile_rows;
     t->rows = min(tile_rows, last - t->row0);
     return true;
