@@ -31,7 +31,7 @@ __device__ __forceinline__ int lane_scan(int v) {
 // gives their places, and the lane that holds the item's tile hands it to the others.  That takes one
 // load's latency and no launch or workspace.  False: no item is left for this workgroup.  Offsets are
 // clamped into [0, R] and to rise, whatever they hold.  (N <= 1024; offsets null: one expert, all rows.)
-template <bool BY_PANEL = false, int BAND = 0>
+template <bool BY_PANEL = false>
 __device__ __forceinline__ bool find_tile(const int* offsets, int N, int R, int tile_rows, int panels,
                                           uint32_t block, RowTile* t) {
     const int lane = threadIdx.x & 63;
@@ -114,11 +114,6 @@ __device__ __forceinline__ bool find_tile(const int* offsets, int N, int R, int 
     if (BY_PANEL) {
         which = (int)(in % (uint32_t)n);
         t->panel = (int)(in / (uint32_t)n);
-    } else if (BAND) {
-        const uint32_t band = in / (uint32_t)(BAND * n), rest = in - band * (uint32_t)(BAND * n);
-        const uint32_t width = (uint32_t)min(BAND, panels - (int)band * BAND);
-        which = (int)(rest / width);
-        t->panel = (int)(band * BAND + rest - (uint32_t)which * width);
     } else {
         which = tile - before;
         t->panel = (int)(in - (uint32_t)which * (uint32_t)panels);
