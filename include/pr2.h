@@ -599,7 +599,8 @@ pr2_status pr2_weight_grad_packed(const pr2_wgrad_desc* desc, const void* dy, co
                                   size_t ws_bytes, pr2_stream_t stream);
 
 /*
- * The same from x itself: x [Rx, n_in] of dy's type, 16-byte aligned, in the place of (q, scale).
+ * The same from x itself: x [Rx, n_in] of dy's type, 16-byte aligned, in the place of (q, scale);
+ * dW apart from dy and x.
  * bf16: MFMA with fp32 accumulation; fp32: fp32 products and sums.  Same workspace.
  */
 pr2_status pr2_weight_grad(const pr2_wgrad_desc* desc, const void* dy, const void* x,

@@ -920,6 +920,9 @@ pr2_status weight_grad(const pr2_wgrad_desc* desc, bool packed, const void* dy, 
                         (long long)d.Rx);
         if ((uintptr_t)offsets % 4 || (uintptr_t)route_of_row % 4)
             return fail(PR2_ERR_ALIGN, "offsets or route_of_row is not 4-byte aligned");
+        const size_t a1 = d.act_dtype == PR2_BF16 ? 2 : 4, out = sizeof(float) * (size_t)d.N * d.n_out * d.n_in;
+        if (!packed && (share_memory(dW, out, dy, a1 * d.R * d.n_out) || share_memory(dW, out, x, a1 * d.Rx * d.n_in)))
+            return fail(PR2_ERR_SHAPE, "dW overlaps dy or x");
         const size_t need = wgrad_ws(d, nullptr).bytes;
         if (need && !ws) return fail(PR2_ERR_NULL, "ws is NULL (need %zu bytes)", need);
         if (ws_bytes < need)
