@@ -620,7 +620,8 @@ pr2_status pr2_weight_grad(const pr2_wgrad_desc* desc, const void* dy, const voi
  * they are terms of, no others.
  * Sums in fp32, one rounding to act_dtype at the end; bf16 products are exact.  N <= 1024, R and Rx
  * below 2^31 - 1024, n_out and n_in at most 2^20, N n_out n_in at most 2^36.  No workspace.  The same
- * call gives the same bits.
+ * call gives the same bits.  (Speed: rows of a multiple of 16 bytes, and tokens below 4 GiB where they are
+ * read through the plan, take the fast tiles; larger ones are better sorted first by pr2_dispatch.)
  */
 pr2_status pr2_grouped_mm(const pr2_wgrad_desc* desc, const void* x, const void* W,
                           const int32_t* offsets, const int32_t* route_of_row, void* out,
