@@ -254,14 +254,11 @@ __global__ void __launch_bounds__(back_threads<NW>()) norm_backward_kernel(NormB
         }
         w.r = a.rstd[row];
     };
-    // Sixteen wavefronts on one row: the next row's pieces are in flight meanwhile (3600 rows of 9000: 90 ->
-    // 68 us).  Smaller workgroups do that for each other, and the registers cost more than it gains (4000 of
-    // 8192: 54 -> 62).
-    Row cur, next;
-    if (NW == 16 && first < a.T) load(cur, first);
+    // (The next row's loads ahead hold twice the registers: on sixteen wavefronts they spill, 3600 rows of 9000 in 96 us
+    // for 65, 2000 fp32 rows of 12000 in 161 for 90, and on four it was slower, too.)
+    Row cur;
     for (int64_t row = first; row < a.T; row += stride) {
-        if (NW != 16) load(cur, row);
-        else if (row + stride < a.T) load(next, row + stride);
+        load(cur, row);
         const float r = cur.r;
         uint32_t part[P];
 #pragma unroll
@@ -300,7 +297,6 @@ __global__ void __launch_bounds__(back_threads<NW>()) norm_backward_kernel(NormB
             if (NW > 1) g.store_own((T*)a.dx + row * a.d, i, Chunk<T>::close(y));
             else g.store((T*)a.dx + row * a.d, i, Chunk<T>::close(y));
         }
-        if (NW == 16) cur = next;
     }
     if (!a.part) return;
     float* out = a.part + (int64_t)blockIdx.x * a.d;
