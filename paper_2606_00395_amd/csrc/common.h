@@ -94,22 +94,6 @@ __device__ __forceinline__ void dma16_at(const void* base, uint32_t off, const u
                  : "v"(off), "s"(base), "s"(m0)
                  : "memory", "m0");
 }
-// Both to an LDS address (lds_address): no pointer arithmetic or test per copy.
-__device__ __forceinline__ uint32_t lds_address(const unsigned char* p) {
-    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const lds_void*)p);
-}
-__device__ __forceinline__ void dma16_to(const void* src, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, off"
-                 :
-                 : "v"(src), "s"(to)
-                 : "memory", "m0");
-}
-__device__ __forceinline__ void dma16_to(const void* base, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 1\n\tglobal_load_lds_dwordx4 %0, %1"
-                 :
-                 : "v"(off), "s"(base), "s"(to)
-                 : "memory", "m0");
-}
 #pragma clang diagnostic pop
 
 // ------------------------------------------------------------ limits -----

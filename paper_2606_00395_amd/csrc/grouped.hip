@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "chunk.h"
+#include "copies.h"
 #include "rowtiles.h"
 
 namespace pr2 {

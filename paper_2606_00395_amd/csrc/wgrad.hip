@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "chunk.h"
+#include "copies.h"
 
 namespace pr2 {
 namespace {
